@@ -241,6 +241,123 @@ fp_status fp_generate(fp_layer* layer, const int32_t* prompt_ids, int32_t B, int
                       void* stream);
 
 /*
+ * Paged KV cache.  A serving profiler's requests are ragged: sequences of different
+ * lengths, prompts taken in chunks, a few drafted tokens checked at once.  These calls
+ * work on one layer's cache held in pages of page_size positions, which the caller
+ * allocates and hands out; the storage formats are those of the handle's own cache
+ * (FP_KV_BF16, or FP_KV_INT8 with one fp16 scale per position and kv head).
+ *
+ * Layout, ps = page_size, nkv = n_kv_heads, d = head_dim, e = bf16 or int8:
+ *   k [n_pages, nkv, ps, d] of e: rows of keys (after the rotary embedding);
+ *   v [n_pages, nkv, ps / 32, d, 32] of e: values transposed in blocks of 32 positions,
+ *     position t of a block in slot 8 ((t % 16) / 4) + 4 (t / 16) + t % 4 (the order in
+ *     which the attention kernels' probabilities leave the matrix cores);
+ *   k_scales, v_scales fp16 [n_pages, nkv, ps] (FP_KV_INT8; unused with FP_KV_BF16).
+ * page_size is a multiple of 32, up to 65536; head_dim 64 or 128; n_pages * nkv * (ps / 32)
+ * below 2^31.  Positions that no call has written may hold anything, NaN included: nothing
+ * reads them into a result.  A page may appear in several sequences' tables (a shared
+ * prefix) as long as no chunk writes it in two of them.
+ */
+typedef struct {
+    int32_t format;              /* fp_kv_quant */
+    int32_t n_pages, page_size, n_kv_heads, head_dim;
+    void* k;
+    void* v;
+    uint16_t* k_scales;
+    uint16_t* v_scales;
+} fp_paged_kv;
+
+/*
+ * A chunk: a ragged batch of rows (tokens) of n_seqs sequences.  Sequence b owns rows
+ * row_start[b] .. row_start[b + 1] - 1, none or several; row row_start[b] + i sits at
+ * position ctx_len[b] + i, and position p of sequence b lives in page
+ * table[b * table_stride + p / page_size] at offset p % page_size.  The three arrays are
+ * device int32 (row_start has n_seqs + 1 entries, not decreasing), read when the kernels
+ * run, so a captured call follows their later contents.  The host knows only the bounds:
+ *   n_rows   rows of the row buffers; rows from row_start[n_seqs] on belong to no sequence
+ *            and are left as they are
+ *   max_new  bound on a sequence's rows
+ *   max_len  bound on ctx_len[b] + rows of b, at most table_stride * page_size
+ * The bounds size the launches (tight ones are faster).  Contents that break them, or a page
+ * number outside [0, n_pages), are no error and touch no memory outside the buffers: rows
+ * beyond max_new are not computed, positions from max_len on are neither written nor read,
+ * and a missing page takes no writes and reads as zeros.
+ * 1 <= n_seqs <= 4096, 0 <= n_rows <= 2^24 (0: nothing to do), 1 <= max_new, max_len.
+ */
+typedef struct {
+    int32_t n_seqs, n_rows, max_new, max_len, table_stride;
+    const int32_t* row_start;
+    const int32_t* ctx_len;
+    const int32_t* table;
+} fp_chunk;
+
+/*
+ * Write a chunk's keys and values into the pages.  k, v: device bf16, row r's head h at
+ * k + r * kv_stride + h * head_dim (the stride in elements, so that k and v may be columns of
+ * one fused projection).  FP_KV_INT8: s = fp16(absmax / 127), code = rint(x / s) clamped to
+ * +-127 per (position, kv head), in fp32 with ties to even; a zero scale gives zero codes.
+ * With cos and sin (device fp32 [n_pos, head_dim / 2], n_pos >= max_len; both or neither)
+ * keys are first rotated by their position (rotate-half: i pairs with i + d / 2), in fp32.
+ * With q (then q_out, n_heads, a multiple of n_kv_heads of at most 16 times as many; and cos and
+ * sin) the queries are rotated in the same launch: q like k with q_stride, q_out device bf16
+ * [n_rows, n_heads, head_dim], not overlapping q.  Pointers and strides are multiples of 16 bytes.
+ */
+fp_status fp_kv_append(const fp_paged_kv* kv, const fp_chunk* chunk, const void* k, const void* v, int64_t kv_stride,
+                       const void* q, int64_t q_stride, int32_t n_heads, void* q_out, const float* cos_t,
+                       const float* sin_t, int32_t n_pos, void* stream);
+
+/*
+ * Read positions back: row r of k_out and v_out (device bf16 [n_rows, n_kv_heads, head_dim],
+ * 16-byte aligned) receives the key and value at row r's position; int8: bf16(code * scale).
+ * With ctx_len zero and row_start the running sum of the lengths, whole sequences.
+ */
+fp_status fp_kv_read(const fp_paged_kv* kv, const fp_chunk* chunk, void* k_out, void* v_out, void* stream);
+
+/*
+ * Attention of a chunk over the cache, causal: out[r, h] = sum_j p_j v_j over the positions
+ * j = 0 .. (row r's position) of r's sequence, p = softmax(scale * q[r, h] . k_j), kv head
+ * h * n_kv_heads / n_heads.  The chunk's own keys and values are read from the pages too:
+ * append first.  q: device bf16, row r's head h at q + r * q_stride + h * head_dim; out: device
+ * bf16 [n_rows, n_heads, head_dim]; both 16-byte aligned.  Query group n_heads / n_kv_heads from
+ * 1 to 16.  Sums and softmax statistics are fp32; probabilities enter the product with V as bf16.
+ * workspace: device memory of at least fp_attn_chunk_workspace bytes, 16-byte aligned, which
+ * the call may use until the stream has passed it (calls that can overlap need one each).
+ * FP_ERR_CAPACITY if workspace_bytes is less.
+ */
+fp_status fp_attn_chunk_workspace(const fp_paged_kv* kv, const fp_chunk* chunk, int32_t n_heads, size_t* bytes);
+fp_status fp_attn_chunk(const fp_paged_kv* kv, const fp_chunk* chunk, const void* q, int64_t q_stride, int32_t n_heads,
+                        float scale, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Decide over drafted tokens.  Sequence b owns rows row_start[b] .. row_start[b + 1] - 1 of the
+ * target's logits (fp32 [n_rows, vocab], row_stride elements apart): row i of it gives the
+ * distribution p_i = softmax(logits / temperature) of the token after i accepted drafts.
+ * draft_ids[row i] is the drafted token that row i judges (the last row judges none: its entry
+ * is not read), drawn from q_i = draft_probs[row i] (fp32 [n_rows, vocab] of draft_stride; NULL:
+ * q_i is one at the drafted token).  Drafts are taken in order: x_i is accepted if
+ *   u[row i] * q_i(x_i) < p_i(x_i);
+ * the first refused one is replaced by a token drawn from max(0, p_i - q_i) (from p_i if that
+ * is zero everywhere), and after the last accepted one a token is drawn from the last row's p.  A
+ * draw takes the lowest id whose running sum exceeds u_last[b] times the total.  The numbers u
+ * and u_last are uniform in [0, 1), the caller's.  All sums and comparisons are in 64 bits.
+ * temperature 0: x_i is accepted if it is the row's argmax (the lowest id among equal ones),
+ * and the last token is an argmax (u, u_last and draft_probs are not read; may be NULL).
+ * out_ids: device int32 [n_seqs, max_rows], sequence b's accepted tokens and then the drawn one,
+ * -1 behind; n_out: device int32 [n_seqs], their number (1 .. its rows; a sequence without rows
+ * gives 0).  -inf and NaN logits have probability zero; +inf ones share it all.  A row with
+ * nothing else gives token -1.  A draft outside [0, vocab) has probability zero; negative and
+ * NaN draft probabilities count as zero.
+ * row_start: device int32 [n_seqs + 1], not decreasing, entries past n_rows or sequences of more
+ * than max_rows rows are cut.  1 <= n_seqs <= 4096, 0 <= n_rows <= 65535, 1 <= max_rows <= 64,
+ * 1 <= vocab <= 2^20, finite temperature >= 0.
+ */
+fp_status fp_verify_draft_workspace(int32_t n_seqs, int32_t n_rows, int32_t vocab, size_t* bytes);
+fp_status fp_verify_draft(const float* logits, int64_t row_stride, int32_t n_seqs, int32_t n_rows, int32_t max_rows,
+                          int32_t vocab, const int32_t* row_start, const int32_t* draft_ids, const float* draft_probs,
+                          int64_t draft_stride, const float* u, const float* u_last, float temperature,
+                          int32_t* out_ids, int32_t* n_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Latency and memory estimation from fingerprints (host arithmetic, no device).
  *
  * Eq. 1 (Sec. 5.3): latency = TTFT + output_length * TPOT.  fp_fit_ttft_tpot solves the

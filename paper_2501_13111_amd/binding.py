@@ -101,6 +101,13 @@ def load(path: str | None = None):
         "fp_extrapolate_layers": [ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_double), i32,
                                   ctypes.POINTER(ctypes.c_double)],
         "fp_device_memory": [ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t)],
+        "fp_kv_append": [vp, vp, vp, vp, i64, vp, i64, i32, vp, vp, vp, i32, vp],
+        "fp_kv_read": [vp, vp, vp, vp, vp],
+        "fp_attn_chunk_workspace": [vp, vp, i32, ctypes.POINTER(ctypes.c_size_t)],
+        "fp_attn_chunk": [vp, vp, vp, i64, i32, ctypes.c_float, vp, vp, ctypes.c_size_t, vp],
+        "fp_verify_draft_workspace": [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
+        "fp_verify_draft": [vp, i64, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, ctypes.c_float, vp, vp, vp,
+                            ctypes.c_size_t, vp],
     }
     for name, args in sig.items():
         f = getattr(L, name)

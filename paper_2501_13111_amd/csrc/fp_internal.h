@@ -259,6 +259,66 @@ int head_logit_blocks(int V);
 hipError_t launch_logits_argmax(const float* part, int ks, int B, int V, float* logits, float* bval, int* bidx,
                                 int* out_ids, hipStream_t st);
 
+// Paged cache (paged.hip).  ks fp32 partials pstride apart are summed by the append when its
+// launch says f32 (the layer stack's own qkv projection), else inputs are bf16.
+struct KvAppendArgs {
+    fp_paged_kv kv;
+    fp_chunk chunk;
+    const void* k;
+    const void* v;
+    const void* q;            // NULL: keys and values only
+    int64_t kv_stride, q_stride;   // elements per row
+    int ks;
+    int64_t pstride;
+    int n_heads;
+    uint16_t* q_out;          // bf16 [n_rows, n_heads, d]
+    const float* cos_t;       // NULL: keys arrive rotated
+    const float* sin_t;
+};
+struct KvReadArgs {
+    fp_paged_kv kv;
+    fp_chunk chunk;
+    uint16_t* k_out;
+    uint16_t* v_out;
+};
+hipError_t launch_kv_append(const KvAppendArgs& a, bool f32, hipStream_t st);
+hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st);
+
+// Attention of a chunk over the paged cache (attn_chunk.hip).
+struct AttnChunkArgs {
+    fp_paged_kv kv;
+    fp_chunk chunk;
+    const uint16_t* q;        // bf16
+    int64_t q_stride;
+    int n_heads;
+    float scale;
+    uint16_t* out;            // [n_rows, n_heads, d], activation format out_fmt
+    int out_fmt;
+    float* ws;
+    int target, min_blocks;   // set by the launcher: see attn_chunk.hip
+};
+size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads);
+hipError_t launch_attn_chunk(const AttnChunkArgs& a, hipStream_t st);
+
+// Verification of drafted tokens (verify.hip).
+struct VerifyArgs {
+    const float* logits;
+    int64_t row_stride;
+    int n_seqs, n_rows, max_rows, V;
+    const int* row_start;
+    const int* draft_ids;
+    const float* draft_probs;
+    int64_t draft_stride;
+    const float* u;
+    const float* u_last;
+    double inv_t;             // 1 / temperature; 0: greedy
+    int* out_ids;
+    int* n_out;
+    void* ws;
+};
+size_t verify_ws_bytes(int n_seqs, int n_rows, int V);
+hipError_t launch_verify(const VerifyArgs& a, hipStream_t st);
+
 // Whether a single decode step launches its inner layers as one graph.
 bool decode_step_inner_graph(int n_layers, bool single, size_t layer_bytes);
 

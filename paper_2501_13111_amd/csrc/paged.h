@@ -1,0 +1,62 @@
+// Device helpers of the paged-cache kernels: a chunk's sequences, the search for a workgroup's
+// share among them, and the pool's 32-position blocks.
+#pragma once
+#include "fp_device.h"
+
+namespace fpk {
+
+// A sequence of a chunk with the chunk's bounds enforced: whatever the device arrays hold, rows
+// lie in [0, n_rows), new rows are at most max_new and positions end at max_len.
+struct Seq {
+    int row0, n, ctx, len;       // first row, rows, position of the first row, positions held
+};
+__device__ __forceinline__ Seq load_seq(const fp_chunk& c, int b) {
+    const int r0 = min(max(c.row_start[b], 0), c.n_rows), r1 = min(max(c.row_start[b + 1], 0), c.n_rows);
+    Seq s;
+    s.row0 = r0;
+    s.ctx = min(max(c.ctx_len[b], 0), c.max_len);
+    s.n = min(min(max(r1 - r0, 0), c.max_new), c.max_len - s.ctx);
+    s.len = s.ctx + s.n;
+    return s;
+}
+
+// Inclusive sum over the wave's lanes.
+__device__ __forceinline__ int wave_scan(int v) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int t = __shfl_up(v, o, 64);
+        if (lane >= o) v += t;
+    }
+    return v;
+}
+
+// The sequence b whose units (count(b) of them, in sequence order) include unit u, with u
+// counted from b's first: b, or -1 past the last unit.  Every lane of the wave gets the answer.
+template <class F>
+__device__ __forceinline__ int find_seq(int n_seqs, int& u, F count) {
+    const int lane = threadIdx.x & 63;
+    for (int b0 = 0; b0 < n_seqs; b0 += 64) {
+        const int c = b0 + lane < n_seqs ? count(b0 + lane) : 0;
+        const int s = wave_scan(c);
+        const uint64_t past = __ballot(s > u);
+        if (past) {
+            const int l = __builtin_ctzll(past);
+            u -= __builtin_amdgcn_readlane(s - c, l);
+            return b0 + l;
+        }
+        u -= __builtin_amdgcn_readlane(s, 63);
+    }
+    return -1;
+}
+
+// The pool's block index of block blk (32 positions) of sequence b for kv head kvh: blocks of
+// one (page, kv head) are consecutive.  -1 for a missing page.
+__device__ __forceinline__ int pool_block(const fp_paged_kv& kv, const fp_chunk& c, int b, int kvh, int blk) {
+    const int bpp = kv.page_size / VT_BLK;
+    const int i = blk / bpp;
+    const int page = i < c.table_stride ? c.table[(int64_t)b * c.table_stride + i] : -1;
+    return page >= 0 && page < kv.n_pages ? (page * kv.n_kv_heads + kvh) * bpp + blk % bpp : -1;
+}
+
+}  // namespace fpk

@@ -1,0 +1,267 @@
+// Writing a chunk's keys and values into a paged cache (with the rotary embedding and the int8
+// quantisation of the handle's own cache), and reading positions back.
+//
+// Both kernels take one workgroup per (32-position block touched, kv head): a block of values is
+// transposed in the cache ([d][32 slots]), so it passes through LDS and moves in 16-byte pieces on
+// both sides.  A thread holds eight dims of a position's lower half and the eight they are rotated
+// with; the 8 (d = 64: 4) threads of a position find its largest magnitude by shuffles.  In an
+// append the workgroup also rotates the queries of its kv head's group for the block's positions,
+// whose cosines and sines it has just read.  Bound by memory: a long chunk's rows move once in, once
+// out.
+#include "paged.h"
+
+namespace fpk {
+
+namespace {
+
+constexpr int T = 256;
+
+// 32-position blocks that the sequence's rows touch
+__device__ __forceinline__ int seq_blocks(const Seq& s) {
+    return s.n > 0 ? (s.len - 1) / VT_BLK - s.ctx / VT_BLK + 1 : 0;
+}
+
+__device__ __forceinline__ void unpack8(u32x4 v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
+    return u32x4{pack_bf16_hw(x[0], x[1]), pack_bf16_hw(x[2], x[3]), pack_bf16_hw(x[4], x[5]), pack_bf16_hw(x[6], x[7])};
+}
+
+// Eight values at p: bf16, or the sum of ks fp32 partials pstride apart, in increasing order.
+template <bool F32>
+__device__ __forceinline__ void load8(const void* base, int64_t off, int ks, int64_t pstride, float (&x)[8]) {
+    if constexpr (F32) {
+        const float* p = (const float*)base + off;
+        f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll 4
+        for (int s = 1; s < ks; ++s) {
+            a += *(const f32x4*)(p + s * pstride);
+            b += *(const f32x4*)(p + s * pstride + 4);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[i] = a[i];
+            x[4 + i] = b[i];
+        }
+    } else {
+        unpack8(*(const u32x4*)((const uint16_t*)base + off), x);
+    }
+}
+
+__device__ __forceinline__ int8_t code8(float x, float s) {
+    return s == 0.f ? (int8_t)0 : (int8_t)(int)fminf(fmaxf(rintf(__fdiv_rn(x, s)), -127.f), 127.f);
+}
+__device__ __forceinline__ u32x2 codes8(const float (&x)[8], float s) {
+    uint32_t w[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)(uint8_t)code8(x[i], s) << (8 * (i & 3));
+    return u32x2{w[0], w[1]};
+}
+
+// contraction off: products and sums are rounded one by one, as the definition's fp32 says
+#pragma clang fp contract(off)
+__device__ __forceinline__ void rotate8(float (&lo)[8], float (&hi)[8], const float* c, const float* s) {
+    const f32x4 c0 = *(const f32x4*)c, c1 = *(const f32x4*)(c + 4), s0 = *(const f32x4*)s, s1 = *(const f32x4*)(s + 4);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float cc = i < 4 ? c0[i & 3] : c1[i & 3], ss = i < 4 ? s0[i & 3] : s1[i & 3];
+        float l, h;
+        rotate_pair(lo[i], hi[i], cc, ss, l, h);
+        lo[i] = l;
+        hi[i] = h;
+    }
+}
+
+template <int D, bool KV8, bool F32>
+__global__ void __launch_bounds__(T) kv_append_paged_kernel(KvAppendArgs a) {
+    constexpr int HALF = D / 2, NP = HALF / 8;             // threads per position
+    constexpr int ES = KV8 ? 1 : 2;
+    constexpr int VS = VT_BLK * ES + 16;                   // LDS bytes per value dim
+    __shared__ __attribute__((aligned(16))) char vt[D * VS];
+    const int tid = threadIdx.x;
+    const int kvh = blockIdx.x % a.kv.n_kv_heads;
+    int u = blockIdx.x / a.kv.n_kv_heads;
+    const int b = find_seq(a.chunk.n_seqs, u, [&](int i) { return seq_blocks(load_seq(a.chunk, i)); });
+    if (b < 0) return;
+    const Seq sq = load_seq(a.chunk, b);
+    const int blk = sq.ctx / VT_BLK + u;
+    const int t0 = max(sq.ctx - blk * VT_BLK, 0), t1 = min(sq.len - blk * VT_BLK, VT_BLK);   // live positions
+    const int np = t1 - t0;
+    const int pb = pool_block(a.kv, a.chunk, b, kvh, blk);
+    const int row0 = sq.row0 + blk * VT_BLK + t0 - sq.ctx;
+    const int G = a.q != nullptr ? a.n_heads / a.kv.n_kv_heads : 0;
+
+    for (int it = tid; it < (2 + G) * np * NP; it += T) {
+        const int what = it / (np * NP), r = it % (np * NP);
+        const int i = r / NP, j = 8 * (r % NP);
+        const int t = t0 + i, pos = blk * VT_BLK + t;
+        const int64_t row = row0 + i;
+        const int h = what < 2 ? kvh : kvh * G + what - 2;
+        const void* src = what == 0 ? a.k : what == 1 ? a.v : a.q;
+        const int64_t off = row * (what < 2 ? a.kv_stride : a.q_stride) + (int64_t)h * D + j;
+        float lo[8], hi[8];
+        load8<F32>(src, off, a.ks, a.pstride, lo);
+        load8<F32>(src, off + HALF, a.ks, a.pstride, hi);
+        if (what != 1 && a.cos_t != nullptr)
+            rotate8(lo, hi, a.cos_t + (int64_t)pos * HALF + j, a.sin_t + (int64_t)pos * HALF + j);
+        if (what >= 2) {
+            uint16_t* q = a.q_out + (row * a.n_heads + h) * D + j;
+            *(u32x4*)q = pack8(lo);
+            *(u32x4*)(q + HALF) = pack8(hi);
+            continue;
+        }
+        float sc = 0.f;
+        if constexpr (KV8) {
+            float m = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m = fmaxf(m, fmaxf(fabsf(lo[e]), fabsf(hi[e])));
+#pragma unroll
+            for (int o = 1; o < NP; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, NP));
+            const uint16_t sh = f2h(__fdiv_rn(m, 127.0f));
+            sc = h2f(sh);
+            if (j == 0 && pb >= 0) (what == 0 ? a.kv.k_scales : a.kv.v_scales)[(int64_t)pb * VT_BLK + t] = sh;
+        }
+        if (what == 0) {
+            if (pb < 0) continue;
+            char* dst = (char*)a.kv.k + ((int64_t)pb * VT_BLK + t) * D * ES;
+            if constexpr (KV8) {
+                *(u32x2*)(dst + j) = codes8(lo, sc);
+                *(u32x2*)(dst + j + HALF) = codes8(hi, sc);
+            } else {
+                *(u32x4*)(dst + 2 * j) = pack8(lo);
+                *(u32x4*)(dst + 2 * (j + HALF)) = pack8(hi);
+            }
+        } else {
+            const int slot = vt_slot(t);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if constexpr (KV8) {
+                    *(int8_t*)(vt + (j + e) * VS + slot) = code8(lo[e], sc);
+                    *(int8_t*)(vt + (j + e + HALF) * VS + slot) = code8(hi[e], sc);
+                } else {
+                    *(__bf16*)(vt + (j + e) * VS + 2 * slot) = (__bf16)lo[e];
+                    *(__bf16*)(vt + (j + e + HALF) * VS + 2 * slot) = (__bf16)hi[e];
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (pb < 0) return;
+    // values: 16-byte pieces of 16 / ES slots where every position is the chunk's, else element by
+    // element (the block's other positions are earlier tokens')
+    char* dst = (char*)a.kv.v + (int64_t)pb * D * VT_BLK * ES;
+    if (np == VT_BLK) {
+        constexpr int PD = VT_BLK * ES / 16;               // pieces per dim
+        for (int it = tid; it < D * PD; it += T)
+            *(u32x4*)(dst + 16 * it) = *(const u32x4*)(vt + it / PD * VS + it % PD * 16);
+    } else {
+        for (int it = tid; it < D * np; it += T) {
+            const int dim = it / np, slot = vt_slot(t0 + it % np);
+            if constexpr (KV8) dst[dim * VT_BLK + slot] = vt[dim * VS + slot];
+            else *(uint16_t*)(dst + 2 * (dim * VT_BLK + slot)) = *(const uint16_t*)(vt + dim * VS + 2 * slot);
+        }
+    }
+}
+#pragma clang fp contract(on)
+
+template <int D, bool KV8>
+__global__ void __launch_bounds__(T) kv_read_paged_kernel(KvReadArgs a) {
+    constexpr int NP = D / 8, ES = KV8 ? 1 : 2, PD = VT_BLK * ES / 16;
+    constexpr int VS = VT_BLK * ES + 16;
+    __shared__ __attribute__((aligned(16))) char vt[D * VS];
+    const int tid = threadIdx.x;
+    const int kvh = blockIdx.x % a.kv.n_kv_heads;
+    int u = blockIdx.x / a.kv.n_kv_heads;
+    const int b = find_seq(a.chunk.n_seqs, u, [&](int i) { return seq_blocks(load_seq(a.chunk, i)); });
+    if (b < 0) return;
+    const Seq sq = load_seq(a.chunk, b);
+    const int blk = sq.ctx / VT_BLK + u;
+    const int t0 = max(sq.ctx - blk * VT_BLK, 0), t1 = min(sq.len - blk * VT_BLK, VT_BLK);
+    const int np = t1 - t0;
+    const int pb = pool_block(a.kv, a.chunk, b, kvh, blk);
+    const int64_t row0 = sq.row0 + blk * VT_BLK + t0 - sq.ctx;
+    const int64_t prow = (int64_t)pb * VT_BLK;
+    if (pb >= 0) {
+        const u32x4* src = (const u32x4*)((const char*)a.kv.v + (int64_t)pb * D * VT_BLK * ES);
+        for (int it = tid; it < D * PD; it += T) *(u32x4*)(vt + it / PD * VS + it % PD * 16) = src[it];
+    }
+    __syncthreads();
+    for (int it = tid; it < 2 * np * NP; it += T) {
+        const int i = it % (np * NP) / NP, j = 8 * (it % NP), t = t0 + i;
+        const bool val = it >= np * NP;
+        uint16_t* dst = (val ? a.v_out : a.k_out) + ((row0 + i) * a.kv.n_kv_heads + kvh) * D + j;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        if (pb >= 0) {
+            const int slot = vt_slot(t);
+            if constexpr (KV8) {
+                const float s = h2f((val ? a.kv.v_scales : a.kv.k_scales)[prow + t]);
+                const u32x2 c = *(const u32x2*)((const int8_t*)a.kv.k + (prow + t) * D + j);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int8_t q = val ? *(const int8_t*)(vt + (j + e) * VS + slot)
+                                         : (int8_t)((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
+                    x[e] = (float)q * s;
+                }
+            } else if (val) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = (float)*(const __bf16*)(vt + (j + e) * VS + 2 * slot);
+            } else {
+                unpack8(*(const u32x4*)((const uint16_t*)a.kv.k + (prow + t) * D + j), x);
+            }
+        }
+        *(u32x4*)dst = pack8(x);
+    }
+}
+
+// workgroups for the blocks that n_rows rows of n_seqs sequences can touch: a sequence's n rows
+// touch at most (n + 30) / 32 + 1, and never more than n
+int64_t max_blocks(const fp_chunk& c) {
+    return std::min<int64_t>(c.n_rows, (int64_t)c.n_rows / VT_BLK + 2 * (int64_t)c.n_seqs);
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvAppendArgs& a, bool f32, hipStream_t st) {
+    const int64_t n = max_blocks(a.chunk) * a.kv.n_kv_heads;
+    if (n < 1 || n > INT_MAX) return hipErrorInvalidValue;
+    const bool i8 = a.kv.format == FP_KV_INT8;
+#define FP_AP(D, I8, F32) FP_LAUNCH((kv_append_paged_kernel<D, I8, F32>), dim3((unsigned)n), dim3(T), 0, st, a)
+#define FP_AP_D(D)                                                                   \
+    do {                                                                             \
+        if (f32) { if (i8) FP_AP(D, true, true); else FP_AP(D, false, true); }       \
+        else { if (i8) FP_AP(D, true, false); else FP_AP(D, false, false); }         \
+    } while (0)
+    if (a.kv.head_dim == 128) FP_AP_D(128);
+    else if (a.kv.head_dim == 64) FP_AP_D(64);
+    else return hipErrorInvalidValue;
+#undef FP_AP_D
+#undef FP_AP
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st) {
+    const int64_t n = max_blocks(a.chunk) * a.kv.n_kv_heads;
+    if (n < 1 || n > INT_MAX) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)n);
+    const bool i8 = a.kv.format == FP_KV_INT8;
+    if (a.kv.head_dim == 128) {
+        if (i8) FP_LAUNCH((kv_read_paged_kernel<128, true>), grid, dim3(T), 0, st, a);
+        else FP_LAUNCH((kv_read_paged_kernel<128, false>), grid, dim3(T), 0, st, a);
+    } else if (a.kv.head_dim == 64) {
+        if (i8) FP_LAUNCH((kv_read_paged_kernel<64, true>), grid, dim3(T), 0, st, a);
+        else FP_LAUNCH((kv_read_paged_kernel<64, false>), grid, dim3(T), 0, st, a);
+    } else {
+        return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace fpk
