@@ -20,42 +20,13 @@
 // The plan depends on the inputs alone, so results repeat bit for bit.
 #include <climits>
 
-#include "paged.h"
+#include <type_traits>
+
+#include "attn_plan.h"
 
 namespace fpk {
 
 namespace {
-
-// pieces a call aims for: enough waves to keep every CU's loads in flight
-constexpr int TARGET = 768;
-constexpr int MINB = 16;                   // blocks per piece at least: four per wave
-
-struct Plan {
-    int tiles, blocks, pieces;             // row tiles, 32-key blocks, pieces per tile
-};
-__device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int RT, int Q) {
-    Plan p;
-    p.tiles = (s.n * G + RT - 1) / RT;
-    p.blocks = s.n > 0 ? (s.len + VT_BLK - 1) / VT_BLK : 0;
-    p.pieces = (p.blocks + Q - 1) / Q;
-    return p;
-}
-// Blocks per piece: from the total over all sequences.
-__device__ __forceinline__ int plan_q(const AttnChunkArgs& a, int G, int RT) {
-    const int lane = threadIdx.x & 63;
-    int64_t total = 0;
-    for (int b = lane; b < a.chunk.n_seqs; b += 64) {
-        const Seq s = load_seq(a.chunk, b);
-        const Plan p = plan_seq(s, G, RT, 1);
-        total += (int64_t)p.tiles * p.blocks;
-    }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o, 64);
-    total = (total * a.kv.n_kv_heads + a.target - 1) / a.target;
-    return (int)std::max<int64_t>(a.min_blocks, std::min<int64_t>(total, 1 << 24));
-}
-
-constexpr int wst(int D) { return D + 4; }     // floats per row of a piece: o, then m, l
 
 template <int D, bool KV8>
 struct Chunk {
@@ -81,7 +52,7 @@ __device__ __forceinline__ u32x4 i8x8_to_bf16(uint32_t lo, uint32_t hi) {
 }
 
 template <int D, bool KV8, int NT>
-__global__ void __launch_bounds__(256, 2) attn_chunk_kernel(AttnChunkArgs a) {
+__global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnChunkArgs a) {
     constexpr int NJ = D / 32, ND = D / 16, RT = 16 * NT;
     constexpr int NK = Chunk<D, KV8>::NK;
     constexpr int RS = D + 4;
@@ -92,36 +63,11 @@ __global__ void __launch_bounds__(256, 2) attn_chunk_kernel(AttnChunkArgs a) {
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
-    const int Q = plan_q(a, G, RT);
-    int u = blockIdx.x, part = 0;                // part: pieces of split tiles before this one
-    int b = -1;
-    {
-        int u2 = u;
-        b = find_seq(a.chunk.n_seqs, u2, [&](int i) {
-            const Plan p = plan_seq(load_seq(a.chunk, i), G, RT, Q);
-            return p.tiles * p.pieces * nkv;
-        });
-        if (b < 0) return;
-        // split pieces of the sequences before b
-        for (int i = lane; i < b; i += 64) {
-            const Plan p = plan_seq(load_seq(a.chunk, i), G, RT, Q);
-            if (p.pieces > 1) part += p.tiles * p.pieces * nkv;
-        }
-#pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) part += __shfl_xor(part, o, 64);
-        u = u2;
-    }
-    const Seq sq = load_seq(a.chunk, b);
-    const Plan pl = plan_seq(sq, G, RT, Q);
-    if (u < 0 || u >= pl.tiles * pl.pieces * nkv) return;      // overlapping rows: sums past int32
-    part += u;
-    // piece -> (kv head, piece of the keys, row tile)
-    const int rt = u % pl.tiles, sp = u / pl.tiles % pl.pieces, kvh = u / (pl.tiles * pl.pieces);
-    const int row0 = rt * RT, rows = min(RT, sq.n * G - row0);
-    // blocks: the piece's share, no further than the tile's last row sees
-    const int tblocks = (sq.ctx + (row0 + rows - 1) / G) / VT_BLK + 1;
-    const int per = (pl.blocks + pl.pieces - 1) / pl.pieces;
-    const int beg = sp * per, end = min(min(beg + per, pl.blocks), tblocks);
+    Unit un;
+    if (!find_unit<false, false>(a, G, RT, un)) return;
+    const Seq& sq = un.sq;
+    const int b = un.b, kvh = un.kvh, beg = un.beg, end = un.end;
+    const int row0 = un.rt * RT, rows = min(RT, sq.n * G - row0);
 
     // queries: column c of tile t is row row0 + 16 t + c
     u32x4 qf[NT][NJ];
@@ -189,7 +135,7 @@ __global__ void __launch_bounds__(256, 2) attn_chunk_kernel(AttnChunkArgs a) {
 
     auto compute = [&](int i, Chunk<D, KV8>& c) {
         const int base = (beg + w + 4 * i) * VT_BLK;
-        float ksc[2][4], vsc[2][4];
+        float ksc[2][4], vsc[2][4], lk = 0.f;
         if constexpr (KV8) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -220,6 +166,16 @@ __global__ void __launch_bounds__(256, 2) attn_chunk_kernel(AttnChunkArgs a) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) vsc[t][e] = 16 * t + 4 * g + e < nk ? vsc[t][e] : 0.f;
             }
+        }
+        if constexpr (KV8) {                     // log2 of the block's largest value scale
+            float m = 5.9604645e-8f;             // 2^-24, the least fp16
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, vsc[t][e]);
+            m = fmaxf(m, __shfl_xor(m, 16, 64));
+            m = fmaxf(m, __shfl_xor(m, 32, 64));
+            lk = __builtin_amdgcn_logf(m);
         }
         u32x4 kf[2][NJ];
 #pragma unroll
@@ -253,7 +209,7 @@ __global__ void __launch_bounds__(256, 2) attn_chunk_kernel(AttnChunkArgs a) {
             }
             mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float m_new = fmaxf(m_run[q], mx);
+            const float m_new = fmaxf(m_run[q], mx + lk);
             const float ms = m_new == -INFINITY ? 0.f : m_new;        // nothing seen yet: all zero
             al[q] = __builtin_amdgcn_exp2f(m_run[q] - ms);
             m_run[q] = m_new;
@@ -268,8 +224,8 @@ __global__ void __launch_bounds__(256, 2) attn_chunk_kernel(AttnChunkArgs a) {
                     ps += p[e];
                     if constexpr (KV8) p[e] *= vsc[t][e];
                 }
-                pw[2 * t] = pack_bf16_hw(p[0], p[1]);
-                pw[2 * t + 1] = pack_bf16_hw(p[2], p[3]);
+                pw[2 * t] = KV8 ? pack_f16_hw(p[0], p[1]) : pack_bf16_hw(p[0], p[1]);
+                pw[2 * t + 1] = KV8 ? pack_f16_hw(p[2], p[3]) : pack_bf16_hw(p[2], p[3]);
             }
             l_run[q] = l_run[q] * al[q] + ps;     // this lane's keys; the lane groups join at the end
             pf[q] = u32x4{pw[0], pw[1], pw[2], pw[3]};
@@ -277,21 +233,36 @@ __global__ void __launch_bounds__(256, 2) attn_chunk_kernel(AttnChunkArgs a) {
 #pragma unroll
         for (int dd = 0; dd < ND; ++dd) {
             u32x4 vf;
-            if constexpr (KV8) vf = i8x8_to_bf16(c.v[dd].x, c.v[dd].y);
-            else vf = c.v[dd];
+            if constexpr (KV8) {
+                const u32x2 c0 = i8x4_to_f16x4(c.v[dd].x), c1 = i8x4_to_f16x4(c.v[dd].y);
+                vf = u32x4{c0.x, c0.y, c1.x, c1.y};
+            } else {
+                vf = c.v[dd];
+            }
 #pragma unroll
             for (int q = 0; q < NT; ++q) {
                 oacc[q][dd] *= al[q];
-                oacc[q][dd] = mfma_bf16(vf, pf[q], oacc[q][dd]);
+                oacc[q][dd] = mfma16<KV8 ? ACT_F16 : ACT_BF16>(vf, pf[q], oacc[q][dd]);
             }
         }
     };
 
-    for (int i = 0; i < n; ++i) {
-        if ((i & 63) == 0) pages(i);
-        Chunk<D, KV8> c;
-        load(i, c);
-        compute(i, c);
+    if (n > 0) {
+        // two blocks in flight; past the last the loads fetch it again, so that every trip issues
+        // the same number
+        Chunk<D, KV8> ca, cb;
+        pages(0);
+        load(0, ca);
+        load(min(1, n - 1), cb);
+        int i = 0;
+        for (; i + 2 <= n; i += 2) {
+            if (((i + 2) & 63) == 0 && i + 2 < n) pages(i + 2);
+            compute(i, ca);
+            load(min(i + 2, n - 1), ca);
+            compute(i + 1, cb);
+            load(min(i + 3, n - 1), cb);
+        }
+        if (i < n) compute(i, ca);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -325,15 +296,10 @@ __global__ void __launch_bounds__(256, 2) attn_chunk_kernel(AttnChunkArgs a) {
                 o += *(const f32x4*)&ow[v][c * RS + d0] * e;
             }
             const int rho = row0 + 16 * t + c;
-            if (pl.pieces == 1) {
-                const float inv = 1.f / l;
-                uint16_t x[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] = act_store((float)(__bf16)(o[e] * inv), a.out_fmt);
-                *(u32x2*)(a.out + ((int64_t)(sq.row0 + rho / G) * a.n_heads + kvh * G + rho % G) * D + d0) =
-                    u32x2{(uint32_t)x[0] | ((uint32_t)x[1] << 16), (uint32_t)x[2] | ((uint32_t)x[3] << 16)};
+            if (un.pieces == 1) {
+                store4(a.out + ((int64_t)(sq.row0 + rho / G) * a.n_heads + kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
             } else {
-                float* dst = a.ws + ((int64_t)part * RT + 16 * t + c) * wst(D);
+                float* dst = a.ws + ((int64_t)un.part * RT + 16 * t + c) * wst(D);
                 *(f32x4*)(dst + d0) = o;
                 if (d0 == 0) {
                     dst[D] = m;
@@ -344,92 +310,99 @@ __global__ void __launch_bounds__(256, 2) attn_chunk_kernel(AttnChunkArgs a) {
     }
 }
 
-// Joins the pieces of split tiles: a workgroup per (sequence, kv head, row tile), a thread per
-// four dims of a row.
-template <int D, int NT>
+// Joins the pieces of split tiles: RPW rows of a tile per workgroup, a thread per four dims of a row.
+// Pieces' statistics and outputs load eight at a time.
+template <int D, int RT>
 __global__ void __launch_bounds__(256) attn_chunk_join_kernel(AttnChunkArgs a) {
-    constexpr int RT = 16 * NT;
-    const int lane = threadIdx.x & 63;
+    constexpr int RPW = 1024 / D, NS = RT / RPW;         // rows per workgroup; workgroups per tile
     const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
-    const int Q = plan_q(a, G, RT);
-    int u = blockIdx.x;
-    const int b = find_seq(a.chunk.n_seqs, u, [&](int i) {
-        const Plan p = plan_seq(load_seq(a.chunk, i), G, RT, Q);
-        return p.pieces > 1 ? p.tiles * nkv : 0;
-    });
-    if (b < 0) return;
-    int part = 0;
-    for (int i = lane; i < b; i += 64) {
-        const Plan p = plan_seq(load_seq(a.chunk, i), G, RT, Q);
-        if (p.pieces > 1) part += p.tiles * p.pieces * nkv;
-    }
+    Unit un;
+    if (!find_unit<true, false>(a, G, RT, un)) return;
+    const int rows = min(RT, un.sq.n * G - un.rt * RT);
+    const int c = blockIdx.y * RPW + threadIdx.x / (D / 4), d0 = threadIdx.x % (D / 4) * 4;
+    static_assert(NS * RPW == RT, "rows of a tile divide evenly");
+    if (c >= rows) return;
+    const int tiles = (un.sq.n * G + RT - 1) / RT;
+    const float* src = a.ws + ((int64_t)un.part * RT + c) * wst(D);
+    const int64_t step = (int64_t)tiles * RT * wst(D);
+    float m = M0, l = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < un.pieces; i0 += 8) {
+        float mi[8], li[8];
+        f32x4 oi[8];
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) part += __shfl_xor(part, o, 64);
-    const Seq sq = load_seq(a.chunk, b);
-    const Plan pl = plan_seq(sq, G, RT, Q);
-    if (u < 0 || u >= pl.tiles * nkv) return;
-    const int rt = u % pl.tiles, kvh = u / pl.tiles;
-    const int row0 = rt * RT, rows = min(RT, sq.n * G - row0);
-    part += kvh * pl.tiles * pl.pieces + rt;
-    for (int it = threadIdx.x; it < rows * (D / 4); it += 256) {
-        const int c = it / (D / 4), d0 = it % (D / 4) * 4;
-        const float* src = a.ws + ((int64_t)part * RT + c) * wst(D);
-        const int64_t step = (int64_t)pl.tiles * RT * wst(D);
-        float m = -INFINITY;
-        for (int i = 0; i < pl.pieces; ++i) m = fmaxf(m, src[i * step + D]);
-        float l = 0.f;
-        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < pl.pieces; ++i) {
-            const float mi = src[i * step + D];
-            const float e = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - m);
-            l += src[i * step + D + 1] * e;
-            o += *(const f32x4*)(src + i * step + d0) * e;
+        for (int j = 0; j < 8; ++j) {
+            const bool on = i0 + j < un.pieces;
+            const float* p = src + (i0 + j) * step;
+            mi[j] = on ? p[D] : M0;
+            li[j] = on ? p[D + 1] : 0.f;
+            oi[j] = on ? *(const f32x4*)(p + d0) : f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        const int rho = row0 + c;
-        const float inv = 1.f / l;
-        uint16_t x[4];
+        float mn = m;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = act_store((float)(__bf16)(o[e] * inv), a.out_fmt);
-        *(u32x2*)(a.out + ((int64_t)(sq.row0 + rho / G) * a.n_heads + kvh * G + rho % G) * D + d0) =
-            u32x2{(uint32_t)x[0] | ((uint32_t)x[1] << 16), (uint32_t)x[2] | ((uint32_t)x[3] << 16)};
+        for (int j = 0; j < 8; ++j) mn = fmaxf(mn, mi[j]);
+        const float f = __builtin_amdgcn_exp2f(m - mn);
+        l *= f;
+        o *= f;
+        m = mn;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float e = __builtin_amdgcn_exp2f(mi[j] - m);
+            l += li[j] * e;
+            o += oi[j] * e;
+        }
     }
+    const int rho = un.rt * RT + c;
+    store4(a.out + ((int64_t)(un.sq.row0 + rho / G) * a.n_heads + un.kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
 }
 
-int row_tiles(const fp_chunk& c, int G) {
-    const int64_t R = std::min<int64_t>((int64_t)c.max_new * G, 1 << 20);
-    return R <= 16 ? 1 : R <= 32 ? 2 : 4;
+// Rows that a sequence can bring to a kv head decide the kernel: up to 64 go to the streaming kernel
+// (tiles of 16, 32 or 64 rows), more to the tiles of 256.
+int tile_rows(const fp_chunk& c, int G) {
+    const int64_t R = (int64_t)std::min(c.max_new, c.n_rows) * G;
+    return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : TILE_ROWS;
 }
+
+// pieces a call aims for, and the least number of blocks worth a piece
+int piece_target(int RT) { return RT == TILE_ROWS ? 256 : 768; }
+int piece_min(int RT) { return RT == TILE_ROWS ? 8 : 16; }
 
 }  // namespace
 
 // Split tiles have more than Q blocks, so their pieces number at most twice total / Q, twice the target.
 size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
-    const int RT = 16 * row_tiles(c, n_heads / kv.n_kv_heads);
-    return (size_t)2 * TARGET * RT * wst(kv.head_dim) * sizeof(float);
+    const int RT = tile_rows(c, n_heads / kv.n_kv_heads);
+    return (size_t)2 * piece_target(RT) * RT * wst(kv.head_dim) * sizeof(float);
 }
 
-template <int D, bool KV8, int NT>
-static hipError_t launch_nt(AttnChunkArgs a, hipStream_t st) {
+template <int D, bool KV8, int RT>
+static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
-    const int64_t tiles = std::min<int64_t>((int64_t)a.chunk.n_rows * G, (int64_t)a.chunk.n_rows * G / (16 * NT) + a.chunk.n_seqs) * nkv;
-    const int64_t n = tiles + TARGET;
+    const int64_t tiles = std::min<int64_t>((int64_t)a.chunk.n_rows * G, (int64_t)a.chunk.n_rows * G / RT + a.chunk.n_seqs) * nkv;
+    a.target = piece_target(RT);
+    a.min_blocks = piece_min(RT);
+    const int64_t n = tiles + a.target + 8;
     if (n > INT_MAX) return hipErrorInvalidValue;
-    a.target = TARGET;
-    a.min_blocks = MINB;
-    FP_LAUNCH((attn_chunk_kernel<D, KV8, NT>), dim3((unsigned)n), dim3(256), 0, st, a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || (a.chunk.max_len + VT_BLK - 1) / VT_BLK <= MINB) return e;
-    // tiles that can be split: each has a piece of at least half of Q blocks
-    FP_LAUNCH((attn_chunk_join_kernel<D, NT>), dim3((unsigned)std::min<int64_t>(tiles, TARGET)), dim3(256), 0, st, a);
-    return hipGetLastError();
+    // tiles that can be split: each has more than Q of the blocks
+    const unsigned split = (a.chunk.max_len + VT_BLK - 1) / VT_BLK <= a.min_blocks ? 0u : (unsigned)std::min<int64_t>(tiles, a.target);
+    if constexpr (RT == TILE_ROWS) {
+        return launch_attn_tile(a, (unsigned)n, split, st);
+    } else {
+        FP_LAUNCH((attn_chunk_kernel<D, KV8, RT / 16>), dim3((unsigned)n), dim3(256), 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || split == 0) return e;
+        FP_LAUNCH((attn_chunk_join_kernel<D, RT>), dim3(split, RT * D / 1024), dim3(256), 0, st, a);
+        return hipGetLastError();
+    }
 }
 
 template <int D, bool KV8>
 static hipError_t launch_d(const AttnChunkArgs& a, hipStream_t st) {
-    switch (row_tiles(a.chunk, a.n_heads / a.kv.n_kv_heads)) {
-        case 1: return launch_nt<D, KV8, 1>(a, st);
-        case 2: return launch_nt<D, KV8, 2>(a, st);
-        default: return launch_nt<D, KV8, 4>(a, st);
+    switch (tile_rows(a.chunk, a.n_heads / a.kv.n_kv_heads)) {
+        case 16: return launch_rt<D, KV8, 16>(a, st);
+        case 32: return launch_rt<D, KV8, 32>(a, st);
+        case 64: return launch_rt<D, KV8, 64>(a, st);
+        default: return launch_rt<D, KV8, TILE_ROWS>(a, st);
     }
 }
 

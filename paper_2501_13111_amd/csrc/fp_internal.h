@@ -299,6 +299,7 @@ struct AttnChunkArgs {
 };
 size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads);
 hipError_t launch_attn_chunk(const AttnChunkArgs& a, hipStream_t st);
+hipError_t launch_attn_tile(const AttnChunkArgs& a, unsigned grid, unsigned split_tiles, hipStream_t st);
 
 // Verification of drafted tokens (verify.hip).
 struct VerifyArgs {

@@ -20,16 +20,18 @@ __device__ __forceinline__ Seq load_seq(const fp_chunk& c, int b) {
     return s;
 }
 
-// Inclusive sum over the wave's lanes.
+// Inclusive sum over the wave's lanes, by data-parallel moves (a few cycles a step, where a shuffle
+// through LDS takes a hundred): within rows of 16, then the rows' sums onwards.
 __device__ __forceinline__ int wave_scan(int v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int t = __shfl_up(v, o, 64);
-        if (lane >= o) v += t;
-    }
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr:1, 2, 4, 8
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
     return v;
 }
+__device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
 
 // The sequence b whose units (count(b) of them, in sequence order) include unit u, with u
 // counted from b's first: b, or -1 past the last unit.  Every lane of the wave gets the answer.

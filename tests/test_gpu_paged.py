@@ -161,6 +161,7 @@ ATTN_SEQS = dict(SEQS, **{
     "drafts": [(200, 5), (31, 5), (0, 5), (511, 2)],
     "long": [(2500, 1), (3, 1), (1100, 1)],
     "split-drafts": [(1700, 4), (90, 6)],
+    "far-chunk": [(2300, 40), (17, 90)],
     "mixed": [(40, 1), (250, 130), (700, 1), (0, 200)],
 })
 
