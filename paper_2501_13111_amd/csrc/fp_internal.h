@@ -312,7 +312,7 @@ struct VerifyArgs {
     int64_t draft_stride;
     const float* u;
     const float* u_last;
-    double inv_t;             // 1 / temperature; 0: greedy
+    double c;                 // log2 e / temperature; 0: greedy
     int* out_ids;
     int* n_out;
     void* ws;

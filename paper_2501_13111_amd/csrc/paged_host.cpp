@@ -220,7 +220,7 @@ fp_status fp_verify_draft(const float* logits, int64_t row_stride, int32_t n_seq
     a.draft_stride = draft_stride;
     a.u = u;
     a.u_last = u_last;
-    a.inv_t = temperature > 0.f ? 1.0 / (double)temperature : 0.0;
+    a.c = temperature > 0.f ? 1.44269504088896340736 / (double)temperature : 0.0;
     a.out_ids = out_ids;
     a.n_out = n_out;
     a.ws = workspace;

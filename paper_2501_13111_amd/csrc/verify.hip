@@ -10,10 +10,13 @@
 // GPU in blocks of VB ids:
 //   row_kernel    per (row, block): maximum, its lowest id, sum of exp((z - max) / T)
 //   mass_kernel   per (sequence, block): the accepted drafts are counted from the blocks' sums
-//                 (every block's workgroup does so for itself), and the sum of the weights that
-//                 the last token is drawn from
-//   pick_kernel   per sequence: the block that holds the draw, then the id in it; writes the tokens
+//                 (every block's workgroup does so for itself), and the sums of the weights that the
+//                 last token is drawn from, per CK ids
+//   pick_kernel   per sequence: the CK ids that hold the draw, then the id; writes the tokens
 // Greedy decoding (T = 0) needs the maxima only: row_kernel, pick_kernel.
+//
+// exp(x) = 2^y, y = x log2 e = n / 256 + r, |r| <= 1 / 512: 2^(n / 256) from a table of 256 and the
+// exponent, 2^r by its power series to the fourth order (the rest is below 4e-17).
 #include <climits>
 
 #include "fp_device.h"
@@ -24,8 +27,10 @@ namespace fpk {
 namespace {
 
 constexpr int VB = 4096;                   // ids per block
+constexpr int CK = 1024;                   // ids per chunk of a draw: four per thread
 constexpr int NT = 256;
 constexpr int EPT = VB / NT;
+static_assert(CK == 4 * NT && VB % CK == 0, "chunks");
 
 struct Part {                              // one block of a row
     double sum;
@@ -33,20 +38,58 @@ struct Part {                              // one block of a row
     int arg;
 };
 
-__device__ __forceinline__ double shfl_xor_d(double v, int o) {
-    return __hiloint2double(__shfl_xor(__double2hiint(v), o, 64), __shfl_xor(__double2loint(v), o, 64));
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_d(double v) {
+    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, ROWS, 0xf, false),
+                            __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, ROWS, 0xf, false));
 }
-__device__ __forceinline__ double wave_sum_d(double v) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += shfl_xor_d(v, o);
+// Inclusive sums over the wave's lanes.
+__device__ __forceinline__ double wave_scan_d(double v) {
+    v += dpp_d<0x111, 0xf>(v);
+    v += dpp_d<0x112, 0xf>(v);
+    v += dpp_d<0x114, 0xf>(v);
+    v += dpp_d<0x118, 0xf>(v);
+    v += dpp_d<0x142, 0xa>(v);
+    v += dpp_d<0x143, 0xc>(v);
     return v;
 }
+__device__ __forceinline__ double lane_d(double v, int l) {
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l));
+}
+__device__ __forceinline__ double wave_sum_d(double v) { return lane_d(wave_scan_d(v), 63); }
 
+// 2^(n / 256), made by the compiler from the power series; a workgroup copies it to LDS (a barrier follows).
+struct ExpTable {
+    double v[256];
+    constexpr ExpTable() : v() {
+        for (int n = 0; n < 256; ++n) {
+            const double x = n * 0.693147180559945309417 / 256.0;
+            double s = 0.0;
+            for (int k = 24; k >= 1; --k) s = (s + 1.0) * x / k;
+            v[n] = 1.0 + s;
+        }
+    }
+};
+__device__ constexpr ExpTable EXP_TABLE;
+__device__ __forceinline__ void exp_table(double* tab) { tab[threadIdx.x] = EXP_TABLE.v[threadIdx.x]; }
+__device__ __forceinline__ double exp2_d(double y, const double* tab) {
+    y = fmax(y, -1200.0);                  // 2^-1200 is zero
+    constexpr double R = 6755399441055744.0 / 256.0;        // 1.5 2^52 / 256: adding it rounds to 1 / 256
+    const double t = y + R;
+    const int n = __double2loint(t);
+    const double r = y - (t - R);
+    constexpr double L = 0.693147180559945309417;
+    double q = L * L * L * L / 24.0;
+    q = fma(q, r, L * L * L / 6.0);
+    q = fma(q, r, L * L / 2.0);
+    q = fma(q, r, L);
+    q = fma(q, r, 1.0);
+    return ldexp(tab[n & 255] * q, n >> 8);
+}
 // exp((z - m) / T) with the weight rules: NaN and -inf have none, +inf all of it
-__device__ __forceinline__ double weight(float z, float m, double inv_t) {
-    if (z == m) return 1.0;
-    if (!(z > -INFINITY) || m == INFINITY) return 0.0;
-    return exp(((double)z - (double)m) * inv_t);
+__device__ __forceinline__ double weight(float z, float m, double c, const double* tab) {
+    const double e = exp2_d(((double)z - (double)m) * c, tab);
+    return z == m ? 1.0 : !(z > -INFINITY) || m == INFINITY ? 0.0 : e;
 }
 
 // the larger value, the lower id among equal ones
@@ -65,9 +108,10 @@ __device__ __forceinline__ int seq_rows(const VerifyArgs& a, int b) {
 __global__ void __launch_bounds__(NT) row_kernel(VerifyArgs a) {
     __shared__ float sm[NT / 64];
     __shared__ int si[NT / 64];
-    __shared__ double sd[NT / 64];
+    __shared__ double sd[NT / 64], tab[NT];
     const int nb = gridDim.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t row = blockIdx.y;
+    if (a.c > 0.0) exp_table(tab);
     const int v0 = blockIdx.x * VB;
     const float* z = a.logits + row * a.row_stride;
     float x[EPT];
@@ -98,9 +142,9 @@ __global__ void __launch_bounds__(NT) row_kernel(VerifyArgs a) {
 #pragma unroll
     for (int j = 1; j < NT / 64; ++j) best_of(m, mi, sm[j], si[j]);
     double s = 0.0;
-    if (a.inv_t > 0.0 && m > -INFINITY) {
+    if (a.c > 0.0 && m > -INFINITY) {
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) s += weight(x[i], m, a.inv_t);
+        for (int i = 0; i < EPT; ++i) s += weight(x[i], m, a.c, tab);
         s = wave_sum_d(s);
         if (lane == 0) sd[w] = s;
         __syncthreads();
@@ -110,158 +154,163 @@ __global__ void __launch_bounds__(NT) row_kernel(VerifyArgs a) {
     if (tid == 0) ((Part*)a.ws)[row * nb + blockIdx.x] = Part{s, m, mi};
 }
 
-// The row's maximum, its lowest id and the sum of its weights (one lane's own row).
-__device__ __forceinline__ void row_total(const VerifyArgs& a, int nb, int64_t row, float& m, int& mi, double& s) {
-    const Part* p = (const Part*)a.ws + row * nb;
-    m = -INFINITY;
-    mi = INT_MAX;
-    for (int j = 0; j < nb; ++j) best_of(m, mi, p[j].max, p[j].arg);
-    s = 0.0;
-    if (a.inv_t > 0.0)
-        for (int j = 0; j < nb; ++j)
-            if (p[j].max > -INFINITY) s += p[j].sum * weight(p[j].max, m, a.inv_t);
-}
-
-// What a sequence's rows decide: accepted drafts, and the deciding row's maximum and sum.
+// What a sequence's rows decide: accepted drafts, and the deciding row's maximum, its id and sum.
 struct Decision {
-    int rows, acc;
-    int64_t row;
-    float m;
-    int arg;
     double sum;
+    int64_t row;
+    int rows, acc, arg;
+    float m;
 };
-__device__ __forceinline__ double draft_p(const VerifyArgs& a, int64_t row, int x) {
-    if (a.draft_probs == nullptr) return 1.0;
-    const double q = (double)a.draft_probs[row * a.draft_stride + x];
-    return q > 0.0 ? q : 0.0;
-}
+__device__ __forceinline__ double draft_p(float q) { return q > 0.f ? (double)q : 0.0; }
 // One wave; lane i judges draft i (max_rows is at most 64).
-__device__ __forceinline__ Decision decide(const VerifyArgs& a, int nb, int b) {
+__device__ __forceinline__ Decision decide(const VerifyArgs& a, int nb, int b, const double* tab) {
     const int lane = threadIdx.x & 63;
     Decision d;
     d.rows = seq_rows(a, b);
     const int64_t r0 = seq_row0(a, b);
+    const bool on = lane < d.rows, judge = lane < d.rows - 1;
+    const int64_t row = r0 + lane;
+    const Part* p = (const Part*)a.ws + row * nb;
+    // the draft's own loads first: they lead to two more
+    const int x = judge ? a.draft_ids[row] : -1;
+    const bool in = x >= 0 && x < a.V;
+    const float zx = in ? a.logits[row * a.row_stride + x] : -INFINITY;
+    const float qx = in && a.draft_probs != nullptr ? a.draft_probs[row * a.draft_stride + x] : 1.f;
+    const float ux = judge && a.c > 0.0 ? a.u[row] : 0.f;
     float m = -INFINITY;
     int mi = INT_MAX;
     double s = 0.0;
     bool ok = false;
-    if (lane < d.rows) {
-        const int64_t row = r0 + lane;
-        row_total(a, nb, row, m, mi, s);
-        if (lane < d.rows - 1) {
-            const int x = a.draft_ids[row];
-            if (x >= 0 && x < a.V && m > -INFINITY) {
-                if (a.inv_t > 0.0) {
-                    const double p = weight(a.logits[row * a.row_stride + x], m, a.inv_t) / s;
-                    ok = (double)a.u[row] * draft_p(a, row, x) < p;
-                } else {
-                    ok = x == mi;
-                }
+    if (on) {
+        // eight blocks' loads together, the running sum rescaled to the running maximum
+        for (int j0 = 0; j0 < nb; j0 += 8) {
+            Part q[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[j] = p[min(j0 + j, nb - 1)];
+            const float old = m;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) best_of(m, mi, q[j].max, q[j].arg);
+            if (a.c > 0.0 && m > -INFINITY) {
+                if (j0 > 0) s *= weight(old, m, a.c, tab);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (j0 + j < nb) s += q[j].sum * weight(q[j].max, m, a.c, tab);
             }
+        }
+        if (in && m > -INFINITY) {
+            if (a.c > 0.0) ok = (double)ux * draft_p(qx) * s < weight(zx, m, a.c, tab);
+            else ok = x == mi;
         }
     }
     d.acc = __builtin_ctzll(~__ballot(ok));           // lanes from rows - 1 on never accept
     d.row = r0 + d.acc;
-    d.m = __shfl(m, d.acc, 64);
-    d.arg = __shfl(mi, d.acc, 64);
-    d.sum = __hiloint2double(__shfl(__double2hiint(s), d.acc, 64), __shfl(__double2loint(s), d.acc, 64));
+    d.m = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(m), d.acc));
+    d.arg = __builtin_amdgcn_readlane(mi, d.acc);
+    d.sum = lane_d(s, d.acc);
     return d;
 }
 
-// Weight of id v in the last draw: p - q (not below zero) at a refused draft, p at the last row,
-// and p at a refused draft too when `plain` (p - q is zero everywhere).
-__device__ __forceinline__ double draw_weight(const VerifyArgs& a, const Decision& d, int v, bool plain) {
-    const double p = weight(a.logits[d.row * a.row_stride + v], d.m, a.inv_t) / d.sum;
-    if (plain || d.acc == d.rows - 1) return p;
-    if (a.draft_probs == nullptr) return v == a.draft_ids[d.row] ? 0.0 : p;
-    return fmax(p - draft_p(a, d.row, v), 0.0);
+// Weights of four ids from v on in the last draw: p - q (not below zero) at a refused draft, p at the
+// last row, and p at a refused draft too when `plain` (p - q is zero everywhere).
+__device__ __forceinline__ void draw_weights(const VerifyArgs& a, const Decision& d, int v, bool plain, const double* tab,
+                                             double (&wt)[4]) {
+    const float* z = a.logits + d.row * a.row_stride;
+    const bool whole = plain || d.acc == d.rows - 1, qs = !whole && a.draft_probs != nullptr;
+    const float* q = a.draft_probs + d.row * a.draft_stride;
+    const int x = !whole && !qs ? a.draft_ids[d.row] : -1;
+    const double inv = 1.0 / d.sum;
+    float zz[4], qq[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool in = v + i < a.V;
+        zz[i] = in ? z[v + i] : -INFINITY;
+        qq[i] = in && qs ? q[v + i] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const double p = weight(zz[i], d.m, a.c, tab) * inv;
+        wt[i] = v + i == x ? 0.0 : fmax(p - draft_p(qq[i]), 0.0);
+    }
 }
 
-__global__ void __launch_bounds__(NT) mass_kernel(VerifyArgs a, double* __restrict__ mass) {
-    __shared__ double sd[2][NT / 64];
+__global__ void __launch_bounds__(NT) mass_kernel(VerifyArgs a, double* __restrict__ mass, Decision* __restrict__ kept) {
+    __shared__ double tab[NT], sd[VB / CK][NT / 64];
     const int nb = gridDim.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const Decision d = decide(a, nb, b);
-    double s = 0.0, sp = 0.0;
-    if (d.rows > 0 && d.m > -INFINITY) {
-        const int v0 = blockIdx.x * VB;
-        for (int i = 0; i < EPT; ++i) {
-            const int v = v0 + tid + NT * i;
-            if (v < a.V) {
-                s += draw_weight(a, d, v, false);
-                sp += draw_weight(a, d, v, true);
-            }
-        }
-    }
-    s = wave_sum_d(s);
-    sp = wave_sum_d(sp);
-    if (lane == 0) {
-        sd[0][w] = s;
-        sd[1][w] = sp;
+    exp_table(tab);
+    __syncthreads();
+    const Decision d = decide(a, nb, b, tab);
+    if (blockIdx.x == 0 && tid == 0) kept[b] = d;
+    const bool live = d.rows > 0 && d.m > -INFINITY;
+#pragma unroll
+    for (int c = 0; c < VB / CK; ++c) {
+        double wt[4] = {0.0, 0.0, 0.0, 0.0};
+        if (live) draw_weights(a, d, blockIdx.x * VB + c * CK + 4 * tid, false, tab, wt);
+        const double s = wave_sum_d((wt[0] + wt[1]) + (wt[2] + wt[3]));
+        if (lane == 0) sd[c][w] = s;
     }
     __syncthreads();
-    if (tid < 2) {
-        double t = 0.0;
-        for (int j = 0; j < NT / 64; ++j) t += sd[tid][j];
-        mass[((int64_t)b * nb + blockIdx.x) * 2 + tid] = t;
-    }
+    if (tid < VB / CK) mass[((int64_t)b * nb + blockIdx.x) * (VB / CK) + tid] = (sd[tid][0] + sd[tid][1]) + (sd[tid][2] + sd[tid][3]);
 }
 
-// One workgroup per sequence.  The draw's block from the blocks' masses, then 1024 ids at a time
-// in id order: four per lane, prefix sums over the workgroup.
-__global__ void __launch_bounds__(NT) pick_kernel(VerifyArgs a, int nb, const double* __restrict__ mass) {
-    __shared__ double sd[NT / 64];
+// One workgroup per sequence.  The chunk that holds the draw from the chunks' masses, then the id in it.
+__global__ void __launch_bounds__(NT) pick_kernel(VerifyArgs a, int nb, const double* __restrict__ mass, const Decision* __restrict__ kept) {
+    __shared__ double tab[NT], sd[NT / 64];
     __shared__ int found, top;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const Decision d = decide(a, nb, b);
+    exp_table(tab);
+    if (tid == 0) {
+        found = INT_MAX;
+        top = -1;
+    }
+    __syncthreads();
+    const Decision d = a.c > 0.0 ? kept[b] : decide(a, nb, b, tab);
     int last = -1;
     if (d.rows > 0 && d.m > -INFINITY) {
-        if (a.inv_t == 0.0) {
+        if (a.c == 0.0) {
             last = d.arg;
         } else {
-            const double* ms = mass + (int64_t)b * nb * 2;
+            // sum of chunk j of the draw: of p - q, or of p where that is zero everywhere (the chunks of p
+            // are then taken as whole blocks, of their first chunk)
+            const double* ms = mass + (int64_t)b * nb * (VB / CK);
+            const Part* pp = (const Part*)a.ws + d.row * nb;
+            const int nc = nb * (VB / CK);
+            bool plain = false;
+            auto chunk_mass = [&](int j) {
+                if (j >= nc) return 0.0;
+                if (!plain) return ms[j];
+                const Part& p = pp[j / (VB / CK)];
+                return j % (VB / CK) ? 0.0 : p.sum * weight(p.max, d.m, a.c, tab) / d.sum;
+            };
             double total = 0.0;
-            for (int j = 0; j < nb; ++j) total += ms[2 * j];
-            const bool plain = !(total > 0.0);
-            if (plain) {
+            for (int j0 = 0; j0 < nc; j0 += 64) total += wave_sum_d(chunk_mass(j0 + lane));
+            if (!(total > 0.0)) {
+                plain = true;
                 total = 0.0;
-                for (int j = 0; j < nb; ++j) total += ms[2 * j + 1];
+                for (int j0 = 0; j0 < nc; j0 += 64) total += wave_sum_d(chunk_mass(j0 + lane));
             }
             const double goal = (double)a.u_last[b] * total;
-            // the first block whose running sum passes the goal; rounding may leave the goal at the
-            // total: then the last block with any mass, and in it the last id with any
-            double base = 0.0;
-            int blk = -1;
-            double at = 0.0;
-            for (int j = 0; j < nb; ++j) {
-                const double mj = ms[2 * j + plain];
-                if (mj > 0.0) {
-                    blk = j;
-                    at = base;
-                    if (base + mj > goal) break;
+            // the first chunk whose running sum passes the goal; rounding may leave the goal at the
+            // total: then the last chunk with any mass, and in it the last id with any
+            double base = 0.0, at = 0.0;
+            int ck = -1;
+            for (int j0 = 0; j0 < nc; j0 += 64) {
+                const double mj = chunk_mass(j0 + lane), inc = base + wave_scan_d(mj);
+                const uint64_t any = __ballot(mj > 0.0), past = any & __ballot(inc > goal);
+                if (any) {
+                    const int l = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any);
+                    ck = j0 + l;
+                    at = lane_d(inc - mj, l);
+                    if (past) break;
                 }
-                base += mj;
+                base = lane_d(inc, 63);
             }
-            if (tid == 0) {
-                found = INT_MAX;
-                top = -1;
-            }
-            __syncthreads();
-            for (int c = 0; c < VB && blk >= 0; c += 4 * NT) {
-                double wt[4], s = 0.0;
-                int hi = -1;
-                const int v0 = blk * VB + c + 4 * tid;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    wt[i] = v0 + i < a.V ? draw_weight(a, d, v0 + i, plain) : 0.0;
-                    if (wt[i] > 0.0) hi = v0 + i;
-                    s += wt[i];
-                }
-                double inc = s;
-#pragma unroll
-                for (int o = 1; o < 64; o <<= 1) {
-                    const double t = __hiloint2double(__shfl_up(__double2hiint(inc), o, 64), __shfl_up(__double2loint(inc), o, 64));
-                    if (lane >= o) inc += t;
-                }
+            const int chunks = plain ? VB / CK : 1;
+            for (int c = 0; c < chunks && ck >= 0; ++c) {
+                double wt[4];
+                const int v0 = (ck + c) * CK + 4 * tid;
+                draw_weights(a, d, v0, plain, tab, wt);
+                const double s = (wt[0] + wt[1]) + (wt[2] + wt[3]);
+                const double inc = wave_scan_d(s);
                 if (lane == 63) sd[w] = inc;
                 __syncthreads();
                 double run = at + (inc - s), chunk = 0.0;
@@ -269,6 +318,10 @@ __global__ void __launch_bounds__(NT) pick_kernel(VerifyArgs a, int nb, const do
                     if (j < w) run += sd[j];
                     chunk += sd[j];
                 }
+                int hi = -1;
+#pragma unroll
+                for (int i = 3; i >= 0; --i)
+                    if (wt[i] > 0.0 && hi < 0) hi = v0 + i;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     run += wt[i];
@@ -295,20 +348,21 @@ int blocks_of(int V) { return (V + VB - 1) / VB; }
 }  // namespace
 
 size_t verify_ws_bytes(int n_seqs, int n_rows, int V) {
-    return (size_t)n_rows * blocks_of(V) * sizeof(Part) + (size_t)n_seqs * blocks_of(V) * 2 * sizeof(double);
+    return (size_t)n_rows * blocks_of(V) * sizeof(Part) + (size_t)n_seqs * (blocks_of(V) * (VB / CK) * sizeof(double) + sizeof(Decision));
 }
 
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t st) {
     const int nb = blocks_of(a.V);
     double* mass = (double*)((Part*)a.ws + (size_t)a.n_rows * nb);
+    Decision* kept = (Decision*)(mass + (size_t)a.n_seqs * nb * (VB / CK));
     if (a.n_rows > 0) FP_LAUNCH(row_kernel, dim3(nb, a.n_rows), dim3(NT), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (a.inv_t > 0.0) {
-        FP_LAUNCH(mass_kernel, dim3(nb, a.n_seqs), dim3(NT), 0, st, a, mass);
+    if (a.c > 0.0) {
+        FP_LAUNCH(mass_kernel, dim3(nb, a.n_seqs), dim3(NT), 0, st, a, mass, kept);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    FP_LAUNCH(pick_kernel, dim3(a.n_seqs), dim3(NT), 0, st, a, nb, mass);
+    FP_LAUNCH(pick_kernel, dim3(a.n_seqs), dim3(NT), 0, st, a, nb, mass, kept);
     return hipGetLastError();
 }
 
