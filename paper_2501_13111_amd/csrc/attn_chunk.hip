@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
     constexpr int NJ = D / 32, ND = D / 16, RT = 16 * NT;
     constexpr int NK = Chunk<D, KV8>::NK;
     constexpr int RS = D + 4;
-    __shared__ __attribute__((aligned(16))) float ow[4][16 * RS];
+    __shared__ __attribute__((aligned(16))) float ow[4][RT * RS];
     __shared__ float mw[4][RT], lw[4][RT];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -69,6 +69,14 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
     const int b = un.b, kvh = un.kvh, beg = un.beg, end = un.end;
     const int row0 = un.rt * RT, rows = min(RT, sq.n * G - row0);
 
+    // the pool block of this wave's i-th block, 64 of them at a time in the lanes
+    const int n = end > beg ? (end - beg - w + 3) / 4 : 0;
+    int pbs = 0;
+    auto pages = [&](int i0) {
+        const int i = i0 + lane;
+        pbs = i < n ? pool_block(a.kv, a.chunk, b, kvh, beg + w + 4 * i) : -1;
+    };
+    pages(0);                                   // on its way while the queries are addressed
     // queries: column c of tile t is row row0 + 16 t + c
     u32x4 qf[NT][NJ];
     int lim[NT];                                 // last position that the lane's row sees
@@ -86,13 +94,6 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
         }
     }
 
-    // the pool block of this wave's i-th block, 64 of them at a time in the lanes
-    const int n = end > beg ? (end - beg - w + 3) / 4 : 0;
-    int pbs = 0;
-    auto pages = [&](int i0) {
-        const int i = i0 + lane;
-        pbs = i < n ? pool_block(a.kv, a.chunk, b, kvh, beg + w + 4 * i) : -1;
-    };
     constexpr int KB = VT_BLK * D * (KV8 ? 1 : 2);      // bytes of a block of keys, and of values
     auto load = [&](int i, Chunk<D, KV8>& c) {
         const int pb = __builtin_amdgcn_readlane(pbs, i & 63);
@@ -251,7 +252,6 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
         // two blocks in flight; past the last the loads fetch it again, so that every trip issues
         // the same number
         Chunk<D, KV8> ca, cb;
-        pages(0);
         load(0, ca);
         load(min(1, n - 1), cb);
         int i = 0;
@@ -273,38 +273,36 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
             lw[w][16 * t + r] = l_run[t];
         }
     }
-    // merge the four waves, one tile of 16 rows after another
+    // merge the four waves
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        __syncthreads();
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int dd = 0; dd < ND; ++dd) *(f32x4*)(&ow[w][r * RS + 16 * dd + 4 * g]) = oacc[t][dd];
-        __syncthreads();
-        for (int it = tid; it < 16 * (D / 4); it += 256) {
-            const int c = it / (D / 4), d0 = it % (D / 4) * 4;
-            if (16 * t + c >= rows) continue;
-            float m = -INFINITY;
+        for (int dd = 0; dd < ND; ++dd) *(f32x4*)(&ow[w][(16 * t + r) * RS + 16 * dd + 4 * g]) = oacc[t][dd];
+    __syncthreads();
+#pragma unroll 4
+    for (int it = tid; it < rows * (D / 4); it += 256) {
+        const int c = it / (D / 4), d0 = it % (D / 4) * 4;
+        float m = -INFINITY;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) m = fmaxf(m, mw[v][16 * t + c]);
-            float l = 0.f;
-            f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int v = 0; v < 4; ++v) m = fmaxf(m, mw[v][c]);
+        float l = 0.f;
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const float mv = mw[v][16 * t + c];
-                const float e = mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv - m);
-                l += lw[v][16 * t + c] * e;
-                o += *(const f32x4*)&ow[v][c * RS + d0] * e;
-            }
-            const int rho = row0 + 16 * t + c;
-            if (un.pieces == 1) {
-                store4(a.out + ((int64_t)(sq.row0 + rho / G) * a.n_heads + kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
-            } else {
-                float* dst = a.ws + ((int64_t)un.part * RT + 16 * t + c) * wst(D);
-                *(f32x4*)(dst + d0) = o;
-                if (d0 == 0) {
-                    dst[D] = m;
-                    dst[D + 1] = l;
-                }
+        for (int v = 0; v < 4; ++v) {
+            const float mv = mw[v][c];
+            const float e = mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv - m);
+            l += lw[v][c] * e;
+            o += *(const f32x4*)&ow[v][c * RS + d0] * e;
+        }
+        const int rho = row0 + c;
+        if (un.pieces == 1) {
+            store4(a.out + ((int64_t)(sq.row0 + rho / G) * a.n_heads + kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
+        } else {
+            float* dst = a.ws + ((int64_t)un.part * RT + c) * wst(D);
+            *(f32x4*)(dst + d0) = o;
+            if (d0 == 0) {
+                dst[D] = m;
+                dst[D + 1] = l;
             }
         }
     }
@@ -363,16 +361,16 @@ int tile_rows(const fp_chunk& c, int G) {
     return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : TILE_ROWS;
 }
 
-// pieces a call aims for, and the least number of blocks worth a piece
-int piece_target(int RT) { return RT == TILE_ROWS ? 256 : 768; }
+// log2 of the pieces a call aims for, and the least number of blocks worth a piece
+int piece_target(int RT) { return RT >= 64 ? 8 : 10; }
 int piece_min(int RT) { return RT == TILE_ROWS ? 8 : 16; }
 
 }  // namespace
 
-// Split tiles have more than Q blocks, so their pieces number at most twice total / Q, twice the target.
+// Split tiles have more than Q blocks, so their pieces number at most twice total / Q, twice the aim.
 size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
     const int RT = tile_rows(c, n_heads / kv.n_kv_heads);
-    return (size_t)2 * piece_target(RT) * RT * wst(kv.head_dim) * sizeof(float);
+    return ((size_t)2 << piece_target(RT)) * RT * wst(kv.head_dim) * sizeof(float);
 }
 
 template <int D, bool KV8, int RT>
@@ -381,10 +379,14 @@ static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     const int64_t tiles = std::min<int64_t>((int64_t)a.chunk.n_rows * G, (int64_t)a.chunk.n_rows * G / RT + a.chunk.n_seqs) * nkv;
     a.target = piece_target(RT);
     a.min_blocks = piece_min(RT);
-    const int64_t n = tiles + a.target + 8;
+    // tiles of 64 rows and more: one workgroup per CU
+    a.slots = RT >= 64 ? 8 : 0;
+    a.over = 10;
+    a.join = 8;
+    const int64_t pieces = (int64_t)1 << a.target, n = std::max(tiles + pieces, 2 * pieces) + 8;
     if (n > INT_MAX) return hipErrorInvalidValue;
     // tiles that can be split: each has more than Q of the blocks
-    const unsigned split = (a.chunk.max_len + VT_BLK - 1) / VT_BLK <= a.min_blocks ? 0u : (unsigned)std::min<int64_t>(tiles, a.target);
+    const unsigned split = (a.chunk.max_len + VT_BLK - 1) / VT_BLK <= a.min_blocks ? 0u : (unsigned)std::min<int64_t>(tiles, pieces);
     if constexpr (RT == TILE_ROWS) {
         return launch_attn_tile(a, (unsigned)n, split, st);
     } else {

@@ -30,16 +30,47 @@ struct Lanes {
     }
     __device__ __forceinline__ Seq get(int b0) const { return b0 == 0 ? s0 : at(b0); }
 };
-// Blocks per piece.  The total is summed in two halves of 24 bits, so that 64 lanes' sums fit.
+// Blocks per piece, Q: about the total over 2^a.target, and at least a.min_blocks.  Where few workgroups run at
+// a time (2^a.slots > 1) and there is one sequence, whose pieces are all alike, a last round of a few pieces
+// would cost as much as a full one: its tiles are cut so that the pieces just fill one round, or two, or not
+// at all, whichever costs least: rounds times (blocks of a piece + a.over, a piece's fixed part), and a.join
+// for joining, all in blocks.  Several sequences' pieces differ in size and fill each other's gaps: there the aim
+// is lowered by half a piece a tile, which rounding up adds, so that one round holds them.
+// Totals are summed in halves of 24 bits, so that 64 lanes' sums fit.
 __device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, int G, int RT) {
+    if (a.slots > 0 && a.chunk.n_seqs == 1) {
+        const Seq s{__builtin_amdgcn_readfirstlane(L.s0.row0), __builtin_amdgcn_readfirstlane(L.s0.n),
+                    __builtin_amdgcn_readfirstlane(L.s0.ctx), __builtin_amdgcn_readfirstlane(L.s0.len)};
+        const Plan p = plan_seq(s, G, RT, 1);
+        const int tiles = std::max(1, p.tiles * a.kv.n_kv_heads);        // above 2^31 the launch is refused
+        int best = std::max(1, p.blocks), cost = ((tiles - 1 >> a.slots) + 1) * (p.blocks + a.over);
+        for (int k = 0; k < 2; ++k) {
+            const int cut = std::min((1 << (a.slots + k)) / tiles, p.blocks / a.min_blocks);
+            if (cut < 2) continue;
+            const int Q = (p.blocks + cut - 1) / cut;
+            const int c = ((tiles * cut - 1 >> a.slots) + 1) * (Q + a.over) + a.join;
+            if (c < cost) {
+                cost = c;
+                best = Q;
+            }
+        }
+        return best;
+    }
     int64_t total = 0;
+    int tiles = 0;
     for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
         const Plan p = plan_seq(L.get(b0), G, RT, 1);
         const int64_t t = (int64_t)p.tiles * p.blocks;
+        if (a.slots > 0) tiles += std::min(wave_total(p.tiles), 1 << 20);
         total += wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24);
     }
-    total = (total * a.kv.n_kv_heads + a.target - 1) / a.target;
-    return (int)std::max<int64_t>(a.min_blocks, std::min<int64_t>(total, 1 << 24));
+    total *= a.kv.n_kv_heads;
+    if (a.slots > 0) {
+        const float aim = fmaxf((float)(1 << a.target) - 0.5f * (float)tiles * (float)a.kv.n_kv_heads, 0.5f * (float)(1 << a.target));
+        return std::max(a.min_blocks, (int)fminf((float)total / aim, 1.6e7f) + 1);
+    }
+    total = (total + ((int64_t)1 << a.target) - 1) >> a.target;
+    return std::max(a.min_blocks, (int)std::min<int64_t>(total, 1 << 24));
 }
 
 // What a workgroup works on: row tile rt of kv head kvh of sequence b, blocks beg .. end - 1 (one of

@@ -9,6 +9,8 @@ from __future__ import annotations
 import ctypes
 import math
 
+import torch
+
 from .binding import KVQ, _check, load
 
 VT_BLK = 32      # positions per transposed block of values
@@ -28,28 +30,46 @@ class _Chunk(ctypes.Structure):
 
 def _tensor(t, dtype, name, shape=None, contiguous=True, device=None):
     """t's address, after checking that it is a HIP tensor of that type (and shape, and device)."""
-    import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    try:
+        if t.dtype is dtype and t.is_cuda and (shape is None or t.shape == shape) and \
+                (device is None or t.device == device) and (not contiguous or t.is_contiguous()):
+            return t.data_ptr()
+    except AttributeError:
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor") from None
+    if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
+
+
+_fn = {}
+# the current stream's handle without a Stream object (about a microsecond less a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def _call(name, device, stream, *args):
     """Run an entry point on `device`, on `stream` or the device's current stream."""
-    import torch
-    with torch.cuda.device(device):
-        s = stream if stream is not None else torch.cuda.current_stream(device)
-        if stream is not None and stream.device != device:
+    f = _fn.get(name)
+    if f is None:
+        f = _fn[name] = getattr(load(), name)
+    if stream is None:
+        s = _raw_stream(device.index)
+    else:
+        if stream.device != device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-        _check(getattr(load(), name)(*args, int(s.cuda_stream)), name)
+        s = stream.cuda_stream
+    if torch.cuda.current_device() == device.index:
+        rc = f(*args, s)
+    else:
+        with torch.cuda.device(device):
+            rc = f(*args, s)
+    if rc != 0:
+        _check(rc, name)
 
 
 class PagedKV:
@@ -61,7 +81,6 @@ class PagedKV:
     """
 
     def __init__(self, k, v, k_scales=None, v_scales=None):
-        import torch
         if not isinstance(k, torch.Tensor) or k.dim() != 4:
             raise ValueError("k must be a [pages, kv heads, page size, head_dim] tensor")
         n, h, ps, d = k.shape
@@ -81,12 +100,11 @@ class PagedKV:
                   for t, nm in ((k_scales, "k_scales"), (v_scales, "v_scales"))]
         elif k_scales is not None or v_scales is not None:
             raise ValueError("a bf16 cache has no scales")
-        self.c = _PagedKv(KVQ[self.kvq], n, ps, h, d, kp, vp, *sp)
+        self.c = ctypes.byref(_PagedKv(KVQ[self.kvq], n, ps, h, d, kp, vp, *sp))
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, kvq: str = "bf16", device="cuda"):
         """A cache of unwritten pages."""
-        import torch
         dt = {"bf16": torch.bfloat16, "int8": torch.int8}[kvq]
         k = torch.empty(n_pages, n_kv_heads, page_size, head_dim, dtype=dt, device=device)
         v = torch.empty(n_pages, n_kv_heads, page_size // VT_BLK, head_dim, VT_BLK, dtype=dt, device=device)
@@ -100,51 +118,50 @@ class Chunk:
     on its positions with them (max_len; the table's whole width if not given)."""
 
     def __init__(self, row_start, ctx_len, table, max_new: int, max_len: int | None = None):
-        import torch
         if not isinstance(table, torch.Tensor) or table.dim() != 2:
             raise ValueError("table must be a [sequences, pages] tensor")
         B = table.shape[0]
         self.device = table.device
         self.row_start, self.ctx_len, self.table = row_start, ctx_len, table
         self.max_new, self.max_len = int(max_new), max_len if max_len is None else int(max_len)
-        tp = _tensor(table, torch.int32, "table", contiguous=False)
-        if table.shape[1] > 1 and table.stride(1) != 1 or B > 1 and table.stride(0) < table.shape[1]:
-            raise ValueError("table rows must be contiguous")
-        # the row stride sets how far a row may be read: a view of a wider table keeps to its columns
         self.width = table.shape[1]
-        if B > 1 and table.stride(0) != self.width:
-            raise ValueError("table must be contiguous")
         self._p = (_tensor(row_start, torch.int32, "row_start", (B + 1,), device=table.device),
-                   _tensor(ctx_len, torch.int32, "ctx_len", (B,), device=table.device), tp)
+                   _tensor(ctx_len, torch.int32, "ctx_len", (B,), device=table.device), _tensor(table, torch.int32, "table"))
         self.n_seqs = B
+        self._c = {}
 
     def c(self, kv: PagedKV, n_rows: int):
+        """The C structure for n_rows rows over kv's pages."""
         if kv.device != self.device:
             raise ValueError(f"the chunk is on {self.device}, the cache on {kv.device}")
-        max_len = self.max_len if self.max_len is not None else min(self.width * kv.page_size, 2**31 - 1)
-        return _Chunk(self.n_seqs, n_rows, self.max_new, max_len, self.width, *self._p)
+        key = (n_rows, kv.page_size)
+        c = self._c.get(key)
+        if c is None:
+            max_len = self.max_len if self.max_len is not None else min(self.width * kv.page_size, 2**31 - 1)
+            c = self._c[key] = ctypes.byref(_Chunk(self.n_seqs, n_rows, self.max_new, max_len, self.width, *self._p))
+        return c
 
 
 def _heads(t, name, n_rows, head_dim, device):
     """Address and row stride of a bf16 [rows, heads, head_dim] tensor whose heads lie side by side
     (a view of a wider row included), and its head count."""
-    import torch
     p = _tensor(t, torch.bfloat16, name, contiguous=False, device=device)
-    if t.dim() != 3 or t.shape[2] != head_dim or (n_rows is not None and t.shape[0] != n_rows):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [{n_rows if n_rows is not None else 'rows'}, heads, {head_dim}]")
-    if t.numel() == 0:
-        return p or None, t.shape[1] * head_dim, t.shape[1]
-    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != head_dim):
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != head_dim or (n_rows is not None and shape[0] != n_rows):
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected [{n_rows if n_rows is not None else 'rows'}, heads, {head_dim}]")
+    n, h, _ = shape
+    if n * h == 0:
+        return p or None, h * head_dim, h
+    rs, hs, ds = t.stride()
+    if ds != 1 or (h > 1 and hs != head_dim):
         raise ValueError(f"{name}'s heads must lie side by side")
-    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1] * head_dim
-    return p, stride, t.shape[1]
+    return p, rs if n > 1 else h * head_dim, h
 
 
 def kv_append(kv: PagedKV, chunk: Chunk, k, v, q=None, q_out=None, cos=None, sin=None, stream=None):
     """Write k and v (bf16 [rows, kv heads, head_dim], views of a fused projection included) to the
     chunk's positions.  With cos and sin (float32 [positions, head_dim / 2]) k is rotated first, and
     q, if given, into q_out."""
-    import torch
     N, d, dev = k.shape[0], kv.head_dim, kv.device
     kp, ks, kh = _heads(k, "k", N, d, dev)
     vp, vs, vh = _heads(v, "v", N, d, dev)
@@ -168,33 +185,30 @@ def kv_append(kv: PagedKV, chunk: Chunk, k, v, q=None, q_out=None, cos=None, sin
         sp = _tensor(sin, torch.float32, "sin", (n_pos, d // 2), device=dev)
     if N == 0:
         return
-    _call("fp_kv_append", dev, stream, ctypes.byref(kv.c), ctypes.byref(chunk.c(kv, N)), kp, vp, ks, qp, qs, H, op,
+    _call("fp_kv_append", dev, stream, kv.c, chunk.c(kv, N), kp, vp, ks, qp, qs, H, op,
           cp, sp, n_pos)
 
 
 def kv_read(kv: PagedKV, chunk: Chunk, k_out, v_out, stream=None):
     """Read the chunk's positions back into k_out and v_out (bf16 [rows, kv heads, head_dim])."""
-    import torch
     shape = (k_out.shape[0], kv.n_kv_heads, kv.head_dim)
     kp = _tensor(k_out, torch.bfloat16, "k_out", shape, device=kv.device)
     vp = _tensor(v_out, torch.bfloat16, "v_out", shape, device=kv.device)
     if shape[0] == 0:
         return
-    _call("fp_kv_read", kv.device, stream, ctypes.byref(kv.c), ctypes.byref(chunk.c(kv, shape[0])), kp, vp)
+    _call("fp_kv_read", kv.device, stream, kv.c, chunk.c(kv, shape[0]), kp, vp)
 
 
 def attn_chunk_workspace(kv: PagedKV, chunk: Chunk, n_rows: int, n_heads: int):
     """A workspace for attn_chunk calls of these bounds.  Calls that may overlap (other streams,
     graphs replayed side by side) need one each."""
-    import torch
     n = ctypes.c_size_t()
-    _check(load().fp_attn_chunk_workspace(ctypes.byref(kv.c), ctypes.byref(chunk.c(kv, n_rows)), int(n_heads),
+    _check(load().fp_attn_chunk_workspace(kv.c, chunk.c(kv, n_rows), int(n_heads),
                                           ctypes.byref(n)), "fp_attn_chunk_workspace")
     return torch.empty(max(n.value, 16), dtype=torch.uint8, device=kv.device)
 
 
 def _workspace(workspace, make, device):
-    import torch
     w = make() if workspace is None else workspace
     return w, _tensor(w, torch.uint8, "workspace", device=device), w.numel()
 
@@ -204,7 +218,6 @@ def attn_chunk(kv: PagedKV, chunk: Chunk, q, out, scale: float | None = None, wo
     fused projection included) over the cache, the chunk's own positions included.  scale defaults to
     1 / sqrt(head_dim); without a workspace the call takes one from torch's allocator, on the current
     stream, so it refuses another `stream` then."""
-    import torch
     N = q.shape[0]
     qp, qs, H = _heads(q, "q", N, kv.head_dim, kv.device)
     op = _tensor(out, torch.bfloat16, "out", (N, H, kv.head_dim), device=kv.device)
@@ -213,14 +226,13 @@ def attn_chunk(kv: PagedKV, chunk: Chunk, q, out, scale: float | None = None, wo
     if workspace is None and stream is not None and stream != torch.cuda.current_stream(kv.device):
         raise ValueError("another stream than the current one needs a workspace of its own")
     w, wp, wn = _workspace(workspace, lambda: attn_chunk_workspace(kv, chunk, N, H), kv.device)
-    _call("fp_attn_chunk", kv.device, stream, ctypes.byref(kv.c), ctypes.byref(chunk.c(kv, N)), qp, qs, H,
+    _call("fp_attn_chunk", kv.device, stream, kv.c, chunk.c(kv, N), qp, qs, H,
           1.0 / math.sqrt(kv.head_dim) if scale is None else float(scale), op, wp, wn)
 
 
 def verify_draft_workspace(n_rows: int, vocab: int, n_seqs: int | None = None, device="cuda"):
     """A workspace for verify_draft calls of up to n_rows rows (and n_seqs sequences, at most one a
     row if not given)."""
-    import torch
     n = ctypes.c_size_t()
     _check(load().fp_verify_draft_workspace(int(n_seqs if n_seqs is not None else max(1, min(n_rows, 4096))), int(n_rows),
                                             int(vocab), ctypes.byref(n)), "fp_verify_draft_workspace")
@@ -234,7 +246,6 @@ def verify_draft(logits, row_start, draft_ids, u, u_last, out_ids, n_out, draft_
     float32 [sequences] in [0, 1) -> out_ids int32 [sequences, most rows of a sequence] (-1 behind
     the last token) and n_out int32 [sequences].  u, u_last and draft_probs are not used at
     temperature 0 and may be None."""
-    import torch
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or not isinstance(out_ids, torch.Tensor) or out_ids.dim() != 2:
         raise ValueError("logits and out_ids must be 2-dimensional tensors")
     (N, V), (B, R), dev = logits.shape, out_ids.shape, logits.device
