@@ -168,7 +168,9 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
                     for (int e = 0; e < 4; ++e) vsc[t][e] = 16 * t + 4 * g + e < nk ? vsc[t][e] : 0.f;
             }
         }
-        if constexpr (KV8) {                     // log2 of the block's largest value scale
+        // P v_scale is at most 2^15: log2 of the block's largest value scale, less 15.  Products down to
+        // 2^-29 of the largest keep fp16's full precision.
+        if constexpr (KV8) {
             float m = 5.9604645e-8f;             // 2^-24, the least fp16
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
                 for (int e = 0; e < 4; ++e) m = fmaxf(m, vsc[t][e]);
             m = fmaxf(m, __shfl_xor(m, 16, 64));
             m = fmaxf(m, __shfl_xor(m, 32, 64));
-            lk = __builtin_amdgcn_logf(m);
+            lk = __builtin_amdgcn_logf(m) - 15.f;
         }
         u32x4 kf[2][NJ];
 #pragma unroll

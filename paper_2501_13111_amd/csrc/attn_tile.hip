@@ -14,12 +14,14 @@
 // written out as a sequence of products, each followed by the five or so instructions that fit beside it,
 // and its length is the number of its instructions.
 //
-// The softmax's reference m moves only when a score passes it by 2^LAZY; the accumulators are rescaled
-// then, outside the inner loop.  Probabilities may exceed 1 by that.
+// The softmax's reference m moves only when a score passes it by 2^LAZY, and then to 2^-BELOW of that
+// score; the accumulators are rescaled then, outside the inner loop.  Probabilities are taken relative to m:
+// at most 2^(LAZY + BELOW), 2^15, so that in fp16 those down to 2^-21 of the largest keep all their bits
+// (smaller ones are off by 2^-32 of it at most).
 //
-// int8: keys and values are unpacked to fp16 with their scales, divided by 2^7 and 2^4 so that no
-// code * scale leaves fp16's range (an absolute rounding of 2^-18 and 2^-21 is left to the smallest);
-// queries are fp16 too, a row of large ones scaled by a power of two.
+// int8: keys and values are unpacked to fp16 with their scales (code * scale rounded to 11 bits, so that
+// none may reach 65520: half the error that bf16's 8 bits leave in the output, and the matrix cores take no
+// scale); queries are fp16 too, a row of large ones scaled by a power of two.
 #include <type_traits>
 #include <utility>
 
@@ -30,7 +32,7 @@ namespace fpk {
 
 namespace {
 
-constexpr float LAZY = 8.f;
+constexpr float LAZY = 8.f, BELOW = 7.f;
 constexpr int RING = 8;                    // LDS slots
 constexpr int AHEAD = 4;                   // blocks on their way (int8: in registers, two; unpacked two ahead)
 constexpr int FD = 4;                      // fragments read ahead
@@ -45,25 +47,9 @@ __device__ __forceinline__ void static_for(F&& f) {
     static_for(f, std::make_integer_sequence<int, N>{});
 }
 
-__device__ __forceinline__ uint32_t pk_add(uint32_t x, f16x2 y) {
-    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) + y);
-}
 __device__ __forceinline__ uint32_t pk_mul(uint32_t x, uint32_t y) {
     return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * __builtin_bit_cast(f16x2, y));
 }
-// Four int8 codes -> fp16 code * 2^-SH (exact): u = code + 128 in the low bits of 2^(10 - SH) gives
-// 2^(10 - SH) + u 2^-SH.
-template <int SH>
-__device__ __forceinline__ u32x2 codes4(uint32_t w) {
-    constexpr uint32_t M = (25u - SH) << 2;                                   // high byte of 2^(10 - SH)
-    constexpr float B = (float)(1024 + 128) / (1 << SH);
-    const uint32_t u = w ^ 0x80808080u;
-    const f16x2 bias = {(_Float16)-B, (_Float16)-B};
-    return u32x2{pk_add(__builtin_amdgcn_perm(M * 0x01010101u, u, 0x04010400u), bias),
-                 pk_add(__builtin_amdgcn_perm(M * 0x01010101u, u, 0x04030402u), bias)};
-}
-constexpr int KSH = 7, VSH = 4;
-
 template <int D, bool KV8>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) attn_tile_kernel(AttnChunkArgs a) {
     constexpr int NKC = D / 16, NDT = D / 32, NVC = 2 * NDT, CH = NKC + NVC;
@@ -153,7 +139,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     u32x2 half;
     auto stage_k = [&](int i, const Raw& r, int x) {
         const uint32_t s2 = r.ks | (r.ks << 16);
-        const u32x2 c = codes4<KSH>(r.k[x]);
+        const u32x2 c = i8x4_to_f16x4(r.k[x]);
         const u32x2 v = u32x2{pk_mul(c.x, s2), pk_mul(c.y, s2)};
         if ((x & 1) == 0) half = v;
         else if (stager)
@@ -162,7 +148,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     auto stage_v = [&](int i, const Raw& r, int x) {
         // slots 4 x .. 4 x + 3 of the 16: keys 4 (x / 2) + 16 (x % 2) + .. of the eight and eight that sa, sb hold
         const uint32_t s0 = (x & 1) ? r.sb[x & 2] : r.sa[x & 2], s1 = (x & 1) ? r.sb[(x & 2) + 1] : r.sa[(x & 2) + 1];
-        const u32x2 c = codes4<VSH>(r.v[x]);
+        const u32x2 c = i8x4_to_f16x4(r.v[x]);
         const u32x2 v = u32x2{pk_mul(c.x, s0), pk_mul(c.y, s1)};
         if ((x & 1) == 0) half = v;
         else if (stager) *(u32x4*)(vst + (i & (RING - 1)) * SB + (x >> 1) * 256) = u32x4{half.x, half.y, v.x, v.y};
@@ -212,7 +198,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                     m = fmaxf(m, fmaxf(fabsf(__uint_as_float(qf[c][j][x] << 16)), fabsf(__uint_as_float(qf[c][j][x] & 0xFFFF0000u))));
             m = fmaxf(m, __shfl_xor(m, 32, 64));
             const int e = live && m >= 32768.f ? __builtin_amdgcn_frexp_expf(m) - 15 : 0;
-            sl2[c] = __builtin_amdgcn_ldexpf(sl2[c], e + KSH);
+            sl2[c] = __builtin_amdgcn_ldexpf(sl2[c], e);
             const float f = __builtin_amdgcn_ldexpf(1.f, -e);
 #pragma unroll
             for (int j = 0; j < NKC; ++j)
@@ -294,7 +280,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
             t[c][0] = max3(t[c][0], t[c][1], t[c][2]);
             t[c][1] = max3(t[c][3], t[c][4], cur.s[c][15]);
         };
-        auto max_c = [&](int c) { t[c][0] = fmaxf(t[c][0], t[c][1]) * sl2[c]; };
+        auto max_c = [&](int c) { t[c][0] = fmaf(fmaxf(t[c][0], t[c][1]), sl2[c], -BELOW); };
         auto ref_a = [&](int c) {          // the other half's keys belong to the same rows
             const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(t[c][0]), __float_as_uint(t[c][0]), false, false);
             t[c][0] = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
@@ -533,14 +519,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     }
 
     // O^T element (dt, e) of lane l: dim 32 dt + 8 (e / 4) + 4 h32 + e % 4 of row 32 c + l % 32
-    constexpr float VF = KV8 ? (float)(1 << VSH) : 1.f;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         const float l = lacc[c][0];
         if (32 * c + l32 >= wrows) continue;
         const int rho = wr0 + 32 * c + l32;
         if (un.pieces == 1) {
-            const float inv = VF / l;
+            const float inv = 1.f / l;
             uint16_t* orow = a.out + ((int64_t)(sq.row0 + rho / G) * a.n_heads + kvh * G + rho % G) * D;
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
@@ -557,7 +542,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
 #pragma unroll
                 for (int e4 = 0; e4 < 4; ++e4)
                     od[(4 * dt + e4) * 64] =
-                        f32x4{oacc[c][dt][4 * e4], oacc[c][dt][4 * e4 + 1], oacc[c][dt][4 * e4 + 2], oacc[c][dt][4 * e4 + 3]} * VF;
+                        f32x4{oacc[c][dt][4 * e4], oacc[c][dt][4 * e4 + 1], oacc[c][dt][4 * e4 + 2], oacc[c][dt][4 * e4 + 3]};
             if (h32 == 0) *(f32x2*)(dst + TILE_ROWS * D + 2 * (64 * w + 32 * c + l32)) = f32x2{m_ref[c], l};
         }
     }

@@ -144,14 +144,17 @@ def test_read_returns_what_the_pages_hold(nkv, d, page, lens, kvq):
 
 
 # ------------------------------------------------------------------ attention
-def _check_attention(pool, table, lens, q, out, scale=None):
+def _check_attention(pool, table, lens, q, out, scale=None, fp16=False, floor=0.0):
+    """fp16: int8 keys and values that meet the matrix cores as fp16 (half a step is 2^-11)."""
     want, mag, smag = ref.attention(pool, table, lens, q, scale)
     N = want.shape[0]
     d = q.shape[2]
     # output rounding; probabilities rounded to bf16 before they meet v (their sum is not); fp32
     # scores of d products, each side of the quotient off by the largest score error
     ds = 2 * (d + 4) * EPS32 * smag
-    tol = HALF_BF16 * want.abs() + (HALF_BF16 + 2 * ds + 1e-5) * mag * (1 + HALF_BF16)
+    if fp16:
+        ds = ds + 2 * 2.0 ** -11 * smag
+    tol = HALF_BF16 * want.abs() + (HALF_BF16 + 2 * ds + 1e-5 + (2.0 ** -11 if fp16 else 0.0)) * mag * (1 + HALF_BF16) + floor
     err = (out[:N].cpu().double() - want).abs()
     assert (err <= tol).all(), f"{(err / tol.clamp(min=1e-30)).max():.3f} of the tolerance"
 
@@ -185,3 +188,272 @@ def test_attention_matches_the_reference(seqs, nkv, G, d, page, kvq):
     again = torch.empty_like(out)
     fp.attn_chunk(kv, chunk, q.cuda(), again)
     assert torch.equal(ref.bits(again[:N]), ref.bits(out[:N]))
+
+
+def _gpu_attention(kv, table, lens, q):
+    """The reference in 64 bits on the device, for lengths that loops would not finish."""
+    d, nkv, H = kv.head_dim, kv.n_kv_heads, q.shape[1]
+    G, slot = H // nkv, ref.SLOT.cuda()
+    out, mag, r = torch.zeros(q.shape, dtype=torch.float64, device="cuda"), torch.zeros(q.shape, dtype=torch.float64, device="cuda"), 0
+    for b, (ctx, new) in enumerate(lens):
+        n = ctx + new
+        pos = torch.arange(n, device="cuda")
+        pg, off = table[b].cuda().long()[pos // kv.page_size], pos % kv.page_size
+        k, v = kv.k[pg, :, off].double(), kv.v[pg, :, off // 32, :, slot[off % 32]].double()
+        if kv.kvq == "int8":
+            k, v = k * kv.k_scales[pg, :, off].double()[..., None], v * kv.v_scales[pg, :, off].double()[..., None]
+        for h in range(H):
+            s = q[r:r + new, h].double() @ k[:, h // G].t().contiguous() / math.sqrt(d)
+            s.masked_fill_(pos[None, :] > ctx + torch.arange(new, device="cuda")[:, None], -math.inf)
+            p = torch.softmax(s, -1)
+            out[r:r + new, h] = p @ v[:, h // G].contiguous()
+            mag[r:r + new, h] = p @ v[:, h // G].abs().contiguous()
+        r += new
+    return out, mag
+
+
+def _fill_gpu(lens, page, nkv, d, kvq, seed, spare=2):
+    """A pool on the device with every position of the sequences written by kv_append."""
+    fp = _fp()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    need = [-(-(c + n) // page) for c, n in lens]
+    table = ref.tables(torch.Generator().manual_seed(seed), need, sum(need) + spare, max(need))
+    kv = fp.PagedKV.empty(sum(need) + spare, page, nkv, d, kvq)
+    whole, starts = _chunk([(0, c + n) for c, n in lens], table)
+    k = (1.5 * torch.randn(starts[-1], nkv, d, generator=g, device="cuda")).bfloat16()
+    v = torch.randn(starts[-1], nkv, d, generator=g, device="cuda").bfloat16()
+    fp.kv_append(kv, whole, k, v)
+    return kv, table, g
+
+
+@pytest.mark.parametrize("nkv,G,d,page,kvq,lens", [
+    (4, 16, 128, 64, "bf16", [(8000, 130)]),          # pieces of more than 64 blocks, many tiles
+    (4, 16, 128, 64, "int8", [(8000, 130)]),
+    (2, 1, 64, 32, "int8", [(5000, 700), (9, 1000)]),
+    (8, 2, 128, 256, "bf16", [(0, 1000), (0, 3), (0, 517)]),
+    (1, 8, 128, 128, "int8", [(70000, 1), (33, 1), (40000, 1)]),
+    (8, 1, 64, 96, "bf16", [(20000, 2)] * 3),
+])
+def test_long_attention(nkv, G, d, page, kvq, lens):
+    fp = _fp()
+    kv, table, g = _fill_gpu(lens, page, nkv, d, kvq, 31)
+    chunk, starts = _chunk(lens, table)
+    q = torch.randn(starts[-1], nkv * G, d, generator=g, device="cuda").bfloat16()
+    out = torch.empty_like(q)
+    fp.attn_chunk(kv, chunk, q, out)
+    want, mag = _gpu_attention(kv, table, lens, q)
+    # as in _check_attention; scores of at most some tens keep fp32's share below 1e-4
+    assert ((out.double() - want).abs() <= HALF_BF16 * want.abs() + (HALF_BF16 + 1e-4) * mag * (1 + HALF_BF16)).all()
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("nkv,G,new", [(2, 2, 1), (1, 8, 5), (2, 4, 90)])
+def test_scores_far_apart_and_rising(nkv, G, new, kvq):
+    """Keys whose scores grow along the sequence (the softmax's reference moves again and again), tiny and
+    large values beside each other, a negative scale, q at the top of bf16's useful range."""
+    fp = _fp()
+    d, page, lens = 128, 64, [(900, new), (333, new)]
+    for scale, qs in ((None, 1.0), (-0.05, 1.0), (1e-7, 3e5), (3.0, 0.2)):
+        g, pool, table = _case(lens, page, nkv, d, kvq, 41)
+        for b, (c, n) in enumerate(lens):
+            m = c + n
+            ramp = torch.linspace(0.1, 6, m)[:, None, None]
+            pool.write(table[b], torch.arange(m), (ramp * (1 + 0.2 * torch.randn(m, nkv, d, generator=g))).bfloat16().float(),
+                       (torch.randn(m, nkv, d, generator=g) * (10.0 ** (torch.arange(m) % 5 - 3))[:, None, None]).bfloat16().float())
+        chunk, starts = _chunk(lens, table)
+        q = (qs * (0.3 + torch.randn(starts[-1], nkv * G, d, generator=g))).bfloat16()
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+        fp.attn_chunk(pool.device(), chunk, q.cuda(), out, scale=scale)
+        # int8, more than 64 rows: keys and values in fp16, of which the smallest are off by 2^-25;
+        # probabilities below 2^-21 of the largest by 2^-32 of it, times at most all values' magnitudes
+        tile = kvq == "int8" and new * G > 64
+        floor = 0.0
+        if kvq == "int8":
+            vmax = max(float(pool.read(table[b], c + n)[1].abs().sum(0).max()) for b, (c, n) in enumerate(lens))
+            floor = 2.0 ** -25 + 2.0 ** -32 * vmax
+        _check_attention(pool, table, lens, q, out, scale, fp16=tile, floor=floor)
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("new,G", [(1, 4), (20, 4), (100, 4)])
+def test_missing_pages_read_as_zeros_and_take_no_writes(kvq, new, G):
+    fp = _fp()
+    nkv, d, page, lens = 2, 64, 32, [(200, new), (70, new)]
+    g, pool, table = _case(lens, page, nkv, d, kvq, 51)
+    _fill(pool, table, lens, g, upto=lambda c, n: c + n)
+    for b, i, bad in ((0, 2, -5), (0, 6, 2**31 - 1), (1, 0, pool.n_pages)):
+        table[b, i] = bad
+    kv = pool.device()
+    chunk, starts = _chunk(lens, table)
+    N = starts[-1]
+    before = [t.clone() for t in ([kv.k, kv.v] + ([kv.k_scales, kv.v_scales] if kvq == "int8" else []))]
+    q = torch.randn(N, nkv * G, d, generator=g).bfloat16()
+    out = torch.empty(N, nkv * G, d, dtype=torch.bfloat16, device="cuda")
+    fp.attn_chunk(kv, chunk, q.cuda(), out)
+    _check_attention(pool, table, lens, q, out)
+    # writing over the missing page alone leaves the pool as it was
+    gone, s2 = _chunk([(64, 30)], table[:1])
+    k = torch.randn(s2[-1], nkv, d, generator=g).bfloat16().cuda()
+    fp.kv_append(kv, gone, k, k)
+    for a, b in zip(before, [kv.k, kv.v] + ([kv.k_scales, kv.v_scales] if kvq == "int8" else [])):
+        assert torch.equal(ref.bits(a), ref.bits(b))
+    ko, vo = torch.ones(30, nkv, d, dtype=torch.bfloat16, device="cuda"), torch.ones(30, nkv, d, dtype=torch.bfloat16, device="cuda")
+    fp.kv_read(kv, gone, ko, vo)
+    assert not ko.any() and not vo.any()
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+def test_contents_that_break_the_bounds_stay_inside_the_buffers(kvq):
+    """Lengths and rows beyond what the host said: rows past max_new and positions past max_len are
+    neither computed nor written; nothing outside the rows and pages changes."""
+    fp = _fp()
+    nkv, G, d, page = 2, 2, 64, 32
+    g, pool, table = _case([(96, 0), (96, 0)], page, nkv, d, kvq, 61, width=3)
+    _fill(pool, table, [(96, 0), (96, 0)], g)
+    kv = pool.device()
+    N = 12
+    rs = torch.tensor([2, 9, 400], dtype=torch.int32).cuda()            # 7 rows, then 391 of which 3 exist
+    cl = torch.tensor([90, -7], dtype=torch.int32).cuda()
+    chunk = fp.Chunk(rs, cl, table.cuda(), max_new=4, max_len=92)       # seq 0: rows 2, 3 at 90, 91; seq 1: 9, 10, 11 at 0, 1, 2
+    q = torch.randn(N, nkv * G, d, generator=g).bfloat16()
+    out = torch.full((N, nkv * G, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    fp.attn_chunk(kv, chunk, q.cuda(), out)
+    seen = [2, 3, 9, 10, 11]
+    assert (out[[r for r in range(N) if r not in seen]] == 7.0).all()
+    _check_attention(pool, table, [(90, 2), (0, 3)], q[seen], out[seen])
+    k, v = (torch.randn(N, nkv, d, generator=g).bfloat16() for _ in range(2))
+    fp.kv_append(kv, chunk, k.cuda(), v.cuda())
+    pool.write(table[0], torch.tensor([90, 91]), k[2:4].float(), v[2:4].float())
+    pool.write(table[1], torch.tensor([0, 1, 2]), k[9:12].float(), v[9:12].float())
+    for a, want in zip([kv.k, kv.v] + ([kv.k_scales, kv.v_scales] if kvq == "int8" else []), pool.tensors()):
+        assert torch.equal(ref.bits(a.cpu()), ref.bits(want))
+    for bad in ([0, 0, 0], [5, 5, 5], [30, 20, 10], [-9, -9, -9]):      # no rows, or rows that run backwards
+        rs.copy_(torch.tensor(bad, dtype=torch.int32))
+        out.fill_(7.0)
+        fp.attn_chunk(kv, chunk, q.cuda(), out)
+        fp.kv_append(kv, chunk, k.cuda(), v.cuda())
+        assert (out == 7.0).all()
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+def test_pages_beyond_four_gibytes(kvq):
+    fp = _fp()
+    nkv, G, d, page = 8, 2, 128, 256
+    n_pages = 12000 if kvq == "bf16" else 20000                         # 6.3 and 5.2 GB of keys, as much of values
+    kv = fp.PagedKV.empty(n_pages, page, nkv, d, kvq)
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 2], [7, n_pages - 3, n_pages - 7]], dtype=torch.int32)
+    lens = [(600, 70), (500, 1)]
+    whole, st = _chunk([(0, c + n) for c, n in lens], table)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn(st[-1], nkv, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    fp.kv_append(kv, whole, k, v)
+    ko, vo = torch.empty_like(k), torch.empty_like(v)
+    fp.kv_read(kv, whole, ko, vo)
+    if kvq == "bf16":
+        assert torch.equal(ko, k) and torch.equal(vo, v)
+    for new in ([70, 1], [1, 1]):
+        ln = [(c + n - m, m) for (c, n), m in zip(lens, new)]
+        chunk, st = _chunk(ln, table)
+        q = torch.randn(st[-1], nkv * G, d, generator=g, device="cuda").bfloat16()
+        out = torch.empty_like(q)
+        fp.attn_chunk(kv, chunk, q, out)
+        want, mag = _gpu_attention(kv, table, ln, q)
+        assert ((out.double() - want).abs() <= HALF_BF16 * want.abs() + (HALF_BF16 + 1e-4) * mag * (1 + HALF_BF16)).all()
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("new", [1, 40])
+def test_captured_calls_follow_the_lengths(kvq, new):
+    """Append, attention and read back in one graph, replayed with other lengths and rows, eager work of the
+    same calls (another workspace) between the replays; two graphs with a workspace each."""
+    fp = _fp()
+    nkv, G, d, page = 2, 4, 64, 64
+    B, width = 3, 40
+    g = torch.Generator().manual_seed(71)
+    table = ref.tables(g, [width] * B, B * width, width).cuda()
+    N = B * new
+    qkv = torch.empty(N, (G + 2) * nkv, d, dtype=torch.bfloat16, device="cuda")
+    q, k, v = qkv[:, :G * nkv], qkv[:, G * nkv:(G + 1) * nkv], qkv[:, (G + 1) * nkv:]
+    cos, sin = (t.cuda() for t in ref.rope_tables(width * page, d))
+    rs = torch.arange(0, N + 1, new, dtype=torch.int32).cuda()
+    cl = torch.zeros(B, dtype=torch.int32).cuda()
+    chunk = fp.Chunk(rs, cl, table, max_new=new)
+
+    def buffers():
+        kv = fp.PagedKV.empty(B * width, page, nkv, d, kvq)
+        for t in (kv.k, kv.v) + ((kv.k_scales, kv.v_scales) if kvq == "int8" else ()):
+            t.zero_()
+        return kv, torch.empty(N, G * nkv, d, dtype=torch.bfloat16, device="cuda"), \
+            torch.empty(N, G * nkv, d, dtype=torch.bfloat16, device="cuda"), \
+            [torch.empty(N, nkv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)], fp.attn_chunk_workspace(kv, chunk, N, G * nkv)
+
+    def run(kv, qr, out, kvo, ws):
+        fp.kv_append(kv, chunk, k, v, q=q, q_out=qr, cos=cos, sin=sin)
+        fp.attn_chunk(kv, chunk, qr, out, workspace=ws)
+        fp.kv_read(kv, chunk, *kvo)
+
+    sets = [buffers() for _ in range(3)]
+    graphs = []
+    for s in sets[:2]:
+        run(*s)
+        torch.cuda.synchronize()
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            run(*s)
+        graphs.append(gr)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for step, ctx in enumerate([[0, 0, 0], [5, 900, 31], [2000, 17, 64], [63, 2500, 1200], [100, 0, 7]]):
+        torch.cuda.synchronize()
+        qkv.copy_(torch.randn(qkv.shape, generator=g).bfloat16())
+        cl.copy_(torch.tensor(ctx, dtype=torch.int32))
+        torch.cuda.synchronize()
+        for gr, st in zip(graphs, streams):            # side by side
+            with torch.cuda.stream(st):
+                gr.replay()
+        torch.cuda.synchronize()
+        run(*sets[2])
+        torch.cuda.synchronize()
+        for s in sets[:2]:
+            assert torch.equal(s[2], sets[2][2]) and torch.equal(s[3][0], sets[2][3][0]) and torch.equal(s[3][1], sets[2][3][1]), step
+            assert torch.isfinite(s[2].float()).all()
+
+
+def test_calls_on_other_streams():
+    fp = _fp()
+    lens = [(700, 3), (40, 60)]
+    kv, table, g = _fill_gpu(lens, 64, 2, 64, "int8", 81)
+    chunk, st = _chunk(lens, table)
+    q = torch.randn(st[-1], 8, 64, generator=g, device="cuda").bfloat16()
+    want = torch.empty_like(q)
+    fp.attn_chunk(kv, chunk, q, want)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    with pytest.raises(ValueError):
+        fp.attn_chunk(kv, chunk, q, a, stream=s)                        # no workspace of its own
+    fp.attn_chunk(kv, chunk, q, a, stream=s, workspace=fp.attn_chunk_workspace(kv, chunk, st[-1], 8))
+    with torch.cuda.stream(s):
+        fp.attn_chunk(kv, chunk, q, b)
+    torch.cuda.synchronize()
+    assert torch.equal(a, want) and torch.equal(b, want)
+
+
+def test_strided_rows_and_single_rows():
+    """q, k and v as columns of wider rows; one row with an odd stride; unaligned rows are refused."""
+    fp = _fp()
+    FpError = fp.FpError
+    lens = [(50, 1)]
+    kv, table, g = _fill_gpu(lens, 32, 2, 64, "bf16", 91)
+    chunk, _ = _chunk(lens, table)
+    wide = torch.randn(1, 9, 64, generator=g, device="cuda").bfloat16()
+    out = torch.empty(1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    fp.attn_chunk(kv, chunk, wide[:, 3:7], out)
+    want, mag = _gpu_attention(kv, table, lens, wide[:, 3:7])
+    assert ((out.double() - want).abs() <= HALF_BF16 * want.abs() + (HALF_BF16 + 1e-4) * mag * 1.01).all()
+    flat = torch.randn(4 * 64 + 1, generator=g, device="cuda").bfloat16()
+    with pytest.raises(FpError):
+        fp.attn_chunk(kv, chunk, flat[1:].view(1, 4, 64), out)          # 2 bytes off
+    with pytest.raises(ValueError):
+        fp.attn_chunk(kv, chunk, wide[:, ::2][:, :4], out)              # heads apart
+    with pytest.raises(FpError):
+        fp.attn_chunk(kv, chunk, out, out)                              # q and out overlap
