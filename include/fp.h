@@ -319,7 +319,11 @@ fp_status fp_kv_read(const fp_paged_kv* kv, const fp_chunk* chunk, void* k_out, 
  * h * n_kv_heads / n_heads.  The chunk's own keys and values are read from the pages too:
  * append first.  q: device bf16, row r's head h at q + r * q_stride + h * head_dim; out: device
  * bf16 [n_rows, n_heads, head_dim]; both 16-byte aligned.  Query group n_heads / n_kv_heads from
- * 1 to 16.  Sums and softmax statistics are fp32; probabilities enter the product with V as bf16.
+ * 1 to 16.  Scores, softmax statistics and sums are fp32; probabilities enter the product with V as bf16
+ * (int8 caches: fp16).  A NaN or infinite value (not key) at a position of the chunk makes the outputs of
+ * its sequence's earlier rows in the call NaN too; positions that a sequence does not hold reach nothing.
+ * int8: keys and values below 65504 in magnitude (calls of more than 64 rows per sequence and kv head
+ * unpack them to fp16).
  * workspace: device memory of at least fp_attn_chunk_workspace bytes, 16-byte aligned, which
  * the call may use until the stream has passed it (calls that can overlap need one each).
  * FP_ERR_CAPACITY if workspace_bytes is less.
@@ -327,6 +331,23 @@ fp_status fp_kv_read(const fp_paged_kv* kv, const fp_chunk* chunk, void* k_out, 
 fp_status fp_attn_chunk_workspace(const fp_paged_kv* kv, const fp_chunk* chunk, int32_t n_heads, size_t* bytes);
 fp_status fp_attn_chunk(const fp_paged_kv* kv, const fp_chunk* chunk, const void* q, int64_t q_stride, int32_t n_heads,
                         float scale, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The layer stack over a chunk: fp_prefill and fp_decode_step for ragged batches on the
+ * caller's pages (a prompt in pieces, next tokens of sequences of any lengths, drafted tokens,
+ * all in one call).  kv: host array of n_layers paged caches (one per layer, the chunk's table
+ * naming the same pages in each), with the fingerprint's n_kv_heads and head_dim; their format
+ * is their own, whatever cache the handle was created with.  x, y: device bf16 [n_rows, hidden], no
+ * aliasing; row r's token sits at its chunk position, its keys and values are written to the
+ * pages, its output goes to row r of y (rows of no sequence: unspecified values).  The handle's
+ * weights and activations are used, its own cache, position and batch are not touched.
+ * n_rows <= max_batch * max_prompt and max_len <= max_seq (FP_ERR_CAPACITY); up to max_batch
+ * rows take the decode projections.  workspace: as for fp_attn_chunk (the attention's, of any
+ * layer).  May be captured into a graph; allocates nothing.  The debug dumps are not written.
+ */
+fp_status fp_extend_workspace(const fp_layer* layer, const fp_paged_kv* kv, const fp_chunk* chunk, size_t* bytes);
+fp_status fp_extend(fp_layer* layer, const fp_paged_kv* kv, const fp_chunk* chunk, const void* x, void* y,
+                    void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Decide over drafted tokens.  Sequence b owns rows row_start[b] .. row_start[b + 1] - 1 of the

@@ -105,6 +105,8 @@ def load(path: str | None = None):
         "fp_kv_read": [vp, vp, vp, vp, vp],
         "fp_attn_chunk_workspace": [vp, vp, i32, ctypes.POINTER(ctypes.c_size_t)],
         "fp_attn_chunk": [vp, vp, vp, i64, i32, ctypes.c_float, vp, vp, ctypes.c_size_t, vp],
+        "fp_extend_workspace": [vp, vp, vp, ctypes.POINTER(ctypes.c_size_t)],
+        "fp_extend": [vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
         "fp_verify_draft_workspace": [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
         "fp_verify_draft": [vp, i64, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, ctypes.c_float, vp, vp, vp,
                             ctypes.c_size_t, vp],
@@ -285,6 +287,45 @@ class Fingerprint:
 
     def decode_ptr(self, x_ptr: int, y_ptr: int, stream_ptr: int = 0):
         _check(load().fp_decode_step(self._h, x_ptr, y_ptr, stream_ptr), "fp_decode_step")
+
+    def extend_workspace(self, kvs, chunk, n_rows: int):
+        """A workspace for extend calls of these bounds (one for each of calls that may overlap)."""
+        import torch
+        n = ctypes.c_size_t()
+        _check(load().fp_extend_workspace(self._h, self._pages(kvs), chunk.c(kvs[0], n_rows), ctypes.byref(n)),
+               "fp_extend_workspace")
+        return torch.empty(max(n.value, 16), dtype=torch.uint8, device=kvs[0].device)
+
+    def extend(self, kvs, chunk, x, y, workspace=None, stream=None):
+        """The layer stack over a chunk's rows: x, y bf16 [rows, hidden], kvs one PagedKV per layer.
+        Without a workspace the call takes one from torch's allocator, on the current stream, so it
+        refuses another `stream` then."""
+        import torch
+        from .paged import _call, _tensor
+        H = self.shape.hidden
+        N = x.numel() // H
+        dev = kvs[0].device
+        xp = _dev_ptr(x, numel=N * H, name="x")
+        yp = _dev_ptr(y, numel=N * H, name="y")
+        if x.device != dev or y.device != dev:
+            raise ValueError(f"x and y must be on the pages' device {dev}")
+        if workspace is None:
+            if stream is not None and stream != torch.cuda.current_stream(dev):
+                raise ValueError("another stream than the current one needs a workspace of its own")
+            workspace = self.extend_workspace(kvs, chunk, N)
+        wp = _tensor(workspace, torch.uint8, "workspace", device=dev)
+        if N == 0:
+            return
+        _call("fp_extend", dev, stream, self._h, self._pages(kvs), chunk.c(kvs[0], N), xp, yp, wp, workspace.numel())
+
+    def _pages(self, kvs):
+        """The C array of the layers' paged caches."""
+        from .paged import _PagedKv
+        if len(kvs) != self.shape.n_layers:
+            raise ValueError(f"{len(kvs)} paged caches for {self.shape.n_layers} layers")
+        if any(kv.device != kvs[0].device or kv.page_size != kvs[0].page_size for kv in kvs):
+            raise ValueError("the layers' pages must be on one device, of one size")
+        return (_PagedKv * len(kvs))(*[kv.struct for kv in kvs])
 
     # blocks outside the hidden layers (vocab > 0) ------------------------
     def embed(self, ids, x, stream=None):

@@ -611,17 +611,69 @@ fp_status run_gemm_split(fp_layer* h, const uint16_t* X, const Mat& m, int M, in
     return FP_OK;
 }
 
+// Split factors of a prefill's projections, for M rows.
+struct PrefillSplit {
+    int q, o, g, d, kr_q, kr_o, kr_g, kr_d;
+};
+PrefillSplit prefill_splits(const fp_layer* h, int M) {
+    const int H = h->s.hidden, F = h->s.ffn;
+    PrefillSplit p;
+    p.q = gemm_qkv_split_factor(M, h->nqkv, H, h->wq, &p.kr_q);
+    p.o = prefill_split(h, M, H, h->q_dim, 0, &p.kr_o);
+    p.g = prefill_split(h, M, 2 * F, H, F, &p.kr_g);
+    p.d = prefill_split(h, M, H, F, 0, &p.kr_d);
+    return p;
+}
+
+// A prefill layer from its attention's output (act_o) on: in -> out.  *normed: act_in already holds the next
+// layer's normalised input.
+fp_status enqueue_prefill_tail(fp_layer* h, int l, int M, const PrefillSplit& sp, const uint16_t* in, uint16_t* out,
+                               bool* normed, hipStream_t st) {
+    const fp_shape& s = h->s;
+    const int H = s.hidden, F = s.ffn;
+    const int ks_o = sp.o, ks_g = sp.g, ks_d = sp.d, kr_o = sp.kr_o, kr_g = sp.kr_g, kr_d = sp.kr_d;
+    const LayerW& W = h->L[l];
+    const bool last = l == s.n_layers - 1;
+    fp_status rc;
+    *normed = false;
+    h->prof.mark(FP_K_O, l);
+    if (ks_o > 1) {
+        // split-K partials; the residual add and the MLP RMSNorm in one row kernel
+        if ((rc = run_gemm_split(h, h->act_o, W.o, M, 0, ks_o, kr_o, st))) return rc;
+        HIPCHK(launch_resid_norm(h->ppart, ks_o, M, H, in, h->hbuf, W.mlp_norm, s.rms_eps, h->act_in,
+                                 h->act_fmt, nullptr, nullptr, st));
+    } else {
+        if ((rc = run_gemm(h, h->act_o, W.o, M, EPI_RESID, nullptr, h->hbuf, in, st))) return rc;
+        h->prof.mark(FP_K_RMSNORM, l);
+        HIPCHK(launch_rmsnorm(h->hbuf, M, s.hidden, W.mlp_norm, s.rms_eps, h->act_in, h->act_fmt, st));
+    }
+    h->prof.mark(FP_K_GATE_UP, l);
+    if (ks_g > 1) {
+        if ((rc = run_gemm_split(h, h->act_in, W.gu, M, F, ks_g, kr_g, st))) return rc;
+        HIPCHK(launch_swiglu(h->ppart, ks_g, M, F, h->act_f, h->act_fmt, st));
+    } else {
+        if ((rc = run_gemm(h, h->act_in, W.gu, M, EPI_SWIGLU, nullptr, h->act_f, nullptr, st))) return rc;
+    }
+    h->prof.mark(FP_K_DOWN, l);
+    if (ks_d > 1) {
+        // the residual add, and the next layer's attention RMSNorm
+        if ((rc = run_gemm_split(h, h->act_f, W.down, M, 0, ks_d, kr_d, st))) return rc;
+        HIPCHK(launch_resid_norm(h->ppart, ks_d, M, H, h->hbuf, out, last ? nullptr : h->L[l + 1].attn_norm,
+                                 s.rms_eps, h->act_in, h->act_fmt, nullptr, nullptr, st));
+        *normed = !last;
+    } else {
+        if ((rc = run_gemm(h, h->act_f, W.down, M, EPI_RESID, nullptr, out, h->hbuf, st))) return rc;
+    }
+    return FP_OK;
+}
+
 fp_status enqueue_prefill(fp_layer* h, const uint16_t* x, int B, int P, uint16_t* y, hipStream_t st) {
     const fp_shape& s = h->s;
     const int M = B * P;
     const float scale = (float)(1.0 / std::sqrt((double)s.head_dim));
     fp_status rc;
-    const int H = s.hidden, F = s.ffn;
-    int kr_q, kr_o, kr_g, kr_d;
-    const int ks_q = gemm_qkv_split_factor(M, h->nqkv, H, h->wq, &kr_q);
-    const int ks_o = prefill_split(h, M, H, h->q_dim, 0, &kr_o);
-    const int ks_g = prefill_split(h, M, 2 * F, H, F, &kr_g);
-    const int ks_d = prefill_split(h, M, H, F, 0, &kr_d);
+    const PrefillSplit sp = prefill_splits(h, M);
+    const int ks_q = sp.q, kr_q = sp.kr_q;
     bool normed = false;    // act_in already holds this layer's normalised input
     for (int l = 0; l < s.n_layers; ++l) {
         const LayerW& W = h->L[l];
@@ -633,7 +685,6 @@ fp_status enqueue_prefill(fp_layer* h, const uint16_t* x, int B, int P, uint16_t
             h->prof.mark(FP_K_RMSNORM, l);
             HIPCHK(launch_rmsnorm(in, M, s.hidden, W.attn_norm, s.rms_eps, h->act_in, h->act_fmt, st));
         }
-        normed = false;
         h->prof.mark(FP_K_QKV, l);
         const RopeKvArgs ro = rope_args(h, l, ks_q > 1 ? h->ppart : h->qkv32, ks_q, M, P, nullptr, dump);
         if (!dump && gemm_rope_supported(M, W.qkv.N, W.qkv.K, P, s.head_dim, W.qkv.wf)) {
@@ -668,34 +719,7 @@ fp_status enqueue_prefill(fp_layer* h, const uint16_t* x, int B, int P, uint16_t
         h->prof.mark(FP_K_ATTN, l);
         if (aa.kv_int8) HIPCHK(launch_attn_stage(aa, B, st));
         HIPCHK(launch_attn_prefill(aa, B, st));
-        h->prof.mark(FP_K_O, l);
-        if (ks_o > 1) {
-            // split-K partials; the residual add and the MLP RMSNorm in one row kernel
-            if ((rc = run_gemm_split(h, h->act_o, W.o, M, 0, ks_o, kr_o, st))) return rc;
-            HIPCHK(launch_resid_norm(h->ppart, ks_o, M, H, in, h->hbuf, W.mlp_norm, s.rms_eps, h->act_in,
-                                     h->act_fmt, nullptr, nullptr, st));
-        } else {
-            if ((rc = run_gemm(h, h->act_o, W.o, M, EPI_RESID, nullptr, h->hbuf, in, st))) return rc;
-            h->prof.mark(FP_K_RMSNORM, l);
-            HIPCHK(launch_rmsnorm(h->hbuf, M, s.hidden, W.mlp_norm, s.rms_eps, h->act_in, h->act_fmt, st));
-        }
-        h->prof.mark(FP_K_GATE_UP, l);
-        if (ks_g > 1) {
-            if ((rc = run_gemm_split(h, h->act_in, W.gu, M, F, ks_g, kr_g, st))) return rc;
-            HIPCHK(launch_swiglu(h->ppart, ks_g, M, F, h->act_f, h->act_fmt, st));
-        } else {
-            if ((rc = run_gemm(h, h->act_in, W.gu, M, EPI_SWIGLU, nullptr, h->act_f, nullptr, st))) return rc;
-        }
-        h->prof.mark(FP_K_DOWN, l);
-        if (ks_d > 1) {
-            // the residual add, and the next layer's attention RMSNorm
-            if ((rc = run_gemm_split(h, h->act_f, W.down, M, 0, ks_d, kr_d, st))) return rc;
-            HIPCHK(launch_resid_norm(h->ppart, ks_d, M, H, h->hbuf, out, last ? nullptr : h->L[l + 1].attn_norm,
-                                     s.rms_eps, h->act_in, h->act_fmt, nullptr, nullptr, st));
-            normed = !last;
-        } else {
-            if ((rc = run_gemm(h, h->act_f, W.down, M, EPI_RESID, nullptr, out, h->hbuf, st))) return rc;
-        }
+        if ((rc = enqueue_prefill_tail(h, l, M, sp, in, out, &normed, st))) return rc;
         if (h->ldump) HIPCHK(hipMemcpyAsync(h->ldump + (size_t)l * M * s.hidden, out, (size_t)M * s.hidden * 2,
                                             hipMemcpyDeviceToDevice, st));
     }
@@ -842,6 +866,78 @@ fp_status enqueue_decode_batch(fp_layer* h, const uint16_t* x, uint16_t* y, hipS
                                             hipMemcpyDeviceToDevice, st));
     }
     h->prof.end();
+    return FP_OK;
+}
+
+// The layer stack over a chunk's rows, keys and values in the caller's pages.  Up to a batch of rows takes
+// the decode projections (weights streamed once past the rows), more the prefill's.
+fp_status enqueue_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk& chunk, const uint16_t* x, uint16_t* y,
+                         float* attn_ws, hipStream_t st) {
+    const fp_shape& s = h->s;
+    const int M = chunk.n_rows, H = s.hidden;
+    const bool few = M <= s.max_batch;
+    const PrefillSplit sp = few ? PrefillSplit{} : prefill_splits(h, M);
+    fp_status rc;
+    int ks = 1;
+    bool normed = false;
+    if (few)
+        HIPCHK(launch_resid_norm(nullptr, 0, M, H, x, nullptr, h->L[0].attn_norm, s.rms_eps, h->act_in, h->act_fmt,
+                                 h->ssq, nullptr, st));
+    for (int l = 0; l < s.n_layers; ++l) {
+        const LayerW& W = h->L[l];
+        const bool last = l == s.n_layers - 1;
+        const uint16_t* in = l == 0 ? x : h->xbuf;
+        uint16_t* out = last ? y : h->xbuf;
+        const float* qkv;
+        if (few) {
+            if ((rc = run_skinny_batch(h, h->act_in, W.qkv, M, 0, h->part, &ks, st))) return rc;
+            qkv = h->part;
+        } else {
+            if (!normed) HIPCHK(launch_rmsnorm(in, M, H, W.attn_norm, s.rms_eps, h->act_in, h->act_fmt, st));
+            if (sp.q > 1) rc = run_gemm_split(h, h->act_in, W.qkv, M, 0, sp.q, sp.kr_q, st);
+            else rc = run_gemm(h, h->act_in, W.qkv, M, EPI_F32, h->qkv32, nullptr, nullptr, st);
+            if (rc) return rc;
+            qkv = sp.q > 1 ? h->ppart : h->qkv32;
+            ks = sp.q;
+        }
+        KvAppendArgs ap{};
+        ap.kv = kv[l];
+        ap.chunk = chunk;
+        ap.q = qkv;
+        ap.k = qkv + h->q_dim;
+        ap.v = qkv + h->q_dim + h->kv_dim;
+        ap.kv_stride = ap.q_stride = h->nqkv;
+        ap.ks = ks;
+        ap.pstride = (int64_t)M * h->nqkv;
+        ap.n_heads = s.n_heads;
+        ap.q_out = h->q16;
+        ap.cos_t = h->cos_t;
+        ap.sin_t = h->sin_t;
+        HIPCHK(launch_kv_append(ap, true, st));
+        AttnChunkArgs at{};
+        at.kv = kv[l];
+        at.chunk = chunk;
+        at.q = h->q16;
+        at.q_stride = h->q_dim;
+        at.n_heads = s.n_heads;
+        at.scale = (float)(1.0 / std::sqrt((double)s.head_dim));
+        at.out = h->act_o;
+        at.out_fmt = h->act_fmt;
+        at.ws = attn_ws;
+        HIPCHK(launch_attn_chunk(at, st));
+        if (!few) {
+            if ((rc = enqueue_prefill_tail(h, l, M, sp, in, out, &normed, st))) return rc;
+            continue;
+        }
+        if ((rc = run_skinny_batch(h, h->act_o, W.o, M, 0, h->part, &ks, st))) return rc;
+        HIPCHK(launch_resid_norm(h->part, ks, M, H, in, h->hbuf, W.mlp_norm, s.rms_eps, h->act_in, h->act_fmt, h->ssq,
+                                 nullptr, st));
+        if ((rc = run_skinny_batch(h, h->act_in, W.gu, M, s.ffn, h->part2, &ks, st))) return rc;
+        HIPCHK(launch_swiglu(h->part2, ks, M, s.ffn, h->act_f, h->act_fmt, st));
+        if ((rc = run_skinny_batch(h, h->act_f, W.down, M, 0, h->part, &ks, st))) return rc;
+        HIPCHK(launch_resid_norm(h->part, ks, M, H, h->hbuf, out, h->L[last ? 0 : l + 1].attn_norm, s.rms_eps, h->act_in,
+                                 h->act_fmt, h->ssq, nullptr, st));
+    }
     return FP_OK;
 }
 
@@ -1548,6 +1644,41 @@ fp_status fp_generate(fp_layer* h, const int32_t* prompt_ids, int32_t B, int32_t
         *elapsed_ms = ms;
     }
     return finish(FP_OK);
+}
+
+static fp_status check_extend(const fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk) {
+    if (!h) return fail(FP_ERR_INVALID_ARG, "layer is NULL");
+    if (!kv) return fail(FP_ERR_INVALID_ARG, "kv is NULL");
+    for (int l = 0; l < h->s.n_layers; ++l) {
+        if (const fp_status rc = check_paged(&kv[l], chunk, !h->unbacked)) return rc;
+        if (kv[l].n_kv_heads != h->s.n_kv_heads || kv[l].head_dim != h->s.head_dim)
+            return fail(FP_ERR_INVALID_ARG, "layer %d's pages have %d kv heads of %d, the fingerprint %d of %d", l, kv[l].n_kv_heads,
+                        kv[l].head_dim, h->s.n_kv_heads, h->s.head_dim);
+    }
+    if (chunk->n_rows > (int64_t)h->s.max_batch * h->s.max_prompt)
+        return fail(FP_ERR_CAPACITY, "%d rows > max_batch * max_prompt = %lld", chunk->n_rows, (long long)h->s.max_batch * h->s.max_prompt);
+    if (chunk->max_len > h->s.max_seq) return fail(FP_ERR_CAPACITY, "max_len %d > max_seq %d", chunk->max_len, h->s.max_seq);
+    return FP_OK;
+}
+
+fp_status fp_extend_workspace(const fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, size_t* bytes) {
+    if (!bytes) return fail(FP_ERR_INVALID_ARG, "bytes is NULL");
+    if (const fp_status rc = check_extend(h, kv, chunk)) return rc;
+    *bytes = attn_chunk_ws_bytes(kv[0], *chunk, h->s.n_heads);
+    return FP_OK;
+}
+
+fp_status fp_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, const void* x, void* y, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+    if (const fp_status rc = check_extend(h, kv, chunk)) return rc;
+    if (!x || !y) return fail(FP_ERR_INVALID_ARG, "x and y must be device pointers");
+    const size_t bytes = (size_t)chunk->n_rows * h->s.hidden * 2;
+    if (overlap(x, bytes, y, bytes)) return fail(FP_ERR_INVALID_ARG, "x and y overlap");
+    const size_t need = attn_chunk_ws_bytes(kv[0], *chunk, h->s.n_heads);
+    if (!workspace || (uintptr_t)workspace % 16 != 0) return fail(FP_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device pointer");
+    if (workspace_bytes < need) return fail(FP_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    if (h->unbacked || chunk->n_rows == 0) return FP_OK;
+    return enqueue_extend(h, kv, *chunk, (const uint16_t*)x, (uint16_t*)y, (float*)workspace, (hipStream_t)stream);
 }
 
 fp_status fp_set_decode_graph(fp_layer* h, int32_t enable) {

@@ -281,6 +281,7 @@ struct KvReadArgs {
     uint16_t* k_out;
     uint16_t* v_out;
 };
+fp_status check_paged(const fp_paged_kv* kv, const fp_chunk* c, bool pointers);
 hipError_t launch_kv_append(const KvAppendArgs& a, bool f32, hipStream_t st);
 hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st);
 

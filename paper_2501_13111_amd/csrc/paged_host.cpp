@@ -48,8 +48,12 @@ fp_status check_shape(const fp_paged_kv* kv, const fp_chunk* c) {
     return FP_OK;
 }
 
-fp_status check_chunk(const fp_paged_kv* kv, const fp_chunk* c) {
+}  // namespace
+
+// The pages' and the chunk's checks, with their pointers' if `pointers`.
+fp_status fpk::check_paged(const fp_paged_kv* kv, const fp_chunk* c, bool pointers) {
     if (const fp_status s = check_shape(kv, c)) return s;
+    if (!pointers) return FP_OK;
     if (!kv->k || !kv->v || !aligned(kv->k, 16) || !aligned(kv->v, 16))
         return fail(FP_ERR_INVALID_ARG, "k and v pools must be 16-byte aligned device pointers");
     if (kv->format == FP_KV_INT8 && (!kv->k_scales || !kv->v_scales || !aligned(kv->k_scales, 16) || !aligned(kv->v_scales, 16)))
@@ -57,6 +61,10 @@ fp_status check_chunk(const fp_paged_kv* kv, const fp_chunk* c) {
     if (!c->row_start || !c->ctx_len || !c->table) return fail(FP_ERR_INVALID_ARG, "row_start, ctx_len and table must be device pointers");
     return FP_OK;
 }
+
+namespace {
+
+fp_status check_chunk(const fp_paged_kv* kv, const fp_chunk* c) { return check_paged(kv, c, true); }
 
 fp_status check_heads(const fp_paged_kv* kv, int n_heads) {
     if (n_heads < 1 || n_heads % kv->n_kv_heads != 0)

@@ -100,7 +100,8 @@ class PagedKV:
                   for t, nm in ((k_scales, "k_scales"), (v_scales, "v_scales"))]
         elif k_scales is not None or v_scales is not None:
             raise ValueError("a bf16 cache has no scales")
-        self.c = ctypes.byref(_PagedKv(KVQ[self.kvq], n, ps, h, d, kp, vp, *sp))
+        self.struct = _PagedKv(KVQ[self.kvq], n, ps, h, d, kp, vp, *sp)
+        self.c = ctypes.byref(self.struct)
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, kvq: str = "bf16", device="cuda"):
