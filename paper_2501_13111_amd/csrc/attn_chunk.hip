@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
     constexpr int RS = D + 4;
     __shared__ __attribute__((aligned(16))) float ow[4][RT * RS];
     __shared__ float mw[4][RT], lw[4][RT];
+    __shared__ int sw[4];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -134,9 +135,29 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
     }
     const float sl2 = a.scale * 1.4426950408889634f;
 
+    bool strays = false;
     auto compute = [&](int i, Chunk<D, KV8>& c) {
         const int base = (beg + w + 4 * i) * VT_BLK;
         float ksc[2][4], vsc[2][4], lk = 0.f;
+        if (base + VT_BLK > sq.ctx + 1) {        // some row may not see all of the block
+            uint32_t bad = 0;
+            if constexpr (KV8) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    bad |= nonfinite<F16_EXP>(c.vs[t].x) | nonfinite<F16_EXP>(c.vs[t].y);
+                    c.vs[t] = u32x2{finite_halves<F16_EXP>(c.vs[t].x), finite_halves<F16_EXP>(c.vs[t].y)};
+                }
+            } else {
+#pragma unroll
+                for (int dd = 0; dd < ND; ++dd)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        bad |= nonfinite<BF16_EXP>(c.v[dd][x]);
+                        c.v[dd][x] = finite_halves<BF16_EXP>(c.v[dd][x]);
+                    }
+            }
+            strays |= __ballot(bad != 0) != 0;
+        }
         if constexpr (KV8) {
 #pragma unroll
             for (int t = 0; t < 2; ++t)
@@ -152,13 +173,8 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
 #pragma unroll
             for (int dd = 0; dd < ND; ++dd) {
                 if constexpr (!KV8) {
-                    u32x4 m;
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {        // word x: slots 8 g + 2 x, + 1: keys 16 (x / 2) + 4 g + 2 (x % 2), + 1
-                        const int key = 16 * (x >> 1) + 4 * g + 2 * (x & 1);
-                        m[x] = (key < nk ? 0x0000FFFFu : 0u) | (key + 1 < nk ? 0xFFFF0000u : 0u);
-                    }
-                    c.v[dd] &= m;
+                    for (int x = 0; x < 4; ++x) c.v[dd][x] &= slots_below(g, x, nk);
                 }
             }
             if constexpr (KV8) {
@@ -175,10 +191,10 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) m = fmaxf(m, vsc[t][e]);
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, fabsf(vsc[t][e]));
             m = fmaxf(m, __shfl_xor(m, 16, 64));
             m = fmaxf(m, __shfl_xor(m, 32, 64));
-            lk = __builtin_amdgcn_logf(m) - 15.f;
+            lk = __builtin_amdgcn_logf(fminf(m, 65504.f)) - 15.f;
         }
         u32x4 kf[2][NJ];
 #pragma unroll
@@ -275,6 +291,7 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
             lw[w][16 * t + r] = l_run[t];
         }
     }
+    if (lane == 0) sw[w] = strays;
     // merge the four waves
 #pragma unroll
     for (int t = 0; t < NT; ++t)
@@ -297,6 +314,14 @@ __global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnCh
             o += *(const f32x4*)&ow[v][c * RS + d0] * e;
         }
         const int rho = row0 + c;
+        if (sw[0] | sw[1] | sw[2] | sw[3]) {
+#pragma unroll 1
+            for (int e = 0; e < 4; ++e) {
+                const float x = stray_sum<D, KV8>(a, b, kvh, d0 + e, max(beg, (sq.ctx + 1) / VT_BLK) * VT_BLK,
+                                                  min(sq.ctx + rho / G, end * VT_BLK - 1));
+                o += f32x4{e == 0 ? x : 0.f, e == 1 ? x : 0.f, e == 2 ? x : 0.f, e == 3 ? x : 0.f};
+            }
+        }
         if (un.pieces == 1) {
             store4(a.out + ((int64_t)(sq.row0 + rho / G) * a.n_heads + kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
         } else {

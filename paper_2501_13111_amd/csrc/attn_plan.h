@@ -132,6 +132,43 @@ __device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, int RT,
     return true;
 }
 
+// Slots of a value block are keys 16 (x / 2) + 4 g + 2 (x % 2), + 1 in word x of the eight of chunk g:
+// the bits of those below key n.
+__device__ __forceinline__ uint32_t slots_below(int g, int x, int n) {
+    const int key = 16 * (x >> 1) + 4 * g + 2 * (x & 1);
+    return (key < n ? 0x0000FFFFu : 0u) | (key + 1 < n ? 0xFFFF0000u : 0u);
+}
+// The high bits of the halves of w whose exponent bits E are all ones.
+template <uint32_t E>
+__device__ __forceinline__ uint32_t nonfinite(uint32_t w) {
+    constexpr uint32_t M = E * 0x10001u, A = (0x8000u - E) * 0x10001u;
+    return ((w & M) + A) & 0x80008000u;
+}
+constexpr uint32_t BF16_EXP = 0x7F80u, F16_EXP = 0x7C00u;
+// w with those halves zero
+template <uint32_t E>
+__device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
+    return w & ~((nonfinite<E>(w) >> 15) * 0xFFFFu);
+}
+
+// Infinite and NaN values that some rows of a tile do not see would make NaN of their zero probabilities.
+// The kernels take them out of the products; this is what they are to a row that sees them: the sum of those of
+// dim d at positions first .. last, 0 if there are none (rare, and not quick).
+template <int D, bool KV8>
+__device__ __forceinline__ float stray_sum(const AttnChunkArgs& a, int b, int kvh, int d, int first, int last) {
+    float sum = 0.f;
+    for (int p = first; p <= last; ++p) {
+        const int pb = pool_block(a.kv, a.chunk, b, kvh, p / VT_BLK), t = p % VT_BLK;
+        if (pb < 0) continue;
+        const int64_t at = ((int64_t)pb * D + d) * VT_BLK + vt_slot(t);
+        float v;
+        if constexpr (KV8) v = (float)((const int8_t*)a.kv.v)[at] * h2f(((const uint16_t*)a.kv.v_scales)[(int64_t)pb * VT_BLK + t]);
+        else v = __uint_as_float((uint32_t)((const uint16_t*)a.kv.v)[at] << 16);
+        if (!(fabsf(v) < INFINITY)) sum += v;
+    }
+    return sum;
+}
+
 constexpr int wst(int D) { return D + 4; }     // floats per row of a piece: o, then m, l
 
 __device__ __forceinline__ void store4(uint16_t* p, f32x4 v, int fmt) {

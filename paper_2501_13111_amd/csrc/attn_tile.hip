@@ -71,6 +71,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     const int wr0 = row0 + 64 * w, wrows = min(max(rows - 64 * w, 0), 64);
     const int nw = uni(wrows > 0 ? min(n, (sq.ctx + (wr0 + wrows - 1) / G) / VT_BLK + 1 - beg) : 0);
     const int wfull = uni((sq.ctx + wr0 / G + 1) / VT_BLK - beg);
+    // From block `edge` on some row of the tile does not see every key.  Values there that are not finite
+    // would make NaN of its zero probabilities: they are taken out, and what they are to the rows that
+    // do see them is written at the end.
+    const int edge = uni((sq.ctx + row0 / G + 1) / VT_BLK - beg);
+    __shared__ int stray;
+    if (tid == 0) stray = 0;
 
     // ---- staging.  The pool blocks of 64 blocks at a time are held across the lanes.
     constexpr int KB = VT_BLK * D * (KV8 ? 1 : 2);
@@ -154,6 +160,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         else if (stager) *(u32x4*)(vst + (i & (RING - 1)) * SB + (x >> 1) * 256) = u32x4{half.x, half.y, v.x, v.y};
     };
     // Scales of positions past the sequence may be anything: zero in the block where it ends.
+    // int8: values are finite if their scales are.
     auto clear_tail = [&](int i, Raw& r) {
         if constexpr (KV8) {
             if ((beg + i + 1) * VT_BLK > sq.len) {
@@ -164,6 +171,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                     r.sb[x] &= (2 * x + 16 < nk ? 0xFFFFu : 0u) | (2 * x + 17 < nk ? 0xFFFF0000u : 0u);
                 }
             }
+            if (i >= edge) {
+                uint32_t bad = 0;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    bad |= nonfinite<F16_EXP>(r.sa[x]) | nonfinite<F16_EXP>(r.sb[x]);
+                    r.sa[x] = finite_halves<F16_EXP>(r.sa[x]);
+                    r.sb[x] = finite_halves<F16_EXP>(r.sb[x]);
+                }
+                if (bad) stray = 1;
+            }
         }
     };
     auto stage = [&](int i, Raw& r) {
@@ -172,6 +189,29 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         for (int x = 0; x < 4; ++x) stage_k(i, r, x);
 #pragma unroll
         for (int x = 0; x < 4; ++x) stage_v(i, r, x);
+    };
+
+    // bf16: a block's values in LDS, each wave a quarter, before the barrier that ends the trip
+    auto scrub = [&](int i) {
+        if constexpr (!KV8) {
+            char* const v = smem + (i & (RING - 1)) * SB + NKC * 1024 + 16 * tid;
+#pragma unroll
+            for (int x = 0; x < NVC / 4; ++x) {
+                u32x4 y = *(const u32x4*)(v + 4096 * x);
+                if (nonfinite<BF16_EXP>(y.x) | nonfinite<BF16_EXP>(y.y) | nonfinite<BF16_EXP>(y.z) | nonfinite<BF16_EXP>(y.w)) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = finite_halves<BF16_EXP>(y[e]);
+                    *(u32x4*)(v + 4096 * x) = y;
+                    stray = 1;
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+    };
+    // what trip i begins with: the next pages, and block i + 1, which the last barrier has made whole
+    auto begin = [&](int i) {
+        turn_pages(i + 4);
+        if (!KV8 && i + 1 >= edge) scrub(i + 1);
     };
 
     // ---- queries: columns 32 c + l % 32 of the wave; a negative scale turns their signs
@@ -408,6 +448,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
             }
             // blocks 0 and 1
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * JPW) : "memory");
+            if (edge <= 0) {
+                scrub(0);
+                asm volatile("s_barrier" ::: "memory");
+            }
         }
         int i = 0;
         if (nw > 0) {
@@ -440,14 +484,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
             while (i < nw) {
                 bool more = false;
                 while (!more && i + 1 < ne) {
-                    turn_pages(i + 4);
+                    begin(i);
                     clear_tail(i + 2, ra);
                     trip(i, cur, nxt, pa, pb, ra, F_{});
                     meet();
                     ++i;
                     more = grown();
                     if (!more) {
-                        turn_pages(i + 4);
+                        begin(i);
                         clear_tail(i + 2, rb);
                         trip(i, nxt, cur, pb, pa, rb, F_{});
                         meet();
@@ -458,7 +502,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                     }
                 }
                 if (!more && i < nw) {
-                    turn_pages(i + 4);
+                    begin(i);
                     clear_tail(i + 2, ra);
                     trip(i, cur, nxt, pa, pb, ra, T_{});
                     meet();
@@ -488,10 +532,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                 u32x4 v = vfrag((nw - 1) & (RING - 1), x);
                 if constexpr (!KV8) {
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {       // word y: keys 4 (2 j2 + h32) + 16 (y / 2) + 2 (y % 2), + 1
-                        const int key = 4 * (2 * (x / NDT) + h32) + 16 * (y >> 1) + 2 * (y & 1);
-                        v[y] &= (key < nk ? 0x0000FFFFu : 0u) | (key + 1 < nk ? 0xFFFF0000u : 0u);
-                    }
+                    for (int y = 0; y < 4; ++y) v[y] &= slots_below(2 * (x / NDT) + h32, y, nk);
                 }
                 oacc[0][x % NDT] = mfma32<PF>(v, pa.p[0][x / NDT], oacc[0][x % NDT]);
                 oacc[1][x % NDT] = mfma32<PF>(v, pa.p[1][x / NDT], oacc[1][x % NDT]);
@@ -503,7 +544,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
             }
         }
         for (; i < n; ++i) {               // a wave past its rows keeps staging
-            turn_pages(i + 4);
+            begin(i);
             if constexpr (KV8) {
                 stage(i + 2, ra);
                 fetch(i + 4, ra);
@@ -546,6 +587,25 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
             if (h32 == 0) *(f32x2*)(dst + TILE_ROWS * D + 2 * (64 * w + 32 * c + l32)) = f32x2{m_ref[c], l};
         }
     }
+    // what the values taken out are to the rows that see them
+    if (edge < n) {
+        __syncthreads();
+        if (stray == 0) return;
+        for (int x = 0; x < 2 * (D / 2); ++x) {
+            const int c = x & 1, d = 8 * (x >> 3) + 4 * h32 + ((x >> 1) & 3), r = 32 * c + l32;
+            if (r >= wrows) continue;
+            const int seen = sq.ctx + (wr0 + r) / G;
+            const float sum = stray_sum<D, KV8>(a, b, kvh, d, (beg + max(edge, 0)) * VT_BLK, min(seen, (beg + n) * VT_BLK - 1));
+            if (sum == 0.f) continue;
+            // added to what the lane wrote there, which may be infinite or NaN too
+            if (un.pieces == 1) {
+                uint16_t* p = a.out + ((int64_t)(sq.row0 + (wr0 + r) / G) * a.n_heads + kvh * G + (wr0 + r) % G) * D + d;
+                *p = act_store(sum + act_load(*p, a.out_fmt), a.out_fmt);
+            } else {
+                a.ws[(int64_t)un.part * TILE_ROWS * wst(D) + ((2 * w + c) * (4 * NDT) + (d >> 3)) * 256 + 4 * lane + (d & 3)] += sum;
+            }
+        }
+    }
 }
 
 // Joins the pieces of split tiles: D / 4 workgroups a tile, a thread per four dims of a row in the order
@@ -573,7 +633,10 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(AttnChunkArgs a) {
             const float* p = src + min(i0 + j, un.pieces - 1) * step;
             ml[j] = *(const f32x2*)(p + TILE_ROWS * D + 2 * row);
             oi[j] = ((const f32x4*)p)[it];
-            if (i0 + j >= un.pieces) ml[j] = f32x2{-INFINITY, 0.f};
+            if (i0 + j >= un.pieces) {
+                ml[j] = f32x2{M0, 0.f};
+                oi[j] = f32x4{0.f, 0.f, 0.f, 0.f};     // not the last piece's infinite sums again
+            }
         }
         float mn = m;
 #pragma unroll

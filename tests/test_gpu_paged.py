@@ -457,3 +457,52 @@ def test_strided_rows_and_single_rows():
         fp.attn_chunk(kv, chunk, wide[:, ::2][:, :4], out)              # heads apart
     with pytest.raises(FpError):
         fp.attn_chunk(kv, chunk, out, out)                              # q and out overlap
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("nkv,G,d,lens", [
+    (2, 3, 64, [(40, 5), (200, 1), (31, 2), (0, 4)]),
+    (1, 4, 128, [(40, 7), (3000, 8), (95, 1)]),
+    (2, 8, 128, [(64, 8), (2000, 5), (25, 7)]),
+    (2, 4, 64, [(40, 70), (200, 5), (1500, 130), (90, 1)]),
+    (1, 1, 128, [(40, 300), (5, 2), (0, 520)]),
+    (1, 16, 128, [(4000, 33)]),
+])
+def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(nkv, G, d, lens, kvq):
+    fp = _fp()
+    page = 64
+    g, pool, table = _case(lens, page, nkv, d, kvq, 101)
+    _fill(pool, table, lens, g, upto=lambda c, n: c + n)
+
+    def poison(b, pos, dim, x, key=False):
+        pg, off = pool._at(table[b], pos)
+        h = pos % nkv
+        if kvq == "int8":
+            (pool.ks if key else pool.vs)[pg, h, off] = x
+        elif key:
+            pool.k[pg, h, off, dim] = x
+        else:
+            pool.v[pg, h, off // 32, dim, ref.SLOT[off % 32]] = x
+
+    for b, (c, n) in enumerate(lens):
+        if c > 10 and b % 2:
+            poison(b, 10, 7, math.inf)                       # in the context: every row sees it
+        if n > 1:
+            poison(b, c + n // 2, 3, math.nan)
+            poison(b, c + n // 2 + (n > 3), d - 1, -math.inf)
+            poison(b, c + n - 1, 20, math.inf)
+            poison(b, c + n - 1, 5, math.nan, key=True)
+    chunk, starts = _chunk(lens, table)
+    q = torch.randn(starts[-1], nkv * G, d, generator=g).bfloat16()
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    fp.attn_chunk(pool.device(), chunk, q.cuda(), out)
+    want, mag, smag = ref.attention(pool, table, lens, q)
+    got = out.cpu().double()
+    odd = ~want.isfinite()
+    assert odd.any() and not odd.all()
+    gn, wn = torch.nan_to_num(got, 1e30, 2e30, 3e30), torch.nan_to_num(want, 1e30, 2e30, 3e30)
+    wrong = [(i.tolist(), float(got[tuple(i)]), float(want[tuple(i)])) for i in ((gn != wn) & odd).nonzero()[:8]]
+    assert not wrong
+    ds = 2 * (d + 4) * EPS32 * smag + (2 * 2.0 ** -11 * smag if kvq == "int8" else 0.0)
+    tol = HALF_BF16 * want.abs() + (HALF_BF16 + 2 * ds + 1e-5 + 2.0 ** -11) * mag * (1 + HALF_BF16)
+    assert ((got - want).abs() <= tol)[~odd].all()
