@@ -199,3 +199,17 @@ def test_speculative_decoding_run(T):
                 hist[b] += toks[b]
                 accepted += len(toks[b]) - 1
         assert accepted > 0 or T > 0        # (at T the nearly flat logits accept one token in hundreds)
+
+
+@pytest.mark.parametrize("max_batch", [1, 3])
+@pytest.mark.parametrize("wq,kvq", [("bf16", "int8"), ("int8", "bf16"), ("int4", "int8"), ("sp24", "bf16")])
+def test_one_sequence_token_by_token(wq, kvq, max_batch):
+    """A prompt, then calls of a single row."""
+    from paper_2501_13111_amd import Fingerprint
+    s = Shape(2, 256, 4, 2, 64, 512, max_batch, 40, 90)
+    x = bf16_round(np.random.default_rng(11).normal(0, 1, (46, s.hidden)).astype(np.float32))
+    want = OracleFingerprint(s, wq, kvq, seed=12).prefill(x[None])[0]
+    with Fingerprint(s, wq, kvq, seed=12) as f:
+        p = Paged(f, kvq, 32, [90])
+        got = [p.extend([x[:40]])[0]] + [p.extend([x[i:i + 1]])[0] for i in range(40, 46)]
+    assert rel_inf(np.concatenate(got), want) <= TOL
