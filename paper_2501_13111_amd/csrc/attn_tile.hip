@@ -75,8 +75,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     // would make NaN of its zero probabilities: they are taken out, and what they are to the rows that
     // do see them is written at the end.
     const int edge = uni((sq.ctx + row0 / G + 1) / VT_BLK - beg);
-    __shared__ int stray;
-    if (tid == 0) stray = 0;
+    __shared__ int sw[4];
+    bool strays = false;                   // this wave has taken some out
 
     // ---- staging.  The pool blocks of 64 blocks at a time are held across the lanes.
     constexpr int KB = VT_BLK * D * (KV8 ? 1 : 2);
@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                     r.sa[x] = finite_halves<F16_EXP>(r.sa[x]);
                     r.sb[x] = finite_halves<F16_EXP>(r.sb[x]);
                 }
-                if (bad) stray = 1;
+                strays |= __ballot(bad != 0) != 0;
             }
         }
     };
@@ -195,16 +195,19 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     auto scrub = [&](int i) {
         if constexpr (!KV8) {
             char* const v = smem + (i & (RING - 1)) * SB + NKC * 1024 + 16 * tid;
+            uint32_t bad = 0;
 #pragma unroll
             for (int x = 0; x < NVC / 4; ++x) {
                 u32x4 y = *(const u32x4*)(v + 4096 * x);
-                if (nonfinite<BF16_EXP>(y.x) | nonfinite<BF16_EXP>(y.y) | nonfinite<BF16_EXP>(y.z) | nonfinite<BF16_EXP>(y.w)) {
+                const uint32_t odd = nonfinite<BF16_EXP>(y.x) | nonfinite<BF16_EXP>(y.y) | nonfinite<BF16_EXP>(y.z) | nonfinite<BF16_EXP>(y.w);
+                if (odd) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) y[e] = finite_halves<BF16_EXP>(y[e]);
                     *(u32x4*)(v + 4096 * x) = y;
-                    stray = 1;
                 }
+                bad |= odd;
             }
+            strays |= __ballot(bad != 0) != 0;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
     };
@@ -213,6 +216,24 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         turn_pages(i + 4);
         if (!KV8 && i + 1 >= edge) scrub(i + 1);
     };
+
+    // the first blocks are on their way while the queries are
+    Raw ra, rb, r0, r1;
+    if (n > 0) {
+        pages(0);
+        if constexpr (KV8) {
+            fetch(0, r0);
+            fetch(1, r1);
+            fetch(2, ra);
+            fetch(3, rb);
+        } else {
+            for (int i = 0; i < AHEAD; ++i) {
+                copy_begin(i);
+#pragma unroll
+                for (int x = 0; x < JPW; ++x) copy(x);
+            }
+        }
+    }
 
     // ---- queries: columns 32 c + l % 32 of the wave; a negative scale turns their signs
     u32x4 qf[2][NKC];
@@ -413,7 +434,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     using F_ = std::integral_constant<bool, false>;
 
     if (n > 0) {
-        Raw ra, rb;
         auto swap_raw = [&]() {
             auto swap = [](auto& x, auto& y) {
                 const auto z = x;
@@ -428,24 +448,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                 swap(ra.ks, rb.ks);
             }
         };
-        pages(0);
         // zeros before block 0: trip 0 multiplies them by zero probabilities
         for (int x = tid; x < NVC * 64; x += 256) *(u32x4*)(smem + (RING - 1) * SB + NKC * 1024 + 16 * x) = u32x4{0u, 0u, 0u, 0u};
         if constexpr (KV8) {
-            Raw r0, r1;
-            fetch(0, r0);
-            fetch(1, r1);
-            fetch(2, ra);
-            fetch(3, rb);
             stage(0, r0);
             stage(1, r1);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         } else {
-            for (int i = 0; i < AHEAD; ++i) {
-                copy_begin(i);
-#pragma unroll
-                for (int x = 0; x < JPW; ++x) copy(x);
-            }
             // blocks 0 and 1
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * JPW) : "memory");
             if (edge <= 0) {
@@ -501,28 +510,38 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                         turn();
                     }
                 }
-                if (!more && i < nw) {
+                while (!more && i < nw) {
                     begin(i);
                     clear_tail(i + 2, ra);
                     trip(i, cur, nxt, pa, pb, ra, T_{});
                     meet();
                     ++i;
                     turn();
+                    more = grown();
                 }
-                // one accumulation register after another (multiplied in plain code, all of them would move to
-                // vector registers, and be copied in the loop)
+                // in accumulation registers, four at a time (multiplied in plain code, all of them would move
+                // to vector registers, and be copied in the loop)
                 static_for<2>([&](auto c) {
                     static_for<NDT + 1>([&](auto dd) {
-                        static_for<16>([&](auto ee) {
-                            constexpr int e = ee, dt = dd;
+                        static_for<4>([&](auto ee) {
+                            constexpr int e = 4 * ee, dt = dd;
                             f32x16& acc = dt < NDT ? oacc[c][dt < NDT ? dt : 0] : lacc[c];
-                            float x = acc[e], v;
-                            asm volatile("v_accvgpr_read_b32 %1, %0\n\ts_nop 1\n\tv_mul_f32 %1, %1, %2\n\ts_nop 1\n\tv_accvgpr_write_b32 %0, %1"
-                                         : "+a"(x), "=&v"(v) : "v"(f[c]));
-                            acc[e] = x;
+                            float x0 = acc[e], x1 = acc[e + 1], x2 = acc[e + 2], x3 = acc[e + 3], v0, v1, v2, v3;
+                            asm volatile("v_accvgpr_read_b32 %4, %0\n\tv_accvgpr_read_b32 %5, %1\n\t"
+                                         "v_accvgpr_read_b32 %6, %2\n\tv_accvgpr_read_b32 %7, %3\n\t"
+                                         "v_mul_f32 %4, %4, %8\n\tv_mul_f32 %5, %5, %8\n\tv_mul_f32 %6, %6, %8\n\tv_mul_f32 %7, %7, %8\n\t"
+                                         "v_accvgpr_write_b32 %0, %4\n\tv_accvgpr_write_b32 %1, %5\n\t"
+                                         "v_accvgpr_write_b32 %2, %6\n\tv_accvgpr_write_b32 %3, %7"
+                                         : "+a"(x0), "+a"(x1), "+a"(x2), "+a"(x3), "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3)
+                                         : "v"(f[c]));
+                            acc[e] = x0;
+                            acc[e + 1] = x1;
+                            acc[e + 2] = x2;
+                            acc[e + 3] = x3;
                         });
                     });
                 });
+                asm volatile("s_nop 4" ::: "memory");      // before a product adds to them
             }
             // the last block's values; a sequence may end inside it, and what lies behind must not meet
             // a zero probability (int8: its scales were cleared)
@@ -589,8 +608,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     }
     // what the values taken out are to the rows that see them
     if (edge < n) {
+        if (lane == 0) sw[w] = strays;
         __syncthreads();
-        if (stray == 0) return;
+        if ((sw[0] | sw[1] | sw[2] | sw[3]) == 0) return;
         for (int x = 0; x < 2 * (D / 2); ++x) {
             const int c = x & 1, d = 8 * (x >> 3) + 4 * h32 + ((x >> 1) & 3), r = 32 * c + l32;
             if (r >= wrows) continue;
