@@ -7,11 +7,21 @@
 
 namespace fpk {
 
+constexpr int TILE_ROWS = 256;             // rows per tile of attn_tile.hip
+constexpr float M0 = -3e38f;               // softmax reference before any score
+
+// Sequences with at most 16 rows to a kv head in a call of 256-row tiles (next tokens beside a prompt's chunk)
+// are streamed like those of a call without larger ones: FEW of their blocks cost about one of a tile's.
+constexpr int FEW = 4;
+__device__ __forceinline__ bool few_rows(const Seq& s, int G) { return s.n * G <= 16; }
+
 struct Plan {
     int tiles, blocks, pieces;             // row tiles, 32-key blocks, pieces per tile
 };
-__device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int RT, int Q) {
+template <int RT>
+__device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int Q, int few) {
     Plan p;
+    if (RT == TILE_ROWS && few_rows(s, G)) Q *= few;
     p.tiles = (s.n * G + RT - 1) / RT;
     p.blocks = s.n > 0 ? (s.len + VT_BLK - 1) / VT_BLK : 0;
     p.pieces = (p.blocks + Q - 1) / Q;
@@ -37,11 +47,12 @@ struct Lanes {
 // for joining, all in blocks.  Several sequences' pieces differ in size and fill each other's gaps: there the aim
 // is lowered by half a piece a tile, which rounding up adds, so that one round holds them.
 // Totals are summed in halves of 24 bits, so that 64 lanes' sums fit.
-__device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, int G, int RT) {
-    if (a.slots > 0 && a.chunk.n_seqs == 1) {
+template <int RT>
+__device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, int G) {
+    if (RT >= 64 && a.chunk.n_seqs == 1) {
         const Seq s{__builtin_amdgcn_readfirstlane(L.s0.row0), __builtin_amdgcn_readfirstlane(L.s0.n),
                     __builtin_amdgcn_readfirstlane(L.s0.ctx), __builtin_amdgcn_readfirstlane(L.s0.len)};
-        const Plan p = plan_seq(s, G, RT, 1);
+        const Plan p = plan_seq<RT>(s, G, 1, 1);
         const int tiles = std::max(1, p.tiles * a.kv.n_kv_heads);        // above 2^31 the launch is refused
         int best = std::max(1, p.blocks), cost = ((tiles - 1 >> a.slots) + 1) * (p.blocks + a.over);
         for (int k = 0; k < 2; ++k) {
@@ -59,13 +70,15 @@ __device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, in
     int64_t total = 0;
     int tiles = 0;
     for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
-        const Plan p = plan_seq(L.get(b0), G, RT, 1);
-        const int64_t t = (int64_t)p.tiles * p.blocks;
-        if (a.slots > 0) tiles += std::min(wave_total(p.tiles), 1 << 20);
+        const Seq s = L.get(b0);
+        const Plan p = plan_seq<RT>(s, G, 1, 1);
+        const bool few = RT == TILE_ROWS && few_rows(s, G);
+        const int64_t t = few ? (p.blocks + FEW - 1) / FEW : (int64_t)p.tiles * p.blocks;
+        if (RT >= 64) tiles += std::min(wave_total(few ? 0 : p.tiles), 1 << 20);
         total += wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24);
     }
     total *= a.kv.n_kv_heads;
-    if (a.slots > 0) {
+    if (RT >= 64) {
         const float aim = fmaxf((float)(1 << a.target) - 0.5f * (float)tiles * (float)a.kv.n_kv_heads, 0.5f * (float)(1 << a.target));
         return std::max(a.min_blocks, (int)fminf((float)total / aim, 1.6e7f) + 1);
     }
@@ -80,28 +93,41 @@ struct Unit {
     int b, kvh, rt, beg, end, pieces, part;
 };
 // Unit u, or false if there are not that many.  SPLIT: u counts the split tiles instead, and the unit
-// is the tile's first piece.  XCD: consecutive units (the row tiles that read the same keys) go to one
-// XCD's workgroups (workgroup i runs on XCD i % 8).
-template <bool SPLIT, bool XCD>
-__device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, int RT, Unit& un) {
+// is the tile's first piece.  SORT: consecutive units (the row tiles that read the same keys) go to one XCD's
+// workgroups (workgroup i runs on XCD i % 8), and those of sequences with few rows, which are short, come last.
+template <int RT, bool SPLIT, bool SORT>
+__device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, Unit& un) {
     const int nkv = a.kv.n_kv_heads, lane = threadIdx.x & 63;
     const Lanes L(a.chunk);
-    const int Q = plan_q(a, L, G, RT);
+    const int Q = plan_q<RT>(a, L, G), few = a.chunk.n_seqs == 1 ? 1 : FEW;
     auto units = [&](const Plan& p) { return SPLIT ? (p.pieces > 1 ? p.tiles * nkv : 0) : p.tiles * p.pieces * nkv; };
     int u = blockIdx.x;
-    if constexpr (XCD) {
-        int all = 0;
-        for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) all += wave_total(units(plan_seq(L.get(b0), G, RT, Q)));
-        const int per = (all + 7) / 8;
-        if (u >> 3 >= per) return false;
-        u = (u & 7) * per + (u >> 3);
+    bool last = false;                         // the sequences with few rows
+    if constexpr (SORT) {
+        int all[2] = {0, 0};
+        for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
+            const Seq s = L.get(b0);
+            const int c = units(plan_seq<RT>(s, G, Q, few));
+            const bool f = few_rows(s, G);
+            all[0] += wave_total(f ? 0 : c);
+            all[1] += wave_total(f ? c : 0);
+        }
+        int per = (all[0] + 7) / 8;
+        last = u >= 8 * per;
+        if (last) {
+            u -= 8 * per;
+            per = (all[1] + 7) / 8;
+        }
+        const int i = u >> 3;
+        u = (u & 7) * per + i;
+        if (i >= per || u >= all[last]) return false;
     }
     int part = 0;
     un.b = -1;
     for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
         const Seq lane_seq = L.get(b0);
-        const Plan p = plan_seq(lane_seq, G, RT, Q);
-        const int c = units(p), sp = p.pieces > 1 ? p.tiles * p.pieces * nkv : 0;
+        const Plan p = plan_seq<RT>(lane_seq, G, Q, few);
+        const int c = !SORT || few_rows(lane_seq, G) == last ? units(p) : 0, sp = p.pieces > 1 ? p.tiles * p.pieces * nkv : 0;
         const int s = wave_scan(c);
         const uint64_t past = __ballot(s > u);
         if (past) {
@@ -117,18 +143,18 @@ __device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, int RT,
         part += wave_total(sp);
     }
     if (un.b < 0) return false;
-    const Plan pl = plan_seq(un.sq, G, RT, Q);
+    const Plan pl = plan_seq<RT>(un.sq, G, Q, few);
     if (u < 0 || u >= units(pl)) return false;         // overlapping rows: sums past int32
     un.pieces = pl.pieces;
     un.rt = u % pl.tiles;
     const int v = u / pl.tiles, sp = SPLIT ? 0 : v % pl.pieces;
     un.kvh = SPLIT ? v : v / pl.pieces;
     un.part = part + (SPLIT ? un.kvh * pl.pieces * pl.tiles + un.rt : u);
-    const int per = (pl.blocks + pl.pieces - 1) / pl.pieces;
-    // no further than the tile's last row sees
-    const int last = min((un.rt + 1) * RT, un.sq.n * G) - 1;
+    // the blocks up to the tile's last row, in equal pieces
+    const int row = min((un.rt + 1) * RT, un.sq.n * G) - 1;
+    const int blocks = min(pl.blocks, (un.sq.ctx + row / G) / VT_BLK + 1), per = (blocks + pl.pieces - 1) / pl.pieces;
     un.beg = sp * per;
-    un.end = min(min(un.beg + per, pl.blocks), (un.sq.ctx + last / G) / VT_BLK + 1);
+    un.end = min(un.beg + per, blocks);
     return true;
 }
 
@@ -178,7 +204,11 @@ __device__ __forceinline__ void store4(uint16_t* p, f32x4 v, int fmt) {
     *(u32x2*)p = u32x2{(uint32_t)x[0] | ((uint32_t)x[1] << 16), (uint32_t)x[2] | ((uint32_t)x[3] << 16)};
 }
 
-constexpr int TILE_ROWS = 256;             // rows per tile of attn_tile.hip
-constexpr float M0 = -3e38f;               // softmax reference before any score
+// Where a piece of a 256-row tile keeps dims d0 .. d0 + 3 of row r: the accumulators as the lanes hold them (whole
+// kilobytes); (m, l) of row r at TILE_ROWS D + 2 r.
+template <int D>
+__device__ __forceinline__ int tile_part(int r, int d0) {
+    return ((r >> 5) * (D / 8) + (d0 >> 3)) * 256 + 4 * ((r & 31) + 8 * (d0 & 4));
+}
 
 }  // namespace fpk

@@ -1,0 +1,329 @@
+// A unit of the chunk attention with few rows: the keys stream past registers.  (attn_chunk.hip has the
+// method.)
+#pragma once
+#include <type_traits>
+
+#include "attn_plan.h"
+
+namespace fpk {
+
+template <int D, bool KV8>
+struct Chunk {
+    static constexpr int NK = KV8 ? D / 64 : D / 32;   // 16-byte key loads per 16-key tile
+    u32x4 k[2][NK];
+    typename std::conditional<KV8, u32x2, u32x4>::type v[D / 16];
+    u32x2 ks[2], vs[2];
+};
+
+// dims that k-step j of lane group g covers (the queries take the same order)
+template <bool KV8>
+__device__ __forceinline__ int qdim(int j, int g) {
+    return KV8 ? 64 * (j >> 1) + 16 * g + 8 * (j & 1) : 32 * j + 8 * g;
+}
+
+// Eight int8 codes -> bf16 (exact).
+__device__ __forceinline__ u32x4 i8x8_to_bf16(uint32_t lo, uint32_t hi) {
+    auto two = [](uint32_t w, int s) {
+        const uint32_t a = __float_as_uint((float)(int8_t)(w >> s)), b = __float_as_uint((float)(int8_t)(w >> (s + 8)));
+        return __builtin_amdgcn_perm(b, a, 0x07060302u);
+    };
+    return u32x4{two(lo, 0), two(lo, 16), two(hi, 0), two(hi, 16)};
+}
+
+// LDS of a unit of 16 NT rows
+template <int D, int NT>
+struct StreamLds {
+    static constexpr int RT = 16 * NT, RS = D + 4;
+    __attribute__((aligned(16))) float ow[4][RT * RS];
+    float mw[4][RT], lw[4][RT];
+    int sw[4];
+};
+
+// One unit of at most 16 NT rows.  TILE: its partial result is laid out as those of the 256-row tiles.
+template <int D, bool KV8, int NT, bool TILE>
+__device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& un, StreamLds<D, NT>& lds) {
+    constexpr int NJ = D / 32, ND = D / 16, RT = 16 * NT;
+    constexpr int NK = Chunk<D, KV8>::NK;
+    constexpr int RS = D + 4;
+    auto& ow = lds.ow;
+    auto& mw = lds.mw;
+    auto& lw = lds.lw;
+    auto& sw = lds.sw;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
+    const Seq& sq = un.sq;
+    const int b = un.b, kvh = un.kvh, beg = un.beg, end = un.end;
+    const int row0 = un.rt * RT, rows = min(RT, sq.n * G - row0);
+
+    // the pool block of this wave's i-th block, 64 of them at a time in the lanes
+    const int n = end > beg ? (end - beg - w + 3) / 4 : 0;
+    int pbs = 0;
+    auto pages = [&](int i0) {
+        const int i = i0 + lane;
+        pbs = i < n ? pool_block(a.kv, a.chunk, b, kvh, beg + w + 4 * i) : -1;
+    };
+    pages(0);                                   // on its way while the queries are addressed
+    // queries: column c of tile t is row row0 + 16 t + c
+    u32x4 qf[NT][NJ];
+    int lim[NT];                                 // last position that the lane's row sees
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int rho = row0 + 16 * t + r;
+        const bool live = 16 * t + r < rows;
+        const int tok = live ? rho / G : 0, h = live ? rho % G : 0;
+        lim[t] = live ? sq.ctx + tok : -1;
+        const uint16_t* q = a.q + (int64_t)(sq.row0 + tok) * a.q_stride + (kvh * G + h) * D;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            const u32x4 x = *(const u32x4*)(q + qdim<KV8>(j, g));
+            qf[t][j] = live ? x : u32x4{0u, 0u, 0u, 0u};
+        }
+    }
+
+    constexpr int KB = VT_BLK * D * (KV8 ? 1 : 2);      // bytes of a block of keys, and of values
+    auto load = [&](int i, Chunk<D, KV8>& c) {
+        const int pb = __builtin_amdgcn_readlane(pbs, i & 63);
+        const bool ok = pb >= 0;
+        const int64_t at = ok ? pb : 0;
+        const auto rk = buf_rsrc((const char*)a.kv.k + at * KB, ok ? KB : 0);
+        const auto rv = buf_rsrc((const char*)a.kv.v + at * KB, ok ? KB : 0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int x = 0; x < NK; ++x)
+                c.k[t][x] = __builtin_amdgcn_raw_buffer_load_b128(rk, (16 * t + r) * D * (KV8 ? 1 : 2) + 64 * x + 16 * g, 0, 0);
+#pragma unroll
+        for (int dd = 0; dd < ND; ++dd) {
+            const int off = ((16 * dd + r) * VT_BLK + 8 * g) * (KV8 ? 1 : 2);
+            if constexpr (KV8) c.v[dd] = __builtin_amdgcn_raw_buffer_load_b64(rv, off, 0, 0);
+            else c.v[dd] = __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0);
+        }
+        if constexpr (KV8) {
+            const auto sk = buf_rsrc(a.kv.k_scales + at * VT_BLK, ok ? 2 * VT_BLK : 0);
+            const auto sv = buf_rsrc(a.kv.v_scales + at * VT_BLK, ok ? 2 * VT_BLK : 0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                c.ks[t] = __builtin_amdgcn_raw_buffer_load_b64(sk, (16 * t + 4 * g) * 2, 0, 0);
+                c.vs[t] = __builtin_amdgcn_raw_buffer_load_b64(sv, (16 * t + 4 * g) * 2, 0, 0);
+            }
+        }
+    };
+
+    f32x4 oacc[NT][ND];
+    float m_run[NT], l_run[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m_run[t] = -INFINITY;
+        l_run[t] = 0.f;
+#pragma unroll
+        for (int dd = 0; dd < ND; ++dd) oacc[t][dd] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float sl2 = a.scale * 1.4426950408889634f;
+
+    bool strays = false;
+    auto compute = [&](int i, Chunk<D, KV8>& c) {
+        const int base = (beg + w + 4 * i) * VT_BLK;
+        float ksc[2][4], vsc[2][4], lk = 0.f;
+        if (base + VT_BLK > sq.ctx + 1) {        // some row may not see all of the block
+            uint32_t bad = 0;
+            if constexpr (KV8) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    bad |= nonfinite<F16_EXP>(c.vs[t].x) | nonfinite<F16_EXP>(c.vs[t].y);
+                    c.vs[t] = u32x2{finite_halves<F16_EXP>(c.vs[t].x), finite_halves<F16_EXP>(c.vs[t].y)};
+                }
+            } else {
+#pragma unroll
+                for (int dd = 0; dd < ND; ++dd)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        bad |= nonfinite<BF16_EXP>(c.v[dd][x]);
+                        c.v[dd][x] = finite_halves<BF16_EXP>(c.v[dd][x]);
+                    }
+            }
+            strays |= __ballot(bad != 0) != 0;
+        }
+        if constexpr (KV8) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    ksc[t][e] = h2f((uint16_t)((e < 2 ? c.ks[t].x : c.ks[t].y) >> (16 * (e & 1)))) * sl2;
+                    vsc[t][e] = h2f((uint16_t)((e < 2 ? c.vs[t].x : c.vs[t].y) >> (16 * (e & 1))));
+                }
+        }
+        // positions past the sequence hold anything: their values must not meet a zero probability
+        if (base + VT_BLK > sq.len) {
+            const int nk = sq.len - base;
+#pragma unroll
+            for (int dd = 0; dd < ND; ++dd) {
+                if constexpr (!KV8) {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) c.v[dd][x] &= slots_below(g, x, nk);
+                }
+            }
+            if constexpr (KV8) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) vsc[t][e] = 16 * t + 4 * g + e < nk ? vsc[t][e] : 0.f;
+            }
+        }
+        // P v_scale is at most 2^15: log2 of the block's largest value scale, less 15.  Products down to
+        // 2^-29 of the largest keep fp16's full precision.
+        if constexpr (KV8) {
+            float m = 5.9604645e-8f;             // 2^-24, the least fp16
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, fabsf(vsc[t][e]));
+            m = fmaxf(m, __shfl_xor(m, 16, 64));
+            m = fmaxf(m, __shfl_xor(m, 32, 64));
+            lk = __builtin_amdgcn_logf(fminf(m, 65504.f)) - 15.f;
+        }
+        u32x4 kf[2][NJ];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                if constexpr (KV8) {
+                    const u32x4 x = c.k[t][j >> 1];
+                    kf[t][j] = (j & 1) ? i8x8_to_bf16(x.z, x.w) : i8x8_to_bf16(x.x, x.y);
+                } else {
+                    kf[t][j] = c.k[t][j];
+                }
+            }
+        u32x4 pf[NT];
+        float al[NT];
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+            float s[2][4];
+            float mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc = mfma_bf16(kf[t][j], qf[q][j], acc);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = KV8 ? acc[e] * ksc[t][e] : acc[e] * sl2;
+                    s[t][e] = base + 16 * t + 4 * g + e <= lim[q] ? v : -INFINITY;
+                    mx = fmaxf(mx, s[t][e]);
+                }
+            }
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float m_new = fmaxf(m_run[q], mx + lk);
+            const float ms = m_new == -INFINITY ? 0.f : m_new;        // nothing seen yet: all zero
+            al[q] = __builtin_amdgcn_exp2f(m_run[q] - ms);
+            m_run[q] = m_new;
+            float ps = 0.f;
+            uint32_t pw[4];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    p[e] = __builtin_amdgcn_exp2f(s[t][e] - ms);
+                    ps += p[e];
+                    if constexpr (KV8) p[e] *= vsc[t][e];
+                }
+                pw[2 * t] = KV8 ? pack_f16_hw(p[0], p[1]) : pack_bf16_hw(p[0], p[1]);
+                pw[2 * t + 1] = KV8 ? pack_f16_hw(p[2], p[3]) : pack_bf16_hw(p[2], p[3]);
+            }
+            l_run[q] = l_run[q] * al[q] + ps;     // this lane's keys; the lane groups join at the end
+            pf[q] = u32x4{pw[0], pw[1], pw[2], pw[3]};
+        }
+#pragma unroll
+        for (int dd = 0; dd < ND; ++dd) {
+            u32x4 vf;
+            if constexpr (KV8) {
+                const u32x2 c0 = i8x4_to_f16x4(c.v[dd].x), c1 = i8x4_to_f16x4(c.v[dd].y);
+                vf = u32x4{c0.x, c0.y, c1.x, c1.y};
+            } else {
+                vf = c.v[dd];
+            }
+#pragma unroll
+            for (int q = 0; q < NT; ++q) {
+                oacc[q][dd] *= al[q];
+                oacc[q][dd] = mfma16<KV8 ? ACT_F16 : ACT_BF16>(vf, pf[q], oacc[q][dd]);
+            }
+        }
+    };
+
+    if (n > 0) {
+        // two blocks in flight; past the last the loads fetch it again, so that every trip issues
+        // the same number
+        Chunk<D, KV8> ca, cb;
+        load(0, ca);
+        load(min(1, n - 1), cb);
+        int i = 0;
+        for (; i + 2 <= n; i += 2) {
+            if (((i + 2) & 63) == 0 && i + 2 < n) pages(i + 2);
+            compute(i, ca);
+            load(min(i + 2, n - 1), ca);
+            compute(i + 1, cb);
+            load(min(i + 3, n - 1), cb);
+        }
+        if (i < n) compute(i, ca);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        l_run[t] += __shfl_xor(l_run[t], 16, 64);
+        l_run[t] += __shfl_xor(l_run[t], 32, 64);
+        if (g == 0) {
+            mw[w][16 * t + r] = m_run[t];
+            lw[w][16 * t + r] = l_run[t];
+        }
+    }
+    if (lane == 0) sw[w] = strays;
+    // merge the four waves
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int dd = 0; dd < ND; ++dd) *(f32x4*)(&ow[w][(16 * t + r) * RS + 16 * dd + 4 * g]) = oacc[t][dd];
+    __syncthreads();
+#pragma unroll 4
+    for (int it = tid; it < rows * (D / 4); it += 256) {
+        const int c = it / (D / 4), d0 = it % (D / 4) * 4;
+        float m = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) m = fmaxf(m, mw[v][c]);
+        float l = 0.f;
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const float mv = mw[v][c];
+            const float e = mv == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mv - m);
+            l += lw[v][c] * e;
+            o += *(const f32x4*)&ow[v][c * RS + d0] * e;
+        }
+        const int rho = row0 + c;
+        if (sw[0] | sw[1] | sw[2] | sw[3]) {
+#pragma unroll 1
+            for (int e = 0; e < 4; ++e) {
+                const float x = stray_sum<D, KV8>(a, b, kvh, d0 + e, max(beg, (sq.ctx + 1) / VT_BLK) * VT_BLK,
+                                                  min(sq.ctx + rho / G, end * VT_BLK - 1));
+                o += f32x4{e == 0 ? x : 0.f, e == 1 ? x : 0.f, e == 2 ? x : 0.f, e == 3 ? x : 0.f};
+            }
+        }
+        if (un.pieces == 1) {
+            store4(a.out + ((int64_t)(sq.row0 + rho / G) * a.n_heads + kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
+        } else {
+            const f32x2 ml = f32x2{fmaxf(m, M0), l};
+            if constexpr (TILE) {
+                float* dst = a.ws + (int64_t)un.part * TILE_ROWS * wst(D);
+                *(f32x4*)(dst + tile_part<D>(c, d0)) = o;
+                if (d0 == 0) *(f32x2*)(dst + TILE_ROWS * D + 2 * c) = ml;
+            } else {
+                float* dst = a.ws + ((int64_t)un.part * RT + c) * wst(D);
+                *(f32x4*)(dst + d0) = o;
+                if (d0 == 0) *(f32x2*)(dst + D) = ml;
+            }
+        }
+    }
+}
+
+}  // namespace fpk

@@ -25,7 +25,7 @@
 #include <type_traits>
 #include <utility>
 
-#include "attn_plan.h"
+#include "attn_stream.h"
 #include "lds_copy.h"
 
 namespace fpk {
@@ -62,7 +62,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     const int l32 = lane & 31, h32 = lane >> 5;
     const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
     Unit un;
-    if (!find_unit<false, true>(a, G, TILE_ROWS, un)) return;
+    if (!find_unit<TILE_ROWS, false, true>(a, G, un)) return;
+    if (few_rows(un.sq, G)) {
+        stream_unit<D, KV8, 1, true>(a, un, *(StreamLds<D, 1>*)smem);
+        return;
+    }
     const Seq& sq = un.sq;
     const int b = un.b, kvh = un.kvh, row0 = un.rt * TILE_ROWS, rows = min(TILE_ROWS, sq.n * G - row0);
     auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
@@ -596,7 +600,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         } else {
             // a piece: the accumulators as the lanes hold them (whole kilobytes), then (m, l) of each row
             float* dst = a.ws + (int64_t)un.part * TILE_ROWS * wst(D);
-            f32x4* od = (f32x4*)dst + (2 * w + c) * (4 * NDT) * 64 + lane;
+            f32x4* od = (f32x4*)(dst + tile_part<D>(64 * w + 32 * c + l32, 4 * h32));
 #pragma unroll
             for (int dt = 0; dt < NDT; ++dt)
 #pragma unroll
@@ -622,7 +626,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                 uint16_t* p = a.out + ((int64_t)(sq.row0 + (wr0 + r) / G) * a.n_heads + kvh * G + (wr0 + r) % G) * D + d;
                 *p = act_store(sum + act_load(*p, a.out_fmt), a.out_fmt);
             } else {
-                a.ws[(int64_t)un.part * TILE_ROWS * wst(D) + ((2 * w + c) * (4 * NDT) + (d >> 3)) * 256 + 4 * lane + (d & 3)] += sum;
+                a.ws[(int64_t)un.part * TILE_ROWS * wst(D) + tile_part<D>(64 * w + r, d & ~3) + (d & 3)] += sum;
             }
         }
     }
@@ -635,7 +639,7 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(AttnChunkArgs a) {
     constexpr int NDT = D / 32;
     const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
     Unit un;
-    if (!find_unit<true, false>(a, G, TILE_ROWS, un)) return;
+    if (!find_unit<TILE_ROWS, true, false>(a, G, un)) return;
     const int it = blockIdx.y * 256 + threadIdx.x, lane = it & 63;
     const int chunk = (it >> 6) % (4 * NDT), row = 32 * (it / (256 * NDT)) + (lane & 31);
     const int rows = min(TILE_ROWS, un.sq.n * G - un.rt * TILE_ROWS);

@@ -233,6 +233,11 @@ def _fill_gpu(lens, page, nkv, d, kvq, seed, spare=2):
     (8, 2, 128, 256, "bf16", [(0, 1000), (0, 3), (0, 517)]),
     (1, 8, 128, 128, "int8", [(70000, 1), (33, 1), (40000, 1)]),
     (8, 1, 64, 96, "bf16", [(20000, 2)] * 3),
+    # next tokens and a few rows beside chunks
+    (2, 4, 128, 64, "int8", [(30000, 1), (10, 100), (9000, 4), (0, 0), (3, 1)]),
+    (2, 4, 64, 64, "bf16", [(40, 1), (20000, 2), (3000, 300), (7000, 1), (5, 5), (8000, 4), (0, 70)]),
+    (1, 16, 128, 32, "bf16", [(6000, 1)] * 70 + [(100, 40)]),
+    (3, 1, 64, 32, "int8", [(9000, 16), (9000, 17), (50, 70)]),
 ])
 def test_long_attention(nkv, G, d, page, kvq, lens):
     fp = _fp()
