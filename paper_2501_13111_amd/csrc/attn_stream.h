@@ -7,6 +7,17 @@
 
 namespace fpk {
 
+// The largest v of the lanes with this lane's column (l % 16): in registers, where a shuffle goes through LDS.
+__device__ __forceinline__ float max_groups(float v) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// The softmax's reference moves only when a score passes it by 2^SLACK, so that few blocks rescale the sums.
+constexpr float SLACK = 8.f;
+
 template <int D, bool KV8>
 struct Chunk {
     static constexpr int NK = KV8 ? D / 64 : D / 32;   // 16-byte key loads per 16-key tile
@@ -65,9 +76,53 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
         pbs = i < n ? pool_block(a.kv, a.chunk, b, kvh, beg + w + 4 * i) : -1;
     };
     pages(0);                                   // on its way while the queries are addressed
-    // queries: column c of tile t is row row0 + 16 t + c
+    constexpr int KB = VT_BLK * D * (KV8 ? 1 : 2);      // bytes of a block of keys, and of values
+    auto load_k = [&](int i, Chunk<D, KV8>& c) {
+        const int pb = __builtin_amdgcn_readlane(pbs, i & 63);
+        const bool ok = pb >= 0;
+        const int64_t at = ok ? pb : 0;
+        const auto rk = buf_rsrc((const char*)a.kv.k + at * KB, ok ? KB : 0);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int x = 0; x < NK; ++x)
+                c.k[t][x] = __builtin_amdgcn_raw_buffer_load_b128(rk, (16 * t + r) * D * (KV8 ? 1 : 2) + 64 * x + 16 * g, 0, 0);
+        if constexpr (KV8) {
+            const auto sk = buf_rsrc(a.kv.k_scales + at * VT_BLK, ok ? 2 * VT_BLK : 0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) c.ks[t] = __builtin_amdgcn_raw_buffer_load_b64(sk, (16 * t + 4 * g) * 2, 0, 0);
+        }
+    };
+    auto load_v = [&](int i, Chunk<D, KV8>& c) {
+        const int pb = __builtin_amdgcn_readlane(pbs, i & 63);
+        const bool ok = pb >= 0;
+        const int64_t at = ok ? pb : 0;
+        const auto rv = buf_rsrc((const char*)a.kv.v + at * KB, ok ? KB : 0);
+#pragma unroll
+        for (int dd = 0; dd < ND; ++dd) {
+            const int off = ((16 * dd + r) * VT_BLK + 8 * g) * (KV8 ? 1 : 2);
+            if constexpr (KV8) c.v[dd] = __builtin_amdgcn_raw_buffer_load_b64(rv, off, 0, 0);
+            else c.v[dd] = __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0);
+        }
+        if constexpr (KV8) {
+            const auto sv = buf_rsrc(a.kv.v_scales + at * VT_BLK, ok ? 2 * VT_BLK : 0);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) c.vs[t] = __builtin_amdgcn_raw_buffer_load_b64(sv, (16 * t + 4 * g) * 2, 0, 0);
+        }
+    };
+    auto load = [&](int i, Chunk<D, KV8>& c) {
+        load_k(i, c);
+        load_v(i, c);
+    };
+
+    Chunk<D, KV8> ca;
+    if (n > 0) load(0, ca);
+
+    // queries: column c of tile t is row row0 + 16 t + c.  Columns past the last row see no position, so
+    // what they hold does not matter.
     u32x4 qf[NT][NJ];
     int lim[NT];                                 // last position that the lane's row sees
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;      // a negative scale turns the queries' signs
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int rho = row0 + 16 * t + r;
@@ -76,40 +131,8 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
         lim[t] = live ? sq.ctx + tok : -1;
         const uint16_t* q = a.q + (int64_t)(sq.row0 + tok) * a.q_stride + (kvh * G + h) * D;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const u32x4 x = *(const u32x4*)(q + qdim<KV8>(j, g));
-            qf[t][j] = live ? x : u32x4{0u, 0u, 0u, 0u};
-        }
+        for (int j = 0; j < NJ; ++j) qf[t][j] = *(const u32x4*)(q + qdim<KV8>(j, g)) ^ sign;
     }
-
-    constexpr int KB = VT_BLK * D * (KV8 ? 1 : 2);      // bytes of a block of keys, and of values
-    auto load = [&](int i, Chunk<D, KV8>& c) {
-        const int pb = __builtin_amdgcn_readlane(pbs, i & 63);
-        const bool ok = pb >= 0;
-        const int64_t at = ok ? pb : 0;
-        const auto rk = buf_rsrc((const char*)a.kv.k + at * KB, ok ? KB : 0);
-        const auto rv = buf_rsrc((const char*)a.kv.v + at * KB, ok ? KB : 0);
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int x = 0; x < NK; ++x)
-                c.k[t][x] = __builtin_amdgcn_raw_buffer_load_b128(rk, (16 * t + r) * D * (KV8 ? 1 : 2) + 64 * x + 16 * g, 0, 0);
-#pragma unroll
-        for (int dd = 0; dd < ND; ++dd) {
-            const int off = ((16 * dd + r) * VT_BLK + 8 * g) * (KV8 ? 1 : 2);
-            if constexpr (KV8) c.v[dd] = __builtin_amdgcn_raw_buffer_load_b64(rv, off, 0, 0);
-            else c.v[dd] = __builtin_amdgcn_raw_buffer_load_b128(rv, off, 0, 0);
-        }
-        if constexpr (KV8) {
-            const auto sk = buf_rsrc(a.kv.k_scales + at * VT_BLK, ok ? 2 * VT_BLK : 0);
-            const auto sv = buf_rsrc(a.kv.v_scales + at * VT_BLK, ok ? 2 * VT_BLK : 0);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                c.ks[t] = __builtin_amdgcn_raw_buffer_load_b64(sk, (16 * t + 4 * g) * 2, 0, 0);
-                c.vs[t] = __builtin_amdgcn_raw_buffer_load_b64(sv, (16 * t + 4 * g) * 2, 0, 0);
-            }
-        }
-    };
 
     f32x4 oacc[NT][ND];
     float m_run[NT], l_run[NT];
@@ -120,13 +143,15 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
 #pragma unroll
         for (int dd = 0; dd < ND; ++dd) oacc[t][dd] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const float sl2 = a.scale * 1.4426950408889634f;
+    const float sl2 = fabsf(a.scale) * 1.4426950408889634f;
 
     bool strays = false;
-    auto compute = [&](int i, Chunk<D, KV8>& c) {
+    // block i from c; tiles of more rows refill c with block `next`, keys and values as soon as they are used
+    auto compute = [&](int i, Chunk<D, KV8>& c, int next) {
         const int base = (beg + w + 4 * i) * VT_BLK;
         float ksc[2][4], vsc[2][4], lk = 0.f;
-        if (base + VT_BLK > sq.ctx + 1) {        // some row may not see all of the block
+        const bool edge = base + VT_BLK > sq.ctx + 1;        // some row may not see all of the block
+        if (edge) {
             uint32_t bad = 0;
             if constexpr (KV8) {
 #pragma unroll
@@ -171,17 +196,16 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
                     for (int e = 0; e < 4; ++e) vsc[t][e] = 16 * t + 4 * g + e < nk ? vsc[t][e] : 0.f;
             }
         }
-        // P v_scale is at most 2^15: log2 of the block's largest value scale, less 15.  Products down to
-        // 2^-29 of the largest keep fp16's full precision.
+        // P v_scale is at most 2^15: log2 of the block's largest value scale, less 15 and the reference's
+        // slack.  Products down to 2^-21 of the largest keep fp16's full precision.
         if constexpr (KV8) {
             float m = 5.9604645e-8f;             // 2^-24, the least fp16
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) m = fmaxf(m, fabsf(vsc[t][e]));
-            m = fmaxf(m, __shfl_xor(m, 16, 64));
-            m = fmaxf(m, __shfl_xor(m, 32, 64));
-            lk = __builtin_amdgcn_logf(fminf(m, 65504.f)) - 15.f;
+            m = max_groups(m);
+            lk = __builtin_amdgcn_logf(fminf(m, 65504.f)) - (15.f - SLACK);
         }
         u32x4 kf[2][NJ];
 #pragma unroll
@@ -197,27 +221,31 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
             }
         u32x4 pf[NT];
         float al[NT];
+        bool grown = false;
 #pragma unroll
         for (int q = 0; q < NT; ++q) {
-            float s[2][4];
-            float mx = -INFINITY;
+            float s[2][4];                       // scores; int8: to base 2 already
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) acc = mfma_bf16(kf[t][j], qf[q][j], acc);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float v = KV8 ? acc[e] * ksc[t][e] : acc[e] * sl2;
-                    s[t][e] = base + 16 * t + 4 * g + e <= lim[q] ? v : -INFINITY;
-                    mx = fmaxf(mx, s[t][e]);
-                }
+                for (int e = 0; e < 4; ++e) s[t][e] = KV8 ? acc[e] * ksc[t][e] : acc[e];
             }
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float m_new = fmaxf(m_run[q], mx + lk);
+            if (edge) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[t][e] = base + 16 * t + 4 * g + e <= lim[q] ? s[t][e] : -INFINITY;
+            }
+            float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
+                             fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+            mx = max_groups(mx) * (KV8 ? 1.f : sl2) + lk;
+            const float m_new = mx > m_run[q] + SLACK ? mx : m_run[q];
             const float ms = m_new == -INFINITY ? 0.f : m_new;        // nothing seen yet: all zero
             al[q] = __builtin_amdgcn_exp2f(m_run[q] - ms);
+            grown |= al[q] != 1.f;
             m_run[q] = m_new;
             float ps = 0.f;
             uint32_t pw[4];
@@ -226,7 +254,7 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
                 float p[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    p[e] = __builtin_amdgcn_exp2f(s[t][e] - ms);
+                    p[e] = __builtin_amdgcn_exp2f(KV8 ? s[t][e] - ms : fmaf(s[t][e], sl2, -ms));
                     ps += p[e];
                     if constexpr (KV8) p[e] *= vsc[t][e];
                 }
@@ -235,6 +263,13 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
             }
             l_run[q] = l_run[q] * al[q] + ps;     // this lane's keys; the lane groups join at the end
             pf[q] = u32x4{pw[0], pw[1], pw[2], pw[3]};
+        }
+        if constexpr (NT > 1) load_k(next, c);
+        if (__ballot(grown) != 0) {
+#pragma unroll
+            for (int q = 0; q < NT; ++q)
+#pragma unroll
+                for (int dd = 0; dd < ND; ++dd) oacc[q][dd] *= al[q];
         }
 #pragma unroll
         for (int dd = 0; dd < ND; ++dd) {
@@ -246,28 +281,32 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
                 vf = c.v[dd];
             }
 #pragma unroll
-            for (int q = 0; q < NT; ++q) {
-                oacc[q][dd] *= al[q];
-                oacc[q][dd] = mfma16<KV8 ? ACT_F16 : ACT_BF16>(vf, pf[q], oacc[q][dd]);
-            }
+            for (int q = 0; q < NT; ++q) oacc[q][dd] = mfma16<KV8 ? ACT_F16 : ACT_BF16>(vf, pf[q], oacc[q][dd]);
         }
+        if constexpr (NT > 1) load_v(next, c);
     };
 
     if (n > 0) {
-        // two blocks in flight; past the last the loads fetch it again, so that every trip issues
-        // the same number
-        Chunk<D, KV8> ca, cb;
-        load(0, ca);
-        load(min(1, n - 1), cb);
-        int i = 0;
-        for (; i + 2 <= n; i += 2) {
-            if (((i + 2) & 63) == 0 && i + 2 < n) pages(i + 2);
-            compute(i, ca);
-            load(min(i + 2, n - 1), ca);
-            compute(i + 1, cb);
-            load(min(i + 3, n - 1), cb);
+        // 16 rows: two blocks in flight.  More: one, whose parts follow each other, for two do not fit the
+        // registers.  Past the last the loads fetch it again, so that every trip issues the same number.
+        if constexpr (NT == 1) {
+            Chunk<D, KV8> cb;
+            load(min(1, n - 1), cb);
+            int i = 0;
+            for (; i + 2 <= n; i += 2) {
+                if (((i + 2) & 63) == 0 && i + 2 < n) pages(i + 2);
+                compute(i, ca, 0);
+                load(min(i + 2, n - 1), ca);
+                compute(i + 1, cb, 0);
+                load(min(i + 3, n - 1), cb);
+            }
+            if (i < n) compute(i, ca, 0);
+        } else {
+            for (int i = 0; i < n; ++i) {
+                if (((i + 1) & 63) == 0 && i + 1 < n) pages(i + 1);
+                compute(i, ca, min(i + 1, n - 1));
+            }
         }
-        if (i < n) compute(i, ca);
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
