@@ -27,7 +27,7 @@ namespace fpk {
 namespace {
 
 template <int D, bool KV8, int NT>
-__global__ void __launch_bounds__(256, NT == 4 ? 1 : 2) attn_chunk_kernel(AttnChunkArgs a) {
+__global__ void __launch_bounds__(256, NT == 4 && D == 128 ? 1 : 2) attn_chunk_kernel(AttnChunkArgs a) {
     __shared__ StreamLds<D, NT> lds;
     Unit un;
     if (!find_unit<16 * NT, false, false>(a, a.n_heads / a.kv.n_kv_heads, un)) return;
@@ -88,7 +88,7 @@ int tile_rows(const fp_chunk& c, int G) {
 }
 
 // log2 of the pieces a call aims for, and the least number of blocks worth a piece
-int piece_target(int RT) { return RT >= 64 ? 8 : 10; }
+int piece_target(int RT, int D) { return RT == TILE_ROWS || (RT == 64 && D == 128) ? 8 : RT == 64 ? 9 : 10; }
 int piece_min(int RT) { return RT == TILE_ROWS ? 8 : 16; }
 
 }  // namespace
@@ -96,17 +96,17 @@ int piece_min(int RT) { return RT == TILE_ROWS ? 8 : 16; }
 // Split tiles have more than Q blocks, so their pieces number at most twice total / Q, twice the aim.
 size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
     const int RT = tile_rows(c, n_heads / kv.n_kv_heads);
-    return ((size_t)2 << piece_target(RT)) * RT * wst(kv.head_dim) * sizeof(float);
+    return ((size_t)2 << piece_target(RT, kv.head_dim)) * RT * wst(kv.head_dim) * sizeof(float);
 }
 
 template <int D, bool KV8, int RT>
 static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
     const int64_t tiles = std::min<int64_t>((int64_t)a.chunk.n_rows * G, (int64_t)a.chunk.n_rows * G / RT + a.chunk.n_seqs) * nkv;
-    a.target = piece_target(RT);
+    a.target = piece_target(RT, D);
     a.min_blocks = piece_min(RT);
     // tiles of 64 rows and more: one workgroup per CU
-    a.slots = RT >= 64 ? 8 : 0;
+    a.slots = RT >= 64 ? a.target : 0;
     a.over = 10;
     a.join = 8;
     const int64_t pieces = (int64_t)1 << a.target, n = std::max(tiles + pieces, 2 * pieces) + 16;
