@@ -27,7 +27,7 @@ namespace fpk {
 namespace {
 
 template <int D, bool KV8, int NT>
-__global__ void __launch_bounds__(256, NT == 4 && D == 128 ? 1 : 2) attn_chunk_kernel(AttnChunkArgs a) {
+__global__ void __launch_bounds__(256, NT == 1 ? 3 : NT == 4 && D == 128 ? 1 : 2) attn_chunk_kernel(AttnChunkArgs a) {
     __shared__ StreamLds<D, NT> lds;
     Unit un;
     if (!find_unit<16 * NT, false, false>(a, a.n_heads / a.kv.n_kv_heads, un)) return;
@@ -87,16 +87,19 @@ int tile_rows(const fp_chunk& c, int G) {
     return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : TILE_ROWS;
 }
 
-// log2 of the pieces a call aims for, and the least number of blocks worth a piece
-int piece_target(int RT, int D) { return RT == TILE_ROWS || (RT == 64 && D == 128) ? 8 : RT == 64 ? 9 : 10; }
+// log2 of the workgroups that run at a time (those of few rows: a half more), and the least number of blocks
+// worth a piece
+int piece_target(int RT, int D) { return RT == TILE_ROWS || (RT == 64 && D == 128) ? 8 : 9; }
 int piece_min(int RT) { return RT == TILE_ROWS ? 8 : 16; }
+// the most pieces that a call aims for (plan_q)
+int64_t piece_aim(int RT, int D) { return (int64_t)1 << (piece_target(RT, D) + (RT < 64 ? 1 : 0)); }
 
 }  // namespace
 
 // Split tiles have more than Q blocks, so their pieces number at most twice total / Q, twice the aim.
 size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
     const int RT = tile_rows(c, n_heads / kv.n_kv_heads);
-    return ((size_t)2 << piece_target(RT, kv.head_dim)) * RT * wst(kv.head_dim) * sizeof(float);
+    return (size_t)(2 * piece_aim(RT, kv.head_dim)) * RT * wst(kv.head_dim) * sizeof(float);
 }
 
 template <int D, bool KV8, int RT>
@@ -105,11 +108,9 @@ static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     const int64_t tiles = std::min<int64_t>((int64_t)a.chunk.n_rows * G, (int64_t)a.chunk.n_rows * G / RT + a.chunk.n_seqs) * nkv;
     a.target = piece_target(RT, D);
     a.min_blocks = piece_min(RT);
-    // tiles of 64 rows and more: one workgroup per CU
-    a.slots = RT >= 64 ? a.target : 0;
     a.over = 10;
     a.join = 8;
-    const int64_t pieces = (int64_t)1 << a.target, n = std::max(tiles + pieces, 2 * pieces) + 16;
+    const int64_t pieces = piece_aim(RT, D), n = std::max(tiles + pieces, 2 * pieces) + 16;
     if (n > INT_MAX) return hipErrorInvalidValue;
     // tiles that can be split: each has more than Q of the blocks
     const unsigned split = (a.chunk.max_len + VT_BLK - 1) / VT_BLK <= a.min_blocks ? 0u : (unsigned)std::min<int64_t>(tiles, pieces);

@@ -40,12 +40,16 @@ struct Lanes {
     }
     __device__ __forceinline__ Seq get(int b0) const { return b0 == 0 ? s0 : at(b0); }
 };
-// Blocks per piece, Q: about the total over 2^a.target, and at least a.min_blocks.  Where few workgroups run at
-// a time (2^a.slots > 1) and there is one sequence, whose pieces are all alike, a last round of a few pieces
-// would cost as much as a full one: its tiles are cut so that the pieces just fill one round, or two, or not
-// at all, whichever costs least: rounds times (blocks of a piece + a.over, a piece's fixed part), and a.join
-// for joining, all in blocks.  Several sequences' pieces differ in size and fill each other's gaps: there the aim
-// is lowered by half a piece a tile, which rounding up adds, so that one round holds them.
+// Blocks per piece, Q: the total over the pieces to aim for, and at least a.min_blocks.  2^a.target workgroups or so
+// run at a time.
+// One sequence's pieces are all alike.  Of 64 rows and more, a last round of a few pieces would cost as much
+// as a full one: its tiles are cut so that the pieces just fill one round, or two, or not at all, whichever
+// costs least: rounds times (blocks of a piece + a.over, a piece's fixed part), and a.join for joining, all in
+// blocks.  Fewer rows stream at the memory's rate however the rounds fall.
+// Several sequences' pieces differ in size and fill each other's gaps: there the aim is lowered by half a piece
+// a tile, which rounding up adds, so that one round holds them.  Tiles of few rows that fill the round by themselves are
+// cut for two.  (Next tokens of 32 sequences of 16384: int8, 8 kv heads 106 us; aiming for 512 or 1024 whatever the tiles 118,
+// 111.  bf16, 32 kv heads 717; lowered there too 791.)
 // Totals are summed in halves of 24 bits, so that 64 lanes' sums fit.
 template <int RT>
 __device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, int G) {
@@ -54,12 +58,12 @@ __device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, in
                     __builtin_amdgcn_readfirstlane(L.s0.ctx), __builtin_amdgcn_readfirstlane(L.s0.len)};
         const Plan p = plan_seq<RT>(s, G, 1, 1);
         const int tiles = std::max(1, p.tiles * a.kv.n_kv_heads);        // above 2^31 the launch is refused
-        int best = std::max(1, p.blocks), cost = ((tiles - 1 >> a.slots) + 1) * (p.blocks + a.over);
+        int best = std::max(1, p.blocks), cost = ((tiles - 1 >> a.target) + 1) * (p.blocks + a.over);
         for (int k = 0; k < 2; ++k) {
-            const int cut = std::min((1 << (a.slots + k)) / tiles, p.blocks / a.min_blocks);
+            const int cut = std::min((1 << (a.target + k)) / tiles, p.blocks / a.min_blocks);
             if (cut < 2) continue;
             const int Q = (p.blocks + cut - 1) / cut;
-            const int c = ((tiles * cut - 1 >> a.slots) + 1) * (Q + a.over) + a.join;
+            const int c = ((tiles * cut - 1 >> a.target) + 1) * (Q + a.over) + a.join;
             if (c < cost) {
                 cost = c;
                 best = Q;
@@ -74,16 +78,15 @@ __device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, in
         const Plan p = plan_seq<RT>(s, G, 1, 1);
         const bool few = RT == TILE_ROWS && few_rows(s, G);
         const int64_t t = few ? (p.blocks + FEW - 1) / FEW : (int64_t)p.tiles * p.blocks;
-        if (RT >= 64) tiles += std::min(wave_total(few ? 0 : p.tiles), 1 << 20);
+        tiles += std::min(wave_total(few ? 0 : p.tiles), 1 << 20);
         total += wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24);
     }
     total *= a.kv.n_kv_heads;
-    if (RT >= 64) {
-        const float aim = fmaxf((float)(1 << a.target) - 0.5f * (float)tiles * (float)a.kv.n_kv_heads, 0.5f * (float)(1 << a.target));
-        return std::max(a.min_blocks, (int)fminf((float)total / aim, 1.6e7f) + 1);
-    }
-    total = (total + ((int64_t)1 << a.target) - 1) >> a.target;
-    return std::max(a.min_blocks, (int)std::min<int64_t>(total, 1 << 24));
+    const float round = (float)(1 << a.target), nt = (float)tiles * (float)a.kv.n_kv_heads;
+    float aim = fmaxf(round - 0.5f * nt, 0.5f * round);
+    if (RT < 64 && a.chunk.n_seqs == 1) aim = round;
+    if (RT < 64 && nt >= round) aim = 2.f * round;
+    return std::max(a.min_blocks, (int)fminf((float)total / aim, 2.5e8f) + 1);      // above any sequence's blocks
 }
 
 // What a workgroup works on: row tile rt of kv head kvh of sequence b, blocks beg .. end - 1 (one of
