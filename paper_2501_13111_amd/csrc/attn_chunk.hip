@@ -8,16 +8,24 @@
 //     S^T = K Q^T     A = 16 keys, B = the tile's rows (columns)
 //     O^T += V^T P^T  A = 16 dims of a value block, B = the probabilities
 // so a lane holds the scores of 4 + 4 keys of a block for one row, and these are what it supplies
-// to the second product (vt_slot order).  int8: a key's scale multiplies its scores, a value's its
-// probabilities.  Online softmax per row in fp32, base 2.
+// to the second product (vt_slot order).  int8: keys stay codes in bf16 (exact), a key's scale multiplies its
+// scores and a value's its probabilities, which go to fp16 (11 bits; with the scale in them bf16's 8 would add to
+// the codes' own error).  Online softmax per row in fp32, base 2.  (attn_stream.h: a unit's work.)
 //
-// Work is split over the keys: from the lengths in device memory every workgroup works out the
-// same plan, the 32-key blocks per piece Q = max(min_blocks, total blocks / target).  A piece is
-// (sequence, kv head, row tile, Q consecutive blocks at most); its four waves take every fourth
-// block and merge in LDS.  A tile of one piece is written out at once; the pieces of the others
+// Many rows to a kv head take tiles of 256 (attn_tile.hip; tile_rows below has the rule): there the matrix cores
+// bound, here the reads of the cache.
+//
+// Work is split over the keys: from the lengths in device memory every workgroup works out the same plan
+// (attn_plan.h).  A piece is (sequence, kv head, row tile, a run of 32-key blocks); its four waves take every
+// fourth block and merge in LDS.  A tile of one piece is written out at once; the pieces of the others
 // go to the workspace as unnormalised (o, m, l) and a second kernel joins them in order:
 //     m = max m_i,  l = sum l_i 2^(m_i - m),  o = sum o_i 2^(m_i - m) / l.
 // The plan depends on the inputs alone, so results repeat bit for bit.
+//
+// Next tokens of 32 sequences of 4096, 8 kv heads of 128 (268 MB of cache): bf16, 8 rows 51 us (5.2 TB/s, the
+// rate of a large copy), 24 rows 53, 48 rows 70; int8 34, 37, 83.  One sequence of 331 positions, 32 kv heads: 9.7 us, of
+// which 1.4 are the plan, 1.3 the first loads, 4 three blocks a wave and 1.8 the merge (a chain of memory latencies
+// and of code fetched for the first time: a second copy of the block's code cost 1 us).
 #include <climits>
 
 #include "attn_stream.h"
@@ -80,11 +88,22 @@ __global__ void __launch_bounds__(256) attn_chunk_join_kernel(AttnChunkArgs a) {
     store4(a.out + ((int64_t)(un.sq.row0 + rho / G) * a.n_heads + un.kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
 }
 
-// Rows that a sequence can bring to a kv head decide the kernel: up to 64 go to the streaming kernel
-// (tiles of 16, 32 or 64 rows), more to the tiles of 256.
-int tile_rows(const fp_chunk& c, int G) {
-    const int64_t R = (int64_t)std::min(c.max_new, c.n_rows) * G;
-    return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : TILE_ROWS;
+// Rows of a tile, by what a sequence can bring to a kv head and by the call's size.  Up to 64 rows stream (tiles of
+// 16, 32 or 64).  More stream too, in tiles of 64, while those tiles times the blocks that they can see are few: the
+// tiles of 256, where the matrix cores bound, need as many to fill the GPU and their longer start to pay.  us streamed
+// and tiled, at (new tokens after context), 8 heads a kv head:
+//     d 128, bf16   up to 2^13: 512 after 0 21, 34; 512 after 512 32, 35    above: 1024 after 0 61, 49; 1024 after 31744 831, 521
+//     d 64, bf16    up to 2^15: 1024 after 0 32, 35; 128 after 16000 40, 46    above: 2048 after 0 74, 63; 1024 after 31744 402, 375
+//     d 64, int8    always: 512 after 0 14, 33; 2048 after 0 77, 83; 8 sequences of 2048 after 2000 505, 551; 1024 after
+//                   31744 554, 523 (the tiles' unpacking costs as much as their products)
+// (a power of two either way changes a case near the border by a few percent).  32 rows of 64 would be cheaper as 64 with
+// d 64 only: 24 rows of 32 sequences of 4096, d 128, bf16 53, as 64 68; int8 37, 79.
+int tile_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
+    const int64_t G = n_heads / kv.n_kv_heads, R = std::min(c.max_new, c.n_rows) * G;
+    if (R <= 64) return R <= 16 ? 16 : R <= 32 ? 32 : 64;
+    if (kv.head_dim == 64 && kv.format == FP_KV_INT8) return 64;
+    const double work = (double)((c.n_rows * G + 63) / 64) * kv.n_kv_heads * ((c.max_len - 1) / VT_BLK + 1);
+    return work <= (kv.head_dim == 128 ? 8192.0 : 32768.0) ? 64 : TILE_ROWS;
 }
 
 // log2 of the workgroups that run at a time (those of few rows: a half more), and the least number of blocks
@@ -98,7 +117,7 @@ int64_t piece_aim(int RT, int D) { return (int64_t)1 << (piece_target(RT, D) + (
 
 // Split tiles have more than Q blocks, so their pieces number at most twice total / Q, twice the aim.
 size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
-    const int RT = tile_rows(c, n_heads / kv.n_kv_heads);
+    const int RT = tile_rows(kv, c, n_heads);
     return (size_t)(2 * piece_aim(RT, kv.head_dim)) * RT * wst(kv.head_dim) * sizeof(float);
 }
 
@@ -110,10 +129,10 @@ static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     a.min_blocks = piece_min(RT);
     a.over = 10;
     a.join = 8;
-    const int64_t pieces = piece_aim(RT, D), n = std::max(tiles + pieces, 2 * pieces) + 16;
+    const int64_t pieces = piece_aim(RT, D), n = std::max(tiles + pieces, 2 * pieces) + 16 * XCD_RUN;
     if (n > INT_MAX) return hipErrorInvalidValue;
     // tiles that can be split: each has more than Q of the blocks
-    const unsigned split = (a.chunk.max_len + VT_BLK - 1) / VT_BLK <= a.min_blocks ? 0u : (unsigned)std::min<int64_t>(tiles, pieces);
+    const unsigned split = (a.chunk.max_len - 1) / VT_BLK < a.min_blocks ? 0u : (unsigned)std::min<int64_t>(tiles, pieces);
     if constexpr (RT == TILE_ROWS) {
         return launch_attn_tile(a, (unsigned)n, split, st);
     } else {
@@ -127,12 +146,13 @@ static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
 
 template <int D, bool KV8>
 static hipError_t launch_d(const AttnChunkArgs& a, hipStream_t st) {
-    switch (tile_rows(a.chunk, a.n_heads / a.kv.n_kv_heads)) {
+    switch (tile_rows(a.kv, a.chunk, a.n_heads)) {
         case 16: return launch_rt<D, KV8, 16>(a, st);
         case 32: return launch_rt<D, KV8, 32>(a, st);
         case 64: return launch_rt<D, KV8, 64>(a, st);
-        default: return launch_rt<D, KV8, TILE_ROWS>(a, st);
     }
+    if constexpr (D == 64 && KV8) return hipErrorInvalidValue;
+    else return launch_rt<D, KV8, TILE_ROWS>(a, st);
 }
 
 hipError_t launch_attn_chunk(const AttnChunkArgs& a, hipStream_t st) {

@@ -11,19 +11,17 @@ constexpr int TILE_ROWS = 256;             // rows per tile of attn_tile.hip
 constexpr float M0 = -3e38f;               // softmax reference before any score
 
 // Sequences with at most 16 rows to a kv head in a call of 256-row tiles (next tokens beside a prompt's chunk)
-// are streamed like those of a call without larger ones: FEW of their blocks cost about one of a tile's.
-constexpr int FEW = 4;
+// are streamed like those of a call without larger ones.
 __device__ __forceinline__ bool few_rows(const Seq& s, int G) { return s.n * G <= 16; }
 
 struct Plan {
     int tiles, blocks, pieces;             // row tiles, 32-key blocks, pieces per tile
 };
 template <int RT>
-__device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int Q, int few) {
+__device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int Q) {
     Plan p;
-    if (RT == TILE_ROWS && few_rows(s, G)) Q *= few;
     p.tiles = (s.n * G + RT - 1) / RT;
-    p.blocks = s.n > 0 ? (s.len + VT_BLK - 1) / VT_BLK : 0;
+    p.blocks = s.n > 0 ? (s.len - 1) / VT_BLK + 1 : 0;
     p.pieces = (p.blocks + Q - 1) / Q;
     return p;
 }
@@ -56,7 +54,7 @@ __device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, in
     if (RT >= 64 && a.chunk.n_seqs == 1) {
         const Seq s{__builtin_amdgcn_readfirstlane(L.s0.row0), __builtin_amdgcn_readfirstlane(L.s0.n),
                     __builtin_amdgcn_readfirstlane(L.s0.ctx), __builtin_amdgcn_readfirstlane(L.s0.len)};
-        const Plan p = plan_seq<RT>(s, G, 1, 1);
+        const Plan p = plan_seq<RT>(s, G, 1);
         const int tiles = std::max(1, p.tiles * a.kv.n_kv_heads);        // above 2^31 the launch is refused
         int best = std::max(1, p.blocks), cost = ((tiles - 1 >> a.target) + 1) * (p.blocks + a.over);
         for (int k = 0; k < 2; ++k) {
@@ -75,10 +73,9 @@ __device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, in
     int tiles = 0;
     for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
         const Seq s = L.get(b0);
-        const Plan p = plan_seq<RT>(s, G, 1, 1);
-        const bool few = RT == TILE_ROWS && few_rows(s, G);
-        const int64_t t = few ? (p.blocks + FEW - 1) / FEW : (int64_t)p.tiles * p.blocks;
-        tiles += std::min(wave_total(few ? 0 : p.tiles), 1 << 20);
+        const Plan p = plan_seq<RT>(s, G, 1);
+        const int64_t t = (int64_t)p.tiles * p.blocks;
+        tiles += std::min(wave_total(RT == TILE_ROWS && few_rows(s, G) ? 0 : p.tiles), 1 << 20);
         total += wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24);
     }
     total *= a.kv.n_kv_heads;
@@ -96,13 +93,14 @@ struct Unit {
     int b, kvh, rt, beg, end, pieces, part;
 };
 // Unit u, or false if there are not that many.  SPLIT: u counts the split tiles instead, and the unit
-// is the tile's first piece.  SORT: consecutive units (the row tiles that read the same keys) go to one XCD's
+// is the tile's first piece.  SORT: XCD_RUN consecutive units (row tiles that read the same keys) go to one XCD's
 // workgroups (workgroup i runs on XCD i % 8), and those of sequences with few rows, which are short, come last.
+constexpr int XCD_RUN = 4;
 template <int RT, bool SPLIT, bool SORT>
 __device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, Unit& un) {
     const int nkv = a.kv.n_kv_heads, lane = threadIdx.x & 63;
     const Lanes L(a.chunk);
-    const int Q = plan_q<RT>(a, L, G), few = a.chunk.n_seqs == 1 ? 1 : FEW;
+    const int Q = plan_q<RT>(a, L, G);
     auto units = [&](const Plan& p) { return SPLIT ? (p.pieces > 1 ? p.tiles * nkv : 0) : p.tiles * p.pieces * nkv; };
     int u = blockIdx.x;
     bool last = false;                         // the sequences with few rows
@@ -110,26 +108,23 @@ __device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, Unit& u
         int all[2] = {0, 0};
         for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
             const Seq s = L.get(b0);
-            const int c = units(plan_seq<RT>(s, G, Q, few));
+            const int c = units(plan_seq<RT>(s, G, Q));
             const bool f = few_rows(s, G);
             all[0] += wave_total(f ? 0 : c);
             all[1] += wave_total(f ? c : 0);
         }
-        int per = (all[0] + 7) / 8;
-        last = u >= 8 * per;
-        if (last) {
-            u -= 8 * per;
-            per = (all[1] + 7) / 8;
-        }
-        const int i = u >> 3;
-        u = (u & 7) * per + i;
-        if (i >= per || u >= all[last]) return false;
+        constexpr int R = 8 * XCD_RUN;
+        const int first = (all[0] + R - 1) / R * R;
+        last = u >= first;
+        if (last) u -= first;
+        u = u / R * R + u % 8 * XCD_RUN + u % R / 8;
+        if (u >= all[last]) return false;
     }
     int part = 0;
     un.b = -1;
     for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
         const Seq lane_seq = L.get(b0);
-        const Plan p = plan_seq<RT>(lane_seq, G, Q, few);
+        const Plan p = plan_seq<RT>(lane_seq, G, Q);
         const int c = !SORT || few_rows(lane_seq, G) == last ? units(p) : 0, sp = p.pieces > 1 ? p.tiles * p.pieces * nkv : 0;
         const int s = wave_scan(c);
         const uint64_t past = __ballot(s > u);
@@ -146,7 +141,7 @@ __device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, Unit& u
         part += wave_total(sp);
     }
     if (un.b < 0) return false;
-    const Plan pl = plan_seq<RT>(un.sq, G, Q, few);
+    const Plan pl = plan_seq<RT>(un.sq, G, Q);
     if (u < 0 || u >= units(pl)) return false;         // overlapping rows: sums past int32
     un.pieces = pl.pieces;
     un.rt = u % pl.tiles;

@@ -1,5 +1,5 @@
-// A unit of the chunk attention with few rows: the keys stream past registers.  (attn_chunk.hip has the
-// method.)
+// A unit of the chunk attention with few rows: a wave's blocks stream through its registers, keys first, values
+// behind them.  (attn_chunk.hip has the method and what it measured.)
 #pragma once
 #include <type_traits>
 

@@ -1,5 +1,5 @@
-// Chunk attention where a sequence brings many rows to a kv head (a prompt's chunk, or a batch with
-// one in it): tiles of 256 rows.  Rows, pieces and their join are those of attn_chunk.hip.
+// Chunk attention where sequences bring many rows to a kv head (a prompt's chunk, or a batch with one in it):
+// tiles of 256 rows.  Rows, pieces and their join are those of attn_chunk.hip, whose tile_rows says when.
 //
 // A workgroup's four waves hold 64 rows each (two MFMA columns of 32) and walk the same 32-key blocks:
 //     S^T = K Q^T,   O^T += V^T P^T,   l += 1 P^T        on MFMA 32x32x16
@@ -22,6 +22,12 @@
 // int8: keys and values are unpacked to fp16 with their scales (code * scale rounded to 11 bits, so that
 // none may reach 65520: half the error that bf16's 8 bits leave in the output, and the matrix cores take no
 // scale); queries are fp16 too, a row of large ones scaled by a power of two.
+//
+// 1024 tokens after 31744, 32 heads on 4 of 128: bf16 555 us, 0.98 PFLOP/s of the 1.31 that a large library matrix
+// product reaches; int8 640, 0.83 (its unpacking takes the instructions that the longer trip shows); heads of 64, bf16
+// 375, 0.72 (half the products, the same softmax).  A trip of 36 products is 1152 cycles of matrix core and takes some
+// 2000 (int8 2600).  A unit's fixed part is 6 us before the first trip (the plan 1.5, the rest the first blocks and
+// queries at the memory's rate when every unit starts at once) and 2.5 after the last.
 #include <type_traits>
 #include <utility>
 
@@ -120,13 +126,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         lds_copy<16>(crs, voff[x & 1], isv ? t * 1024u : (t & 3) * (16 * D) + (t >> 2) * 128u,
                      __builtin_amdgcn_readfirstlane(cdst + x * 1024));
     };
-    // int8: a thread's 16 codes of a key and 16 slots of a value dim (D = 64: the first 128 threads), and
+    // int8 (D = 128): a thread's 16 codes of a key and 16 slots of a value dim, and
     // their scales: one for the key, those of 16 positions for the values.
     struct Raw {
         u32x4 k, v, sa, sb;
         uint32_t ks;
     };
-    const bool stager = D == 128 || tid < 2 * D;
+    static_assert(!KV8 || D == 128, "256 threads' pieces make a block");
     auto fetch = [&](int i, Raw& x) {
         const int pb = block_of(i);
         const int64_t at = max(pb, 0);
@@ -152,7 +158,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         const u32x2 c = i8x4_to_f16x4(r.k[x]);
         const u32x2 v = u32x2{pk_mul(c.x, s2), pk_mul(c.y, s2)};
         if ((x & 1) == 0) half = v;
-        else if (stager)
+        else
             *(u32x4*)(kst + (i & (RING - 1)) * SB + ((x >> 1) ^ (sa8 & 1)) * 128) = u32x4{half.x, half.y, v.x, v.y};
     };
     auto stage_v = [&](int i, const Raw& r, int x) {
@@ -161,7 +167,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         const u32x2 c = i8x4_to_f16x4(r.v[x]);
         const u32x2 v = u32x2{pk_mul(c.x, s0), pk_mul(c.y, s1)};
         if ((x & 1) == 0) half = v;
-        else if (stager) *(u32x4*)(vst + (i & (RING - 1)) * SB + (x >> 1) * 256) = u32x4{half.x, half.y, v.x, v.y};
+        else *(u32x4*)(vst + (i & (RING - 1)) * SB + (x >> 1) * 256) = u32x4{half.x, half.y, v.x, v.y};
     };
     // Scales of positions past the sequence may be anything: zero in the block where it ends.
     // int8: values are finite if their scales are.
@@ -686,13 +692,10 @@ __global__ void __launch_bounds__(256) attn_tile_join_kernel(AttnChunkArgs a) {
 hipError_t launch_attn_tile(const AttnChunkArgs& a, unsigned grid, unsigned split_tiles, hipStream_t st) {
     const bool i8 = a.kv.format == FP_KV_INT8;
     const int D = a.kv.head_dim;
-    if (D == 128) {
-        if (i8) FP_LAUNCH((attn_tile_kernel<128, true>), dim3(grid), dim3(256), 0, st, a);
-        else FP_LAUNCH((attn_tile_kernel<128, false>), dim3(grid), dim3(256), 0, st, a);
-    } else {
-        if (i8) FP_LAUNCH((attn_tile_kernel<64, true>), dim3(grid), dim3(256), 0, st, a);
-        else FP_LAUNCH((attn_tile_kernel<64, false>), dim3(grid), dim3(256), 0, st, a);
-    }
+    if (D == 64 && i8) return hipErrorInvalidValue;
+    if (D == 64) FP_LAUNCH((attn_tile_kernel<64, false>), dim3(grid), dim3(256), 0, st, a);
+    else if (i8) FP_LAUNCH((attn_tile_kernel<128, true>), dim3(grid), dim3(256), 0, st, a);
+    else FP_LAUNCH((attn_tile_kernel<128, false>), dim3(grid), dim3(256), 0, st, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || split_tiles == 0) return e;
     if (D == 128) FP_LAUNCH(attn_tile_join_kernel<128>, dim3(split_tiles, D / 4), dim3(256), 0, st, a);

@@ -36,8 +36,13 @@ def _fill(pool, table, lens, g, upto=lambda c, n: c, scale=1.0):
                        torch.randn(m, pool.nkv, pool.d, generator=g).bfloat16().float())
 
 
-def _chunk(lens, table, extra_rows=0, max_len=None, max_new=None):
+def _chunk(lens, table, extra_rows=0, max_len=None, max_new=None, loose=0):
+    """loose: a bound on the positions far beyond the sequences' (pages of this size), which large calls have:
+    more than 64 rows to a kv head then take the kernel of 256-row tiles."""
     fp = _fp()
+    if loose:
+        max_len = 1 << 22
+        table = torch.nn.functional.pad(table, (0, max_len // loose + 1 - table.shape[1]), value=-7)
     starts = [0]
     for _, n in lens:
         starts.append(starts[-1] + n)
@@ -169,16 +174,17 @@ ATTN_SEQS = dict(SEQS, **{
 })
 
 
+@pytest.mark.parametrize("loose", [False, True])
 @pytest.mark.parametrize("kvq", ["bf16", "int8"])
 @pytest.mark.parametrize("nkv,G,d,page", SHAPES)
 @pytest.mark.parametrize("seqs", sorted(ATTN_SEQS))
-def test_attention_matches_the_reference(seqs, nkv, G, d, page, kvq):
+def test_attention_matches_the_reference(seqs, nkv, G, d, page, kvq, loose):
     fp = _fp()
     lens = ATTN_SEQS[seqs]
     g, pool, table = _case(lens, page, nkv, d, kvq, 21)
     _fill(pool, table, lens, g, upto=lambda c, n: c + n, scale=1.5)
     kv = pool.device()
-    chunk, starts = _chunk(lens, table)
+    chunk, starts = _chunk(lens, table, loose=page * loose)
     N = starts[-1]
     q = torch.randn(N + 2, nkv * G, d, generator=g).bfloat16()
     out = torch.full((N + 2, nkv * G, d), 7.0, dtype=torch.bfloat16).cuda()
@@ -226,6 +232,7 @@ def _fill_gpu(lens, page, nkv, d, kvq, seed, spare=2):
     return kv, table, g
 
 
+@pytest.mark.parametrize("loose", [False, True])
 @pytest.mark.parametrize("nkv,G,d,page,kvq,lens", [
     (4, 16, 128, 64, "bf16", [(8000, 130)]),          # pieces of more than 64 blocks, many tiles
     (4, 16, 128, 64, "int8", [(8000, 130)]),
@@ -239,10 +246,10 @@ def _fill_gpu(lens, page, nkv, d, kvq, seed, spare=2):
     (1, 16, 128, 32, "bf16", [(6000, 1)] * 70 + [(100, 40)]),
     (3, 1, 64, 32, "int8", [(9000, 16), (9000, 17), (50, 70)]),
 ])
-def test_long_attention(nkv, G, d, page, kvq, lens):
+def test_long_attention(nkv, G, d, page, kvq, lens, loose):
     fp = _fp()
     kv, table, g = _fill_gpu(lens, page, nkv, d, kvq, 31)
-    chunk, starts = _chunk(lens, table)
+    chunk, starts = _chunk(lens, table, loose=page * loose)
     q = torch.randn(starts[-1], nkv * G, d, generator=g, device="cuda").bfloat16()
     out = torch.empty_like(q)
     fp.attn_chunk(kv, chunk, q, out)
@@ -252,8 +259,8 @@ def test_long_attention(nkv, G, d, page, kvq, lens):
 
 
 @pytest.mark.parametrize("kvq", ["bf16", "int8"])
-@pytest.mark.parametrize("nkv,G,new", [(2, 2, 1), (1, 8, 5), (2, 4, 90)])
-def test_scores_far_apart_and_rising(nkv, G, new, kvq):
+@pytest.mark.parametrize("nkv,G,new,loose", [(2, 2, 1, 0), (1, 8, 5, 0), (2, 4, 90, 0), (2, 4, 90, 64)])
+def test_scores_far_apart_and_rising(nkv, G, new, loose, kvq):
     """Keys whose scores grow along the sequence (the softmax's reference moves again and again), tiny and
     large values beside each other, a negative scale, q at the top of bf16's useful range."""
     fp = _fp()
@@ -265,7 +272,7 @@ def test_scores_far_apart_and_rising(nkv, G, new, kvq):
             ramp = torch.linspace(0.1, 6, m)[:, None, None]
             pool.write(table[b], torch.arange(m), (ramp * (1 + 0.2 * torch.randn(m, nkv, d, generator=g))).bfloat16().float(),
                        (torch.randn(m, nkv, d, generator=g) * (10.0 ** (torch.arange(m) % 5 - 3))[:, None, None]).bfloat16().float())
-        chunk, starts = _chunk(lens, table)
+        chunk, starts = _chunk(lens, table, loose=loose)
         q = (qs * (0.3 + torch.randn(starts[-1], nkv * G, d, generator=g))).bfloat16()
         out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
         fp.attn_chunk(pool.device(), chunk, q.cuda(), out, scale=scale)
@@ -280,16 +287,16 @@ def test_scores_far_apart_and_rising(nkv, G, new, kvq):
 
 
 @pytest.mark.parametrize("kvq", ["bf16", "int8"])
-@pytest.mark.parametrize("new,G", [(1, 4), (20, 4), (100, 4)])
-def test_missing_pages_read_as_zeros_and_take_no_writes(kvq, new, G):
+@pytest.mark.parametrize("new,G,d,loose", [(1, 4, 64, 0), (20, 4, 64, 0), (100, 4, 64, 0), (100, 4, 64, 32), (100, 4, 128, 32)])
+def test_missing_pages_read_as_zeros_and_take_no_writes(kvq, new, G, d, loose):
     fp = _fp()
-    nkv, d, page, lens = 2, 64, 32, [(200, new), (70, new)]
+    nkv, page, lens = 2, 32, [(200, new), (70, new)]
     g, pool, table = _case(lens, page, nkv, d, kvq, 51)
     _fill(pool, table, lens, g, upto=lambda c, n: c + n)
     for b, i, bad in ((0, 2, -5), (0, 6, 2**31 - 1), (1, 0, pool.n_pages)):
         table[b, i] = bad
     kv = pool.device()
-    chunk, starts = _chunk(lens, table)
+    chunk, starts = _chunk(lens, table, loose=loose)
     N = starts[-1]
     before = [t.clone() for t in ([kv.k, kv.v] + ([kv.k_scales, kv.v_scales] if kvq == "int8" else []))]
     q = torch.randn(N, nkv * G, d, generator=g).bfloat16()
@@ -464,6 +471,7 @@ def test_strided_rows_and_single_rows():
         fp.attn_chunk(kv, chunk, out, out)                              # q and out overlap
 
 
+@pytest.mark.parametrize("loose", [0, 64])
 @pytest.mark.parametrize("kvq", ["bf16", "int8"])
 @pytest.mark.parametrize("nkv,G,d,lens", [
     (2, 3, 64, [(40, 5), (200, 1), (31, 2), (0, 4)]),
@@ -473,7 +481,7 @@ def test_strided_rows_and_single_rows():
     (1, 1, 128, [(40, 300), (5, 2), (0, 520)]),
     (1, 16, 128, [(4000, 33)]),
 ])
-def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(nkv, G, d, lens, kvq):
+def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(nkv, G, d, lens, kvq, loose):
     fp = _fp()
     page = 64
     g, pool, table = _case(lens, page, nkv, d, kvq, 101)
@@ -497,7 +505,7 @@ def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(nkv, G, d,
             poison(b, c + n // 2 + (n > 3), d - 1, -math.inf)
             poison(b, c + n - 1, 20, math.inf)
             poison(b, c + n - 1, 5, math.nan, key=True)
-    chunk, starts = _chunk(lens, table)
+    chunk, starts = _chunk(lens, table, loose=loose)
     q = torch.randn(starts[-1], nkv * G, d, generator=g).bfloat16()
     out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
     fp.attn_chunk(pool.device(), chunk, q.cuda(), out)
