@@ -7,6 +7,8 @@
 
 namespace fpk {
 
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
 constexpr int TILE_ROWS = 256;             // rows per tile of attn_tile.hip
 constexpr float M0 = -3e38f;               // softmax reference before any score
 
