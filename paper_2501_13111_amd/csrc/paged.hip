@@ -21,6 +21,14 @@ __device__ __forceinline__ int seq_blocks(const Seq& s) {
     return s.n > 0 ? (s.len - 1) / VT_BLK - s.ctx / VT_BLK + 1 : 0;
 }
 
+// The workgroup's block and kv head.  Workgroup i runs on XCD i % 8: the heads of a block follow each other on one,
+// whose L2 fetches the block's angles once.
+__device__ __forceinline__ void unit(int nkv, int& u, int& kvh) {
+    const int k = blockIdx.x >> 3;
+    u = k / nkv * 8 + (blockIdx.x & 7);
+    kvh = k % nkv;
+}
+
 __device__ __forceinline__ void unpack8(u32x4 v, float (&x)[8]) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -85,8 +93,8 @@ __global__ void __launch_bounds__(T) kv_append_paged_kernel(KvAppendArgs a) {
     constexpr int VS = VT_BLK * ES + 16;                   // LDS bytes per value dim
     __shared__ __attribute__((aligned(16))) char vt[D * VS];
     const int tid = threadIdx.x;
-    const int kvh = blockIdx.x % a.kv.n_kv_heads;
-    int u = blockIdx.x / a.kv.n_kv_heads;
+    int u, kvh;
+    unit(a.kv.n_kv_heads, u, kvh);
     const int b = find_seq(a.chunk.n_seqs, u, [&](int i) { return seq_blocks(load_seq(a.chunk, i)); });
     if (b < 0) return;
     const Seq sq = load_seq(a.chunk, b);
@@ -176,8 +184,8 @@ __global__ void __launch_bounds__(T) kv_read_paged_kernel(KvReadArgs a) {
     constexpr int VS = VT_BLK * ES + 16;
     __shared__ __attribute__((aligned(16))) char vt[D * VS];
     const int tid = threadIdx.x;
-    const int kvh = blockIdx.x % a.kv.n_kv_heads;
-    int u = blockIdx.x / a.kv.n_kv_heads;
+    int u, kvh;
+    unit(a.kv.n_kv_heads, u, kvh);
     const int b = find_seq(a.chunk.n_seqs, u, [&](int i) { return seq_blocks(load_seq(a.chunk, i)); });
     if (b < 0) return;
     const Seq sq = load_seq(a.chunk, b);
@@ -192,32 +200,51 @@ __global__ void __launch_bounds__(T) kv_read_paged_kernel(KvReadArgs a) {
         for (int it = tid; it < D * PD; it += T) *(u32x4*)(vt + it / PD * VS + it % PD * 16) = src[it];
     }
     __syncthreads();
-    for (int it = tid; it < 2 * np * NP; it += T) {
-        const int i = it % (np * NP) / NP, j = 8 * (it % NP), t = t0 + i;
-        const bool val = it >= np * NP;
-        uint16_t* dst = (val ? a.v_out : a.k_out) + ((row0 + i) * a.kv.n_kv_heads + kvh) * D + j;
-        float x[8];
+    auto store = [&](uint16_t* out, int i, int j, const float (&x)[8]) {
+        *(u32x4*)(out + ((row0 + i) * a.kv.n_kv_heads + kvh) * D + j) = pack8(x);
+    };
+    if (tid < T / 2) {
+        // values: four positions, whose slots are neighbours, of eight dims at a time
+        for (int it = tid; it < VT_BLK / 4 * NP; it += T / 2) {
+            const int t = it / NP * 4, j = 8 * (it % NP);
+            if (t + 4 <= t0 || t >= t1) continue;
+            constexpr int W = ES;                          // words of four values
+            uint32_t c[8][W];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        if (pb >= 0) {
-            const int slot = vt_slot(t);
-            if constexpr (KV8) {
-                const float s = h2f((val ? a.kv.v_scales : a.kv.k_scales)[prow + t]);
-                const u32x2 c = *(const u32x2*)((const int8_t*)a.kv.k + (prow + t) * D + j);
+            for (int e = 0; e < 8; ++e)
+#pragma unroll
+                for (int w = 0; w < W; ++w) c[e][w] = pb >= 0 ? *(const uint32_t*)(vt + (j + e) * VS + ES * vt_slot(t) + 4 * w) : 0u;
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                if (t + p < t0 || t + p >= t1) continue;
+                float x[8];
+                const float s = KV8 && pb >= 0 ? h2f(a.kv.v_scales[prow + t + p]) : 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int8_t q = val ? *(const int8_t*)(vt + (j + e) * VS + slot)
-                                         : (int8_t)((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
-                    x[e] = (float)q * s;
+                    if constexpr (KV8) x[e] = (float)(int8_t)(c[e][0] >> (8 * p)) * s;
+                    else x[e] = __uint_as_float(p & 1 ? c[e][p >> 1] & 0xFFFF0000u : c[e][p >> 1] << 16);
                 }
-            } else if (val) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = (float)*(const __bf16*)(vt + (j + e) * VS + 2 * slot);
-            } else {
-                unpack8(*(const u32x4*)((const uint16_t*)a.kv.k + (prow + t) * D + j), x);
+                store(a.v_out, t + p - t0, j, x);
             }
         }
-        *(u32x4*)dst = pack8(x);
+    } else {
+        for (int it = tid - T / 2; it < np * NP; it += T / 2) {
+            const int i = it / NP, j = 8 * (it % NP);
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = 0.f;
+            if (pb >= 0) {
+                if constexpr (KV8) {
+                    const float s = h2f(a.kv.k_scales[prow + t0 + i]);
+                    const u32x2 c = *(const u32x2*)((const int8_t*)a.kv.k + (prow + t0 + i) * D + j);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = (float)(int8_t)((e < 4 ? c.x : c.y) >> (8 * (e & 3))) * s;
+                } else {
+                    unpack8(*(const u32x4*)((const uint16_t*)a.kv.k + (prow + t0 + i) * D + j), x);
+                }
+            }
+            store(a.k_out, i, j, x);
+        }
     }
 }
 
@@ -230,7 +257,7 @@ int64_t max_blocks(const fp_chunk& c) {
 }  // namespace
 
 hipError_t launch_kv_append(const KvAppendArgs& a, bool f32, hipStream_t st) {
-    const int64_t n = max_blocks(a.chunk) * a.kv.n_kv_heads;
+    const int64_t n = (max_blocks(a.chunk) + 7) / 8 * 8 * a.kv.n_kv_heads;
     if (n < 1 || n > INT_MAX) return hipErrorInvalidValue;
     const bool i8 = a.kv.format == FP_KV_INT8;
 #define FP_AP(D, I8, F32) FP_LAUNCH((kv_append_paged_kernel<D, I8, F32>), dim3((unsigned)n), dim3(T), 0, st, a)
@@ -248,7 +275,7 @@ hipError_t launch_kv_append(const KvAppendArgs& a, bool f32, hipStream_t st) {
 }
 
 hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st) {
-    const int64_t n = max_blocks(a.chunk) * a.kv.n_kv_heads;
+    const int64_t n = (max_blocks(a.chunk) + 7) / 8 * 8 * a.kv.n_kv_heads;
     if (n < 1 || n > INT_MAX) return hipErrorInvalidValue;
     const dim3 grid((unsigned)n);
     const bool i8 = a.kv.format == FP_KV_INT8;
