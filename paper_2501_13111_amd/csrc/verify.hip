@@ -92,6 +92,12 @@ __device__ __forceinline__ double weight(float z, float m, double c, const doubl
     return z == m ? 1.0 : !(z > -INFINITY) || m == INFINITY ? 0.0 : e;
 }
 
+// The same for z that is no NaN and m < +inf, without the rules: -inf gives 2^-1200, zero, and m itself one.
+__device__ __forceinline__ double weight_below(float z, double m, double c, const double* tab) {
+    return exp2_d(((double)z - m) * c, tab);
+}
+__device__ __forceinline__ float no_nan(float z) { return fmaxf(z, -INFINITY); }
+
 // the larger value, the lower id among equal ones
 __device__ __forceinline__ void best_of(float& v, int& i, float ov, int oi) {
     if (ov > v || (ov == v && oi < i)) {
@@ -143,8 +149,16 @@ __global__ void __launch_bounds__(NT) row_kernel(VerifyArgs a) {
     for (int j = 1; j < NT / 64; ++j) best_of(m, mi, sm[j], si[j]);
     double s = 0.0;
     if (a.c > 0.0 && m > -INFINITY) {
+        if (m < INFINITY) {
+            const double md = m;
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) s += weight(x[i], m, a.c, tab);
+            for (int i = 0; i < EPT; ++i) s += weight_below(no_nan(x[i]), md, a.c, tab);
+        } else {
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < EPT; ++i) n += x[i] == m ? 1 : 0;
+            s = n;
+        }
         s = wave_sum_d(s);
         if (lane == 0) sd[w] = s;
         __syncthreads();
@@ -228,7 +242,7 @@ __device__ __forceinline__ void draw_weights(const VerifyArgs& a, const Decision
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const double p = weight(zz[i], d.m, a.c, tab) * inv;
+        const double p = (d.m < INFINITY ? weight_below(no_nan(zz[i]), d.m, a.c, tab) : zz[i] == d.m ? 1.0 : 0.0) * inv;
         wt[i] = v + i == x ? 0.0 : fmax(p - draft_p(qq[i]), 0.0);
     }
 }
