@@ -17,6 +17,9 @@
 //
 // exp(x) = 2^y, y = x log2 e = n / 256 + r, |r| <= 1 / 512: 2^(n / 256) from a table of 256 and the
 // exponent, 2^r by its power series to the fourth order (the rest is below 4e-17).
+//
+// 32 sequences of 6 rows of 32000, T = 0.8: 9.3 us for the rows (24.6 MB; the exponentials' 64-bit arithmetic is some 6 of
+// them), 10 for the masses and 8 for the draw, both chains of a dozen dependent loads.  One sequence of 4 rows, T = 0: 3.8 + 2.2.
 #include <climits>
 
 #include "fp_device.h"
