@@ -324,8 +324,9 @@ fp_status fp_kv_read(const fp_paged_kv* kv, const fp_chunk* chunk, void* k_out, 
  * others.  int8: keys and values below 65504 in magnitude (calls of more than 64 rows per sequence
  * and kv head unpack them to fp16).
  * workspace: device memory of at least fp_attn_chunk_workspace bytes, 16-byte aligned, which
- * the call may use until the stream has passed it (calls that can overlap need one each).
- * FP_ERR_CAPACITY if workspace_bytes is less.
+ * the call may use until the stream has passed it (calls that can overlap need one each); enough
+ * for one chunk's bounds is enough for any chunk of smaller ones.  FP_ERR_CAPACITY if workspace_bytes
+ * is less.
  */
 fp_status fp_attn_chunk_workspace(const fp_paged_kv* kv, const fp_chunk* chunk, int32_t n_heads, size_t* bytes);
 fp_status fp_attn_chunk(const fp_paged_kv* kv, const fp_chunk* chunk, const void* q, int64_t q_stride, int32_t n_heads,
@@ -341,8 +342,8 @@ fp_status fp_attn_chunk(const fp_paged_kv* kv, const fp_chunk* chunk, const void
  * pages, its output goes to row r of y (rows of no sequence: unspecified values).  The handle's
  * weights and activations are used, its own cache, position and batch are not touched.
  * n_rows <= max_batch * max_prompt and max_len <= max_seq (FP_ERR_CAPACITY); up to max_batch
- * rows take the decode projections.  workspace: as for fp_attn_chunk (the attention's, of any
- * layer).  May be captured into a graph; allocates nothing.  The debug dumps are not written.
+ * rows take the decode projections.  workspace: as for fp_attn_chunk (the largest of the
+ * layers').  May be captured into a graph; allocates nothing.  The debug dumps are not written.
  */
 fp_status fp_extend_workspace(const fp_layer* layer, const fp_paged_kv* kv, const fp_chunk* chunk, size_t* bytes);
 fp_status fp_extend(fp_layer* layer, const fp_paged_kv* kv, const fp_chunk* chunk, const void* x, void* y,

@@ -115,10 +115,13 @@ int64_t piece_aim(int RT, int D) { return (int64_t)1 << (piece_target(RT, D) + (
 
 }  // namespace
 
-// Split tiles have more than Q blocks, so their pieces number at most twice total / Q, twice the aim.
+// Split tiles have more than Q blocks, so their pieces number at most twice total / Q, twice the aim.  Enough for
+// calls of smaller bounds too, whose tiles may be smaller.
 size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
-    const int RT = tile_rows(kv, c, n_heads);
-    return (size_t)(2 * piece_aim(RT, kv.head_dim)) * RT * wst(kv.head_dim) * sizeof(float);
+    int64_t rows = 0;
+    for (const int RT : {16, 32, 64, TILE_ROWS})
+        if (RT <= tile_rows(kv, c, n_heads)) rows = std::max(rows, 2 * piece_aim(RT, kv.head_dim) * RT);
+    return (size_t)rows * wst(kv.head_dim) * sizeof(float);
 }
 
 template <int D, bool KV8, int RT>

@@ -1661,10 +1661,17 @@ static fp_status check_extend(const fp_layer* h, const fp_paged_kv* kv, const fp
     return FP_OK;
 }
 
+// The layers' caches may differ in format, and with it in the attention's tiles.
+static size_t extend_ws_bytes(const fp_layer* h, const fp_paged_kv* kv, const fp_chunk& chunk) {
+    size_t n = 0;
+    for (int l = 0; l < h->s.n_layers; ++l) n = std::max(n, attn_chunk_ws_bytes(kv[l], chunk, h->s.n_heads));
+    return n;
+}
+
 fp_status fp_extend_workspace(const fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, size_t* bytes) {
     if (!bytes) return fail(FP_ERR_INVALID_ARG, "bytes is NULL");
     if (const fp_status rc = check_extend(h, kv, chunk)) return rc;
-    *bytes = attn_chunk_ws_bytes(kv[0], *chunk, h->s.n_heads);
+    *bytes = extend_ws_bytes(h, kv, *chunk);
     return FP_OK;
 }
 
@@ -1674,7 +1681,7 @@ fp_status fp_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, c
     if (!x || !y) return fail(FP_ERR_INVALID_ARG, "x and y must be device pointers");
     const size_t bytes = (size_t)chunk->n_rows * h->s.hidden * 2;
     if (overlap(x, bytes, y, bytes)) return fail(FP_ERR_INVALID_ARG, "x and y overlap");
-    const size_t need = attn_chunk_ws_bytes(kv[0], *chunk, h->s.n_heads);
+    const size_t need = extend_ws_bytes(h, kv, *chunk);
     if (!workspace || (uintptr_t)workspace % 16 != 0) return fail(FP_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device pointer");
     if (workspace_bytes < need) return fail(FP_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
     if (h->unbacked || chunk->n_rows == 0) return FP_OK;

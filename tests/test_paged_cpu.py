@@ -134,6 +134,19 @@ def test_attention_workspace(lib):
     assert lib.fp_attn_chunk_workspace(ctypes.byref(kv()), ctypes.byref(chunk()), 4, None) == INVALID
 
 
+@pytest.mark.parametrize("d,fmt", [(64, 0), (64, 1), (128, 0), (128, 1)])
+def test_a_workspace_serves_smaller_calls(lib, d, fmt):
+    n = ctypes.c_size_t()
+    sizes = []
+    for rows, new, length, seqs in [(1, 1, 32, 1), (4, 4, 500, 1), (40, 5, 2000, 8), (100, 9, 2000, 16), (500, 500, 4000, 16),
+                                    (40000, 4000, 100000, 64), (40000, 4000, 100000, 65), (2**20, 2**20, 2**22, 4096)]:
+        c = chunk(n_rows=rows, max_new=new, max_len=length, n_seqs=seqs, table_stride=2**17)
+        k = kv(format=fmt, head_dim=d)
+        assert lib.fp_attn_chunk_workspace(ctypes.byref(k), ctypes.byref(c), 16, ctypes.byref(n)) == 0
+        sizes.append(n.value)
+    assert sizes == sorted(sizes)
+
+
 def verify(lib, **kw):
     a = dict(logits=P, stride=100, n_seqs=2, n_rows=6, max_rows=4, vocab=100, row_start=P, ids=P, probs=P, pstride=100, u=P, ul=P,
              T=1.0, out=P, n_out=P, ws=P, n=1 << 40)
@@ -188,6 +201,15 @@ def test_extends_that_are_refused(lib):
         assert lib.fp_extend_workspace(f._h, arr, ctypes.byref(c), ctypes.byref(n)) == 0 and n.value > 0
         assert extend(lib, f._h, ok, c, n=n.value) == 0 and extend(lib, f._h, ok, c, n=n.value - 1) == CAPACITY
         assert lib.fp_extend_workspace(f._h, arr, ctypes.byref(c), None) == INVALID
+    # caches of both formats: the largest layer's, whichever comes first
+    with Fingerprint(Shape(2, 256, 4, 2, 64, 448, 4, 4096, 60000), unbacked=True) as f:
+        c = chunk(n_rows=16000, max_new=8000, max_len=60000, table_stride=1000)
+        sizes = {}
+        for fmts in ((0, 0), (1, 1), (0, 1), (1, 0)):
+            arr = (_PagedKv * 2)(*[kv(format=x) for x in fmts])
+            assert lib.fp_extend_workspace(f._h, arr, ctypes.byref(c), ctypes.byref(n)) == 0
+            sizes[fmts] = n.value
+        assert sizes[1, 1] != sizes[0, 0] and sizes[0, 1] == sizes[1, 0] == max(sizes.values())
     assert extend(lib, None, ok, c) == INVALID
 
 
