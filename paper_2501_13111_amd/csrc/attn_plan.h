@@ -16,6 +16,17 @@ constexpr float M0 = -3e38f;               // softmax reference before any score
 // are streamed like those of a call without larger ones.
 __device__ __forceinline__ bool few_rows(const Seq& s, int G) { return s.n * G <= 16; }
 
+// Scores are scaled as |scale| (q with its signs turned for a negative scale).  A scale of zero, or too small to
+// matter, would make NaN of a masked score's -infinity: the queries are zero then, and the scale one.
+struct QScale {
+    float sl2;                             // |scale| log2 e
+    uint32_t sign, keep;                   // of two bf16 or fp16 queries: (q ^ sign) & keep
+};
+__device__ __forceinline__ QScale q_scale(float scale) {
+    const bool none = fabsf(scale) < 1.2e-38f;
+    return QScale{none ? 1.f : fabsf(scale) * 1.4426950408889634f, scale < 0.f ? 0x80008000u : 0u, none ? 0u : 0xFFFFFFFFu};
+}
+
 struct Plan {
     int tiles, blocks, pieces;             // row tiles, 32-key blocks, pieces per tile
 };

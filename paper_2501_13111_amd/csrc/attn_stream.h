@@ -120,7 +120,7 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
     // what they hold does not matter.
     u32x4 qf[NT][NJ];
     int lim[NT];                                 // last position that the lane's row sees
-    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;      // a negative scale turns the queries' signs
+    const QScale qs = q_scale(a.scale);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int rho = row0 + 16 * t + r;
@@ -129,7 +129,7 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
         lim[t] = live ? sq.ctx + tok : -1;
         const uint16_t* q = a.q + (int64_t)(sq.row0 + tok) * a.q_stride + (kvh * G + h) * D;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) qf[t][j] = *(const u32x4*)(q + qdim<KV8>(j, g)) ^ sign;
+        for (int j = 0; j < NJ; ++j) qf[t][j] = (*(const u32x4*)(q + qdim<KV8>(j, g)) ^ qs.sign) & qs.keep;
     }
 
     f32x4 oacc[NT][ND];
@@ -141,7 +141,7 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
 #pragma unroll
         for (int dd = 0; dd < ND; ++dd) oacc[t][dd] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const float sl2 = fabsf(a.scale) * 1.4426950408889634f;
+    const float sl2 = qs.sl2;
 
     bool strays = false;
     // Block i from c, which is refilled with block `next`, keys and values as soon as they are used.  (A second

@@ -249,15 +249,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     u32x4 qf[2][NKC];
     int lim[2];                            // last position that the lane's row sees
     float sl2[2];                          // scores to base 2
+    const QScale qs = q_scale(a.scale);
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         const int rho = wr0 + 32 * c + l32;
         const bool live = 32 * c + l32 < wrows;
         const int tok = live ? rho / G : 0, h = live ? rho % G : 0;
         lim[c] = live ? sq.ctx + tok : -1;
-        sl2[c] = fabsf(a.scale) * 1.4426950408889634f;
+        sl2[c] = qs.sl2;
         const uint16_t* q = a.q + (int64_t)(sq.row0 + tok) * a.q_stride + (kvh * G + h) * D;
-        const uint32_t keep = live ? 0xFFFFFFFFu : 0u, sign = a.scale < 0.f ? 0x80008000u : 0u;
+        const uint32_t keep = live ? qs.keep : 0u, sign = qs.sign;
 #pragma unroll
         for (int j = 0; j < NKC; ++j) qf[c][j] = *(const u32x4*)(q + 16 * j + 8 * h32);
         if constexpr (KV8) {

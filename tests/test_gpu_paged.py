@@ -519,3 +519,18 @@ def test_values_that_are_not_finite_reach_only_the_rows_that_see_them(nkv, G, d,
     ds = 2 * (d + 4) * EPS32 * smag + (2 * 2.0 ** -11 * smag if kvq == "int8" else 0.0)
     tol = HALF_BF16 * want.abs() + (HALF_BF16 + 2 * ds + 1e-5 + 2.0 ** -11) * mag * (1 + HALF_BF16)
     assert ((got - want).abs() <= tol)[~odd].all()
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("nkv,G,d,new,loose", [(2, 2, 64, 1, 0), (1, 8, 128, 4, 0), (2, 8, 64, 6, 0), (2, 4, 128, 50, 64), (2, 4, 64, 50, 64)])
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-42, 1e-30])
+def test_a_scale_of_nothing_averages(nkv, G, d, new, loose, scale, kvq):
+    fp = _fp()
+    lens = [(75, new), (0, new), (2100, new)]
+    g, pool, table = _case(lens, 64, nkv, d, kvq, 111)
+    _fill(pool, table, lens, g, upto=lambda c, n: c + n)
+    chunk, starts = _chunk(lens, table, loose=loose)
+    q = torch.randn(starts[-1], nkv * G, d, generator=g).bfloat16()
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    fp.attn_chunk(pool.device(), chunk, q.cuda(), out, scale=scale)
+    _check_attention(pool, table, lens, q, out, scale, fp16=kvq == "int8")
