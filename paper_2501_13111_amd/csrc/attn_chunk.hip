@@ -15,8 +15,8 @@
 // Many rows to a kv head take tiles of 256 (attn_tile.hip; tile_rows below has the rule): there the matrix cores
 // bound, here the reads of the cache.
 //
-// Work is split over the keys: from the lengths in device memory every workgroup works out the same plan
-// (attn_plan.h).  A piece is (sequence, kv head, row tile, a run of 32-key blocks); its four waves take every
+// Work is split over the keys: from the lengths in device memory every workgroup works out the same plan, or for more than
+// 256 sequences a kernel before it (attn_plan.h).  A piece is (sequence, kv head, row tile, a run of 32-key blocks); its four waves take every
 // fourth block and merge in LDS.  A tile of one piece is written out at once; the pieces of the others
 // go to the workspace as unnormalised (o, m, l) and a second kernel joins them in order:
 //     m = max m_i,  l = sum l_i 2^(m_i - m),  o = sum o_i 2^(m_i - m) / l.
@@ -40,6 +40,88 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : NT == 4 && D == 128 ? 1 : 2
     Unit un;
     if (!find_unit<16 * NT, false, false>(a, a.n_heads / a.kv.n_kv_heads, un)) return;
     stream_unit<D, KV8, NT, false>(a, un, lds);
+}
+
+// The plan of more than 256 sequences (attn_plan.h), by one workgroup: PER sequences a thread, their sums and running
+// counts over the waves.  Next tokens of 1024 sequences of up to 200, 8 heads of 128, bf16: 142 us with it, of which it takes
+// 5; 306 with every workgroup planning for itself.  4096 sequences: 497, 2988.
+constexpr int PLAN_T = 1024, PER = 4096 / PLAN_T;
+template <int RT>
+__global__ void __launch_bounds__(PLAN_T) attn_plan_kernel(AttnChunkArgs a) {
+    constexpr int W = PLAN_T / 64;
+    __shared__ int64_t st[W];
+    __shared__ int sn[W], sc[4][W];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
+    Seq sq[PER];
+    int64_t total = 0;
+    int tiles = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int b = tid * PER + i;
+        sq[i] = b < a.chunk.n_seqs ? load_seq(a.chunk, b) : Seq{0, 0, 0, 0};
+        const Plan p = plan_seq<RT>(sq[i], G, 1);
+        total += (int64_t)p.tiles * p.blocks;
+        tiles = std::min(tiles + long_tiles<RT>(sq[i], G, p), 1 << 20);
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        total += __shfl_xor(total, o, 64);
+        tiles = std::min(tiles + __shfl_xor(tiles, o, 64), 1 << 24);
+    }
+    if (lane == 0) {
+        st[w] = total;
+        sn[w] = tiles;
+    }
+    __syncthreads();
+    total = 0;
+    tiles = 0;
+    for (int j = 0; j < W; ++j) {
+        total += st[j];
+        tiles += sn[j];
+    }
+    const int Q = plan_all<RT>(a, total, tiles);
+    int mine[4] = {0, 0, 0, 0}, base[4];
+    PlanRow row[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        row[i] = plan_row<RT, RT == TILE_ROWS>(sq[i], G, nkv, Q);
+        mine[0] += row[i].units;
+        mine[1] += row[i].few;
+        mine[2] += row[i].split;
+        mine[3] += row[i].part;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        base[k] = wave_scan(mine[k]);
+        if (lane == 63) sc[k][w] = base[k];
+        base[k] -= mine[k];
+    }
+    __syncthreads();
+    int all[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        all[k] = 0;
+        for (int j = 0; j < W; ++j) {
+            base[k] += j < w ? sc[k][j] : 0;
+            all[k] += sc[k][j];
+        }
+    }
+    PlanRow* rows = (PlanRow*)(a.plan + PLAN_HEAD);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int b = tid * PER + i;
+        if (b < a.chunk.n_seqs) rows[b] = PlanRow{base[0], base[1], base[2], base[3]};
+        base[0] += row[i].units;
+        base[1] += row[i].few;
+        base[2] += row[i].split;
+        base[3] += row[i].part;
+    }
+    if (tid == 0) {
+        a.plan[PLAN_Q] = Q;
+        a.plan[PLAN_UNITS] = all[0];
+        a.plan[PLAN_FEW] = all[1];
+        a.plan[PLAN_SPLIT] = all[2];
+    }
 }
 
 // Joins the pieces of split tiles: RPW rows of a tile per workgroup, a thread per four dims of a row.
@@ -121,7 +203,7 @@ size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads
     int64_t rows = 0;
     for (const int RT : {16, 32, 64, TILE_ROWS})
         if (RT <= tile_rows(kv, c, n_heads)) rows = std::max(rows, 2 * piece_aim(RT, kv.head_dim) * RT);
-    return (size_t)rows * wst(kv.head_dim) * sizeof(float);
+    return (size_t)rows * wst(kv.head_dim) * sizeof(float) + (size_t)plan_ints(c.n_seqs) * sizeof(int);
 }
 
 template <int D, bool KV8, int RT>
@@ -132,10 +214,16 @@ static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     a.min_blocks = piece_min(RT);
     a.over = 10;
     a.join = 8;
+    a.plan = (int*)(a.ws + 2 * piece_aim(RT, D) * RT * wst(D));
     const int64_t pieces = piece_aim(RT, D), n = std::max(tiles + pieces, 2 * pieces) + 16 * XCD_RUN;
     if (n > INT_MAX) return hipErrorInvalidValue;
     // tiles that can be split: each has more than Q of the blocks
     const unsigned split = (a.chunk.max_len - 1) / VT_BLK < a.min_blocks ? 0u : (unsigned)std::min<int64_t>(tiles, pieces);
+    if (a.chunk.n_seqs > PLAN_LANES) {
+        FP_LAUNCH(attn_plan_kernel<RT>, dim3(1), dim3(PLAN_T), 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     if constexpr (RT == TILE_ROWS) {
         return launch_attn_tile(a, (unsigned)n, split, st);
     } else {

@@ -1,5 +1,4 @@
-// Work plan of the chunk attention, made by every workgroup from the lengths in device memory, and what
-// its kernels share.
+// Work plan of the chunk attention, made on the device from the lengths there, and what its kernels share.
 #pragma once
 #include <algorithm>
 
@@ -39,18 +38,6 @@ __device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int Q) {
     return p;
 }
 
-// The chunk's sequences across a wave's lanes, 64 at a time: f(b, sequence) for lane's b of each
-// round.  The first 64 are loaded once and kept.
-struct Lanes {
-    const fp_chunk& c;
-    Seq s0;
-    __device__ __forceinline__ explicit Lanes(const fp_chunk& ch) : c(ch) { s0 = at(0); }
-    __device__ __forceinline__ Seq at(int b0) const {
-        const int b = b0 + (int)(threadIdx.x & 63);
-        return b < c.n_seqs ? load_seq(c, b) : Seq{0, 0, 0, 0};
-    }
-    __device__ __forceinline__ Seq get(int b0) const { return b0 == 0 ? s0 : at(b0); }
-};
 // Blocks per piece, Q: the total over the pieces to aim for, and at least a.min_blocks.  2^a.target workgroups or so
 // run at a time.
 // One sequence's pieces are all alike.  Of 64 rows and more, a last round of a few pieces would cost as much
@@ -61,42 +48,54 @@ struct Lanes {
 // a tile, which rounding up adds, so that one round holds them.  Tiles of few rows that fill the round by themselves are
 // cut for two.  (Next tokens of 32 sequences of 16384: int8, 8 kv heads 106 us; aiming for 512 or 1024 whatever the tiles 118,
 // 111.  bf16, 32 kv heads 717; lowered there too 791.)
-// Totals are summed in halves of 24 bits, so that 64 lanes' sums fit.
 template <int RT>
-__device__ __forceinline__ int plan_q(const AttnChunkArgs& a, const Lanes& L, int G) {
-    if (RT >= 64 && a.chunk.n_seqs == 1) {
-        const Seq s{__builtin_amdgcn_readfirstlane(L.s0.row0), __builtin_amdgcn_readfirstlane(L.s0.n),
-                    __builtin_amdgcn_readfirstlane(L.s0.ctx), __builtin_amdgcn_readfirstlane(L.s0.len)};
-        const Plan p = plan_seq<RT>(s, G, 1);
-        const int tiles = std::max(1, p.tiles * a.kv.n_kv_heads);        // above 2^31 the launch is refused
-        int best = std::max(1, p.blocks), cost = ((tiles - 1 >> a.target) + 1) * (p.blocks + a.over);
-        for (int k = 0; k < 2; ++k) {
-            const int cut = std::min((1 << (a.target + k)) / tiles, p.blocks / a.min_blocks);
-            if (cut < 2) continue;
-            const int Q = (p.blocks + cut - 1) / cut;
-            const int c = ((tiles * cut - 1 >> a.target) + 1) * (Q + a.over) + a.join;
-            if (c < cost) {
-                cost = c;
-                best = Q;
-            }
+__device__ __forceinline__ int plan_one(const AttnChunkArgs& a, const Seq& s, int G) {
+    const Plan p = plan_seq<RT>(s, G, 1);
+    const int tiles = std::max(1, p.tiles * a.kv.n_kv_heads);        // above 2^31 the launch is refused
+    int best = std::max(1, p.blocks), cost = ((tiles - 1 >> a.target) + 1) * (p.blocks + a.over);
+    for (int k = 0; k < 2; ++k) {
+        const int cut = std::min((1 << (a.target + k)) / tiles, p.blocks / a.min_blocks);
+        if (cut < 2) continue;
+        const int Q = (p.blocks + cut - 1) / cut;
+        const int c = ((tiles * cut - 1 >> a.target) + 1) * (Q + a.over) + a.join;
+        if (c < cost) {
+            cost = c;
+            best = Q;
         }
-        return best;
     }
-    int64_t total = 0;
-    int tiles = 0;
-    for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
-        const Seq s = L.get(b0);
-        const Plan p = plan_seq<RT>(s, G, 1);
-        const int64_t t = (int64_t)p.tiles * p.blocks;
-        tiles += std::min(wave_total(RT == TILE_ROWS && few_rows(s, G) ? 0 : p.tiles), 1 << 20);
-        total += wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24);
-    }
+    return best;
+}
+// total: tiles times blocks of all sequences; tiles: those not of few rows.  Both of one kv head.
+template <int RT>
+__device__ __forceinline__ int plan_all(const AttnChunkArgs& a, int64_t total, int tiles) {
     total *= a.kv.n_kv_heads;
     const float round = (float)(1 << a.target), nt = (float)tiles * (float)a.kv.n_kv_heads;
     float aim = fmaxf(round - 0.5f * nt, 0.5f * round);
     if (RT < 64 && a.chunk.n_seqs == 1) aim = round;
     if (RT < 64 && nt >= round) aim = 2.f * round;
     return std::max(a.min_blocks, (int)fminf((float)total / aim, 2.5e8f) + 1);      // above any sequence's blocks
+}
+template <int RT>
+__device__ __forceinline__ int long_tiles(const Seq& s, int G, const Plan& p) {
+    return RT == TILE_ROWS && few_rows(s, G) ? 0 : p.tiles;
+}
+
+// Up to 256 sequences every workgroup plans for itself, up to four sequences a lane.  For more a kernel of its own does it
+// first (attn_plan_kernel, 5 us), and leaves Q, the totals and per sequence the running counts in a.plan:
+enum { PLAN_Q, PLAN_UNITS, PLAN_FEW, PLAN_SPLIT, PLAN_HEAD };        // totals: units, those of few rows, split tiles
+struct PlanRow {
+    int units, few, split, part;           // of the sequences before: units (of many rows, of few), split tiles, their pieces
+};
+constexpr int PER_LANE = 4, PLAN_LANES = 64 * PER_LANE;
+constexpr int64_t plan_ints(int n_seqs) { return n_seqs > PLAN_LANES ? PLAN_HEAD + 4 * (int64_t)n_seqs : 0; }
+
+// What a sequence adds to the running counts.
+template <int RT, bool SORT>
+__device__ __forceinline__ PlanRow plan_row(const Seq& s, int G, int nkv, int Q) {
+    const Plan p = plan_seq<RT>(s, G, Q);
+    const int u = p.tiles * p.pieces * nkv;
+    const bool few = SORT && few_rows(s, G), split = p.pieces > 1;
+    return PlanRow{few ? 0 : u, few ? u : 0, split ? p.tiles * nkv : 0, split ? u : 0};
 }
 
 // What a workgroup works on: row tile rt of kv head kvh of sequence b, blocks beg .. end - 1 (one of
@@ -111,59 +110,106 @@ struct Unit {
 constexpr int XCD_RUN = 4;
 template <int RT, bool SPLIT, bool SORT>
 __device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, Unit& un) {
-    const int nkv = a.kv.n_kv_heads, lane = threadIdx.x & 63;
-    const Lanes L(a.chunk);
-    const int Q = plan_q<RT>(a, L, G);
-    auto units = [&](const Plan& p) { return SPLIT ? (p.pieces > 1 ? p.tiles * nkv : 0) : p.tiles * p.pieces * nkv; };
+    constexpr bool CLASSES = RT == TILE_ROWS;            // as the plan counts them
+    const int nkv = a.kv.n_kv_heads, lane = threadIdx.x & 63, n_seqs = a.chunk.n_seqs;
+    int Q, all[2], splits;
+    const bool lanes = n_seqs <= PLAN_LANES;
+    const int per_lane = (n_seqs + 63) / 64;             // sequences per_lane * lane + i
+    Seq mine[PER_LANE];
+    PlanRow row[PER_LANE], sum{0, 0, 0, 0};
+    if (lanes) {
+#pragma unroll
+        for (int i = 0; i < PER_LANE; ++i) {
+            const int b = per_lane * lane + i;
+            mine[i] = i < per_lane && b < n_seqs ? load_seq(a.chunk, b) : Seq{0, 0, 0, 0};
+        }
+        if (RT >= 64 && n_seqs == 1) {
+            Q = plan_one<RT>(a, lane_seq(mine[0], 0), G);
+        } else {
+            int64_t t = 0;                               // summed in halves of 24 bits
+            int tiles = 0;
+#pragma unroll
+            for (int i = 0; i < PER_LANE; ++i) {
+                if (i >= per_lane) break;
+                const Plan p = plan_seq<RT>(mine[i], G, 1);
+                t += (int64_t)p.tiles * p.blocks;
+                tiles += long_tiles<RT>(mine[i], G, p);
+            }
+            Q = plan_all<RT>(a, wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24),
+                             std::min(wave_total(tiles), 1 << 24));
+        }
+#pragma unroll
+        for (int i = 0; i < PER_LANE; ++i) {
+            row[i] = PlanRow{0, 0, 0, 0};
+            if (i >= per_lane) continue;
+            row[i] = plan_row<RT, CLASSES>(mine[i], G, nkv, Q);
+            sum.units += row[i].units;
+            sum.few += row[i].few;
+            sum.split += row[i].split;
+            sum.part += row[i].part;
+        }
+        all[0] = wave_total(sum.units);
+        all[1] = CLASSES ? wave_total(sum.few) : 0;
+        splits = SPLIT ? wave_total(sum.split) : 0;
+    } else {
+        Q = a.plan[PLAN_Q];
+        all[0] = a.plan[PLAN_UNITS];
+        all[1] = a.plan[PLAN_FEW];
+        splits = a.plan[PLAN_SPLIT];
+    }
     int u = blockIdx.x;
     bool last = false;                         // the sequences with few rows
     if constexpr (SORT) {
-        int all[2] = {0, 0};
-        for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
-            const Seq s = L.get(b0);
-            const int c = units(plan_seq<RT>(s, G, Q));
-            const bool f = few_rows(s, G);
-            all[0] += wave_total(f ? 0 : c);
-            all[1] += wave_total(f ? c : 0);
-        }
         constexpr int R = 8 * XCD_RUN;
         const int first = (all[0] + R - 1) / R * R;
         last = u >= first;
         if (last) u -= first;
         u = u / R * R + u % 8 * XCD_RUN + u % R / 8;
-        if (u >= all[last]) return false;
     }
-    int part = 0;
-    un.b = -1;
-    for (int b0 = 0; b0 < a.chunk.n_seqs; b0 += 64) {
-        const Seq lane_seq = L.get(b0);
-        const Plan p = plan_seq<RT>(lane_seq, G, Q);
-        const int c = !SORT || few_rows(lane_seq, G) == last ? units(p) : 0, sp = p.pieces > 1 ? p.tiles * p.pieces * nkv : 0;
-        const int s = wave_scan(c);
+    if (u < 0 || u >= (SPLIT ? splits : all[last])) return false;
+    int part;
+    if (lanes) {
+        auto count = [&](const PlanRow& w) { return SPLIT ? w.split : last ? w.few : w.units; };
+        const int c = count(sum), s = wave_scan(c);
         const uint64_t past = __ballot(s > u);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            u -= __builtin_amdgcn_readlane(s - c, l);
-            part += wave_total(lane < l ? sp : 0);
-            un.b = b0 + l;
-            un.sq = Seq{__builtin_amdgcn_readlane(lane_seq.row0, l), __builtin_amdgcn_readlane(lane_seq.n, l),
-                        __builtin_amdgcn_readlane(lane_seq.ctx, l), __builtin_amdgcn_readlane(lane_seq.len, l)};
-            break;
+        if (past == 0) return false;
+        const int l = __builtin_ctzll(past);
+        u -= __builtin_amdgcn_readlane(s - c, l);
+        part = wave_total(lane < l ? sum.part : 0);
+        un.b = per_lane * l;
+        un.sq = lane_seq(mine[0], l);
+        bool here = true;                                // among the lane's sequences
+#pragma unroll
+        for (int i = 0; i + 1 < PER_LANE; ++i) {
+            if (i + 1 >= per_lane) break;
+            const int ci = __builtin_amdgcn_readlane(count(row[i]), l);
+            here = here && u >= ci;
+            if (!here) break;
+            u -= ci;
+            part += __builtin_amdgcn_readlane(row[i].part, l);
+            un.b = per_lane * l + i + 1;
+            un.sq = lane_seq(mine[i + 1], l);
         }
-        u -= __builtin_amdgcn_readlane(s, 63);
-        part += wave_total(sp);
+    } else {
+        const PlanRow* rows = (const PlanRow*)(a.plan + PLAN_HEAD);
+        auto before = [&](int b) { return SPLIT ? rows[b].split : last ? rows[b].few : rows[b].units; };
+        un.b = last_at_most(n_seqs, u, before);
+        if (un.b < 0) return false;
+        u -= before(un.b);
+        part = rows[un.b].part;
+        un.sq = load_seq(a.chunk, un.b);
     }
-    if (un.b < 0) return false;
     const Plan pl = plan_seq<RT>(un.sq, G, Q);
-    if (u < 0 || u >= units(pl)) return false;         // overlapping rows: sums past int32
+    const int units = SPLIT ? pl.tiles * nkv : pl.tiles * pl.pieces * nkv;
+    if (u < 0 || u >= units) return false;             // overlapping rows: sums past int32
     un.pieces = pl.pieces;
     un.rt = u % pl.tiles;
     const int v = u / pl.tiles, sp = SPLIT ? 0 : v % pl.pieces;
     un.kvh = SPLIT ? v : v / pl.pieces;
     un.part = part + (SPLIT ? un.kvh * pl.pieces * pl.tiles + un.rt : u);
     // the blocks up to the tile's last row, in equal pieces
-    const int row = min((un.rt + 1) * RT, un.sq.n * G) - 1;
-    const int blocks = min(pl.blocks, (un.sq.ctx + row / G) / VT_BLK + 1), per = (blocks + pl.pieces - 1) / pl.pieces;
+    const int last_row = min((un.rt + 1) * RT, un.sq.n * G) - 1;
+    const int blocks = min(pl.blocks, (un.sq.ctx + last_row / G) / VT_BLK + 1), per = (blocks + pl.pieces - 1) / pl.pieces;
     un.beg = sp * per;
     un.end = min(un.beg + per, blocks);
     return true;

@@ -296,6 +296,7 @@ struct AttnChunkArgs {
     uint16_t* out;            // [n_rows, n_heads, d], activation format out_fmt
     int out_fmt;
     float* ws;
+    int* plan;                // of many sequences, behind the partial results
     int target, min_blocks, over, join;   // set by the launcher: see attn_plan.h
 };
 size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads);

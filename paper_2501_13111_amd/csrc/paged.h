@@ -1,5 +1,5 @@
-// Device helpers of the paged-cache kernels: a chunk's sequences, the search for a workgroup's
-// share among them, and the pool's 32-position blocks.
+// Device helpers of the paged-cache kernels: a chunk's sequences, sums and searches over them, and the
+// pool's 32-position blocks.
 #pragma once
 #include "fp_device.h"
 
@@ -33,23 +33,25 @@ __device__ __forceinline__ int wave_scan(int v) {
 }
 __device__ __forceinline__ int wave_total(int v) { return __builtin_amdgcn_readlane(wave_scan(v), 63); }
 
-// The sequence b whose units (count(b) of them, in sequence order) include unit u, with u
-// counted from b's first: b, or -1 past the last unit.  Every lane of the wave gets the answer.
+// Sequence l of a wave's lanes' sequences.
+__device__ __forceinline__ Seq lane_seq(const Seq& s, int l) {
+    return Seq{__builtin_amdgcn_readlane(s.row0, l), __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.ctx, l),
+               __builtin_amdgcn_readlane(s.len, l)};
+}
+
+// The last b < n (at most 4096) with before(b) <= u, or -1, for a before() that does not decrease: 64 of them at a time, so two
+// loads after each other whatever n.  Where several sequences begin at one count, all but the last are empty.
 template <class F>
-__device__ __forceinline__ int find_seq(int n_seqs, int& u, F count) {
+__device__ __forceinline__ int last_at_most(int n, int u, F before) {
     const int lane = threadIdx.x & 63;
-    for (int b0 = 0; b0 < n_seqs; b0 += 64) {
-        const int c = b0 + lane < n_seqs ? count(b0 + lane) : 0;
-        const int s = wave_scan(c);
-        const uint64_t past = __ballot(s > u);
-        if (past) {
-            const int l = __builtin_ctzll(past);
-            u -= __builtin_amdgcn_readlane(s - c, l);
-            return b0 + l;
-        }
-        u -= __builtin_amdgcn_readlane(s, 63);
+    int base = 0;
+    if (n > 64) {
+        const int b = 64 * lane;
+        base = 64 * (__popcll(__ballot(b < n && before(b) <= u)) - 1);
+        if (base < 0) return -1;
     }
-    return -1;
+    const int b = base + lane;
+    return base + __popcll(__ballot(b < n && before(b) <= u)) - 1;
 }
 
 // The pool's block index of block blk (32 positions) of sequence b for kv head kvh: blocks of

@@ -22,6 +22,22 @@ __device__ __forceinline__ int seq_blocks(const Seq& s) {
     return s.n > 0 ? (s.len - 1) / VT_BLK - s.ctx / VT_BLK + 1 : 0;
 }
 
+// Room for the blocks of b sequences with r rows together: a sequence's n rows touch at most n / 32 + 2 blocks, and never more
+// than n.  Sequence b's begin at that of its first row, so a workgroup finds them by row_start alone.
+__host__ __device__ __forceinline__ int64_t blocks_before(int r, int b) {
+    const int64_t few = (int64_t)r / VT_BLK + 2 * (int64_t)b;
+    return few < r ? few : r;
+}
+// The sequence of block u, with u counted from its first block then; -1 if u is none.
+__device__ __forceinline__ int find_block(const fp_chunk& c, int& u, Seq& sq) {
+    auto before = [&](int b) { return (int)blocks_before(min(max(c.row_start[b], 0), c.n_rows), b); };
+    const int b = last_at_most(c.n_seqs, u, before);
+    if (b < 0) return -1;
+    u -= before(b);
+    sq = load_seq(c, b);
+    return u < seq_blocks(sq) ? b : -1;
+}
+
 // The workgroup's block and kv head.  Workgroup i runs on XCD i % 8: the heads of a block follow each other on one,
 // whose L2 fetches the block's angles once.
 __device__ __forceinline__ void unit(int nkv, int& u, int& kvh) {
@@ -96,9 +112,9 @@ __global__ void __launch_bounds__(T) kv_append_paged_kernel(KvAppendArgs a) {
     const int tid = threadIdx.x;
     int u, kvh;
     unit(a.kv.n_kv_heads, u, kvh);
-    const int b = find_seq(a.chunk.n_seqs, u, [&](int i) { return seq_blocks(load_seq(a.chunk, i)); });
+    Seq sq;
+    const int b = find_block(a.chunk, u, sq);
     if (b < 0) return;
-    const Seq sq = load_seq(a.chunk, b);
     const int blk = sq.ctx / VT_BLK + u;
     const int t0 = max(sq.ctx - blk * VT_BLK, 0), t1 = min(sq.len - blk * VT_BLK, VT_BLK);   // live positions
     const int np = t1 - t0;
@@ -187,9 +203,9 @@ __global__ void __launch_bounds__(T) kv_read_paged_kernel(KvReadArgs a) {
     const int tid = threadIdx.x;
     int u, kvh;
     unit(a.kv.n_kv_heads, u, kvh);
-    const int b = find_seq(a.chunk.n_seqs, u, [&](int i) { return seq_blocks(load_seq(a.chunk, i)); });
+    Seq sq;
+    const int b = find_block(a.chunk, u, sq);
     if (b < 0) return;
-    const Seq sq = load_seq(a.chunk, b);
     const int blk = sq.ctx / VT_BLK + u;
     const int t0 = max(sq.ctx - blk * VT_BLK, 0), t1 = min(sq.len - blk * VT_BLK, VT_BLK);
     const int np = t1 - t0;
@@ -249,11 +265,7 @@ __global__ void __launch_bounds__(T) kv_read_paged_kernel(KvReadArgs a) {
     }
 }
 
-// workgroups for the blocks that n_rows rows of n_seqs sequences can touch: a sequence's n rows
-// touch at most (n + 30) / 32 + 1, and never more than n
-int64_t max_blocks(const fp_chunk& c) {
-    return std::min<int64_t>(c.n_rows, (int64_t)c.n_rows / VT_BLK + 2 * (int64_t)c.n_seqs);
-}
+int64_t max_blocks(const fp_chunk& c) { return blocks_before(c.n_rows, c.n_seqs); }
 
 }  // namespace
 

@@ -534,3 +534,102 @@ def test_a_scale_of_nothing_averages(nkv, G, d, new, loose, scale, kvq):
     out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
     fp.attn_chunk(pool.device(), chunk, q.cuda(), out, scale=scale)
     _check_attention(pool, table, lens, q, out, scale, fp16=kvq == "int8")
+
+
+def _many(B, longest, new, seed, empty=0.1):
+    g = torch.Generator().manual_seed(seed)
+    ctx = (torch.rand(B, generator=g) ** 3 * longest).int().tolist()
+    n = torch.randint(1, new + 1, (B,), generator=g)
+    n[torch.rand(B, generator=g) < empty] = 0
+    return list(zip(ctx, n.tolist()))
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("B,longest,new,nkv,d", [(64, 300, 1, 2, 64), (65, 300, 90, 1, 128), (200, 100, 3, 2, 64), (1000, 50, 40, 1, 64),
+                                                 (4096, 40, 2, 1, 64), (4095, 10, 1, 1, 128)])
+def test_many_sequences_append_and_read(B, longest, new, nkv, d, kvq):
+    """Rows of every sequence land in its pages and come back; everything else stays as it was."""
+    fp = _fp()
+    lens = _many(B, longest, new, 121)
+    page = 32
+    need = [-(-(c + n) // page) for c, n in lens]
+    g = torch.Generator(device="cuda").manual_seed(122)
+    table = ref.tables(torch.Generator().manual_seed(122), need, sum(need) + 2, max(max(need), 1))
+    kv = fp.PagedKV.empty(sum(need) + 2, page, nkv, d, kvq)
+    pools = [kv.k, kv.v] + ([kv.k_scales, kv.v_scales] if kvq == "int8" else [])
+    for t in pools:
+        t.zero_()
+    # the whole sequences first, then the new rows over them with other values
+    whole, st = _chunk([(0, c + n) for c, n in lens], table)
+    k, v = (torch.randn(st[-1], nkv, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    fp.kv_append(kv, whole, k, v)
+    chunk, starts = _chunk(lens, table)
+    N = starts[-1]
+    k2, v2 = (torch.randn(N + 3, nkv, d, generator=g, device="cuda").bfloat16() for _ in range(2))
+    fp.kv_append(kv, chunk, k2, v2)
+    at = torch.cat([torch.arange(st[b] + c, st[b] + c + n) for b, (c, n) in enumerate(lens)]).cuda()
+    k[at], v[at] = k2[:N], v2[:N]
+    ko, vo = torch.empty_like(k), torch.empty_like(v)
+    fp.kv_read(kv, whole, ko, vo)
+    k3, v3 = (torch.full_like(t, 7.0) for t in (k2, v2))
+    fp.kv_read(kv, chunk, k3, v3)
+    assert (k3[N:] == 7.0).all() and (v3[N:] == 7.0).all()
+    for got, want in ((ko, k), (vo, v), (k3[:N], k2[:N]), (v3[:N], v2[:N])):
+        if kvq == "int8":
+            code, scale = ref.quantise(want.float().cpu())
+            want = (code.float() * scale.float()[..., None]).bfloat16().cuda()
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("loose", [False, True])
+@pytest.mark.parametrize("B,longest,new,nkv,G,d,kvq", [
+    (64, 3000, 1, 2, 4, 64, "bf16"), (65, 9000, 1, 2, 4, 128, "int8"), (200, 2000, 6, 1, 5, 64, "bf16"), (130, 2000, 9, 2, 8, 128, "bf16"),
+    (300, 900, 30, 1, 8, 64, "int8"), (100, 4000, 40, 1, 4, 128, "bf16"), (4096, 60, 2, 1, 1, 64, "int8"), (1000, 200, 1, 1, 16, 128, "bf16"),
+    (70, 4000, 30, 1, 8, 128, "int8"),
+])
+def test_many_sequences_attention(B, longest, new, nkv, G, d, kvq, loose):
+    fp = _fp()
+    if loose and new * G <= 64:
+        pytest.skip("the bound changes nothing for so few rows")
+    lens = _many(B, longest, new, 131)
+    kv, table, g = _fill_gpu(lens, 64, nkv, d, kvq, 131)
+    chunk, starts = _chunk(lens, table, loose=64 * loose)
+    q = torch.randn(starts[-1] + 1, nkv * G, d, generator=g, device="cuda").bfloat16()
+    out = torch.full_like(q, 7.0)
+    fp.attn_chunk(kv, chunk, q, out)
+    assert (out[starts[-1]:] == 7.0).all()
+    want, mag = _gpu_attention(kv, table, lens, q[:-1])
+    assert ((out[:-1].double() - want).abs() <= HALF_BF16 * want.abs() + (HALF_BF16 + 1e-4) * mag * (1 + HALF_BF16)).all()
+
+
+def test_many_sequences_captured():
+    """The plan of many sequences is made in the graph, for the lengths at the time of the replay."""
+    fp = _fp()
+    B, nkv, G, d, page = 150, 2, 4, 64, 64
+    kv, table, g = _fill_gpu([(2500, 0)] * B, page, nkv, d, "int8", 141)
+    rs = torch.zeros(B + 1, dtype=torch.int32).cuda()
+    cl = torch.zeros(B, dtype=torch.int32).cuda()
+    N = 3 * B
+    chunk = fp.Chunk(rs, cl, table.cuda(), max_new=3, max_len=2503 // page * page)
+    q = torch.randn(N, nkv * G, d, generator=g, device="cuda").bfloat16()
+    out, again = torch.zeros_like(q), torch.zeros_like(q)
+    ws = fp.attn_chunk_workspace(kv, chunk, N, nkv * G)
+    fp.attn_chunk(kv, chunk, q, out, workspace=ws)
+    torch.cuda.synchronize()
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        fp.attn_chunk(kv, chunk, q, out, workspace=ws)
+    for seed, longest in ((1, 2400), (2, 30), (3, 700), (4, 2400)):
+        lens = _many(B, longest, 3, seed, empty=0.3)
+        rs.copy_(torch.tensor([0] + torch.tensor([n for _, n in lens]).cumsum(0).tolist(), dtype=torch.int32))
+        cl.copy_(torch.tensor([c for c, _ in lens], dtype=torch.int32))
+        q.copy_(torch.randn(N, nkv * G, d, generator=g, device="cuda").bfloat16())
+        n = int(rs[-1])
+        out.zero_()
+        torch.cuda.synchronize()
+        gr.replay()
+        torch.cuda.synchronize()
+        fp.attn_chunk(kv, chunk, q, again)
+        assert torch.equal(out[:n], again[:n]) and not out[n:].any()
+        want, mag = _gpu_attention(kv, table, lens, q[:n])
+        assert ((out[:n].double() - want).abs() <= HALF_BF16 * want.abs() + (HALF_BF16 + 1e-4) * mag * (1 + HALF_BF16)).all()
