@@ -124,3 +124,53 @@ def test_rows_past_the_bounds_are_cut():
                     temperature=0.0)
     best = logits.argmax(-1)
     assert n.tolist() == [3, 2] and out[0].tolist() == best[:3].tolist() and out[1].tolist() == best[5:7].tolist() + [-1]
+
+
+@pytest.mark.parametrize("T", [0.0, 0.9])
+@pytest.mark.parametrize("rows,V", [([3, 2], 2**20), ([2], 2**20 - 1), ([1, 0, 4] * 1365 + [2], 40)])
+def test_largest_vocabulary_and_most_sequences(rows, V, T):
+    g = torch.Generator().manual_seed(V % 977)
+    starts, logits, probs, ids, u, ul = _inputs(g, rows, V, T, True)
+    _run(logits, starts, ids, probs, u, ul, T, max(rows))
+
+
+@pytest.mark.parametrize("T", [0.0, 0.9])
+def test_captured_calls_and_another_stream(T):
+    """Replays with other logits, drafts and row counts, eager calls between them."""
+    import paper_2501_13111_amd as fp
+    g = torch.Generator().manual_seed(21)
+    B, R, V = 7, 5, 9000
+    N = B * R
+    logits, probs = torch.zeros(N, V, device="cuda"), torch.zeros(N, V, device="cuda")
+    starts, ids = torch.zeros(B + 1, dtype=torch.int32, device="cuda"), torch.zeros(N, dtype=torch.int32, device="cuda")
+    u, ul = torch.zeros(N, device="cuda"), torch.zeros(B, device="cuda")
+    outs = [(torch.empty(B, R, dtype=torch.int32, device="cuda"), torch.empty(B, dtype=torch.int32, device="cuda")) for _ in range(3)]
+    ws = [fp.verify_draft_workspace(N, V, B) for _ in range(2)]
+
+    def run(o, w, stream=None):
+        fp.verify_draft(logits, starts, ids, u, ul, *o, draft_probs=probs, temperature=T, workspace=w, stream=stream)
+
+    run(outs[0], ws[0])
+    torch.cuda.synchronize()
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        run(outs[0], ws[0])
+    side = torch.cuda.Stream()
+    for step in range(4):
+        rows = torch.randint(0, R + 1, (B,), generator=g).tolist()
+        st, lg, pr, dr, uu, uul = _inputs(g, rows, V, T or 1.0, True)
+        n = st[-1]
+        starts.copy_(torch.tensor(st, dtype=torch.int32))
+        logits[:n], probs[:n], ids[:n], u[:n] = lg.cuda(), pr.cuda(), dr.cuda(), uu.cuda()
+        ul.copy_(uul)
+        torch.cuda.synchronize()
+        gr.replay()
+        with pytest.raises(ValueError):
+            run(outs[1], None, stream=side)
+        run(outs[1], ws[1], stream=side)
+        torch.cuda.synchronize()
+        run(outs[2], None)
+        torch.cuda.synchronize()
+        want = ref.verify(lg, st, dr, pr if T > 0 else None, uu, uul, T, R)
+        for o, k in outs:
+            assert [o[b, :k[b]].tolist() for b in range(B)] == want, step
