@@ -875,12 +875,12 @@ fp_status enqueue_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk& chu
                          float* attn_ws, hipStream_t st) {
     const fp_shape& s = h->s;
     const int M = chunk.n_rows, H = s.hidden;
-    const bool few = M <= s.max_batch;
+    const bool few = M <= s.max_batch, one = M == 1 && h->wq != FP_WQ_BF16_2OF4;
     const PrefillSplit sp = few ? PrefillSplit{} : prefill_splits(h, M);
     fp_status rc;
     int ks = 1;
     bool normed = false;
-    if (few)
+    if (few && !one)
         HIPCHK(launch_resid_norm(nullptr, 0, M, H, x, nullptr, h->L[0].attn_norm, s.rms_eps, h->act_in, h->act_fmt,
                                  h->ssq, nullptr, st));
     for (int l = 0; l < s.n_layers; ++l) {
@@ -889,7 +889,15 @@ fp_status enqueue_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk& chu
         const uint16_t* in = l == 0 ? x : h->xbuf;
         uint16_t* out = last ? y : h->xbuf;
         const float* qkv;
-        if (few) {
+        if (one) {                     // the decode step's schedule of one sequence
+            XIn xq;
+            xq.xf = XF_NORM;
+            xq.gain = W.attn_norm;
+            xq.ssq = l == 0 ? nullptr : h->ssq;
+            xq.ssq_blocks = resid_ssq_blocks(H);
+            if ((rc = run_skinny(h, in, W.qkv, 1, 0, xq, h->part, &ks, st))) return rc;
+            qkv = h->part;
+        } else if (few) {
             if ((rc = run_skinny_batch(h, h->act_in, W.qkv, M, 0, h->part, &ks, st))) return rc;
             qkv = h->part;
         } else {
@@ -927,6 +935,22 @@ fp_status enqueue_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk& chu
         HIPCHK(launch_attn_chunk(at, st));
         if (!few) {
             if ((rc = enqueue_prefill_tail(h, l, M, sp, in, out, &normed, st))) return rc;
+            continue;
+        }
+        if (one) {
+            XIn xo, xg, xd;
+            if ((rc = run_skinny(h, h->act_o, W.o, 1, 0, xo, h->part, &ks, st))) return rc;
+            HIPCHK(launch_resid_norm(h->part, ks, 1, H, in, h->hbuf, nullptr, s.rms_eps, nullptr, h->act_fmt, h->ssq, nullptr, st));
+            xg.xf = XF_NORM;
+            xg.gain = W.mlp_norm;
+            xg.ssq = h->ssq;
+            xg.ssq_blocks = resid_ssq_blocks(H);
+            if ((rc = run_skinny(h, h->hbuf, W.gu, 1, s.ffn, xg, h->part2, &ks, st))) return rc;
+            xd.xf = XF_SWIGLU;
+            xd.src_part = h->part2;
+            xd.src_ks = ks;
+            if ((rc = run_skinny(h, nullptr, W.down, 1, 0, xd, h->part, &ks, st))) return rc;
+            HIPCHK(launch_resid_norm(h->part, ks, 1, H, h->hbuf, out, nullptr, s.rms_eps, nullptr, h->act_fmt, h->ssq, nullptr, st));
             continue;
         }
         if ((rc = run_skinny_batch(h, h->act_o, W.o, M, 0, h->part, &ks, st))) return rc;
