@@ -218,7 +218,7 @@ static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     const int64_t pieces = piece_aim(RT, D), n = std::max(tiles + pieces, 2 * pieces) + 16 * XCD_RUN;
     if (n > INT_MAX) return hipErrorInvalidValue;
     // tiles that can be split: each has more than Q of the blocks
-    const unsigned split = (a.chunk.max_len - 1) / VT_BLK < a.min_blocks ? 0u : (unsigned)std::min<int64_t>(tiles, pieces);
+    const unsigned split = (a.chunk.max_len - 1) / VT_BLK < WHOLE<RT> ? 0u : (unsigned)std::min<int64_t>(tiles, pieces);
     if (a.chunk.n_seqs > PLAN_LANES) {
         FP_LAUNCH(attn_plan_kernel<RT>, dim3(1), dim3(PLAN_T), 0, st, a);
         const hipError_t e = hipGetLastError();

@@ -29,12 +29,17 @@ __device__ __forceinline__ QScale q_scale(float scale) {
 struct Plan {
     int tiles, blocks, pieces;             // row tiles, 32-key blocks, pieces per tile
 };
+// A tile of so few blocks is not split: joining costs as much as they do.  (Streamed, 600 positions, 8 kv heads of 128, bf16:
+// 64 sequences 22 us whole, 26 in two pieces; one sequence of 1000 17, 15.  Tiles of 256, 4 prompts of 512, 32 heads of 128, bf16
+// 37 whole, 47 in two.)
+template <int RT>
+constexpr int WHOLE = RT == TILE_ROWS ? 16 : 24;
 template <int RT>
 __device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int Q) {
     Plan p;
     p.tiles = (s.n * G + RT - 1) / RT;
     p.blocks = s.n > 0 ? (s.len - 1) / VT_BLK + 1 : 0;
-    p.pieces = (p.blocks + Q - 1) / Q;
+    p.pieces = p.blocks <= WHOLE<RT> ? std::min(p.blocks, 1) : (p.blocks + Q - 1) / Q;
     return p;
 }
 
