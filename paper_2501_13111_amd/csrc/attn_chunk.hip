@@ -43,8 +43,8 @@ __global__ void __launch_bounds__(256, NT == 1 ? 3 : NT == 4 && D == 128 ? 1 : 2
 }
 
 // The plan of more than 256 sequences (attn_plan.h), by one workgroup: PER sequences a thread, their sums and running
-// counts over the waves.  Next tokens of 1024 sequences of up to 200, 8 heads of 128, bf16: 142 us with it, of which it takes
-// 5; 306 with every workgroup planning for itself.  4096 sequences: 497, 2988.
+// counts over the waves.  Next tokens of 1024 sequences of up to 200, 8 heads of 128, bf16: 138 us with it, of which it takes
+// 5; 306 with every workgroup planning for itself.  4096 sequences: 496, 2988.
 constexpr int PLAN_T = 1024, PER = 4096 / PLAN_T;
 template <int RT>
 __global__ void __launch_bounds__(PLAN_T) attn_plan_kernel(AttnChunkArgs a) {

@@ -33,7 +33,7 @@ struct Plan {
 // 64 sequences 22 us whole, 26 in two pieces; one sequence of 1000 17, 15.  Tiles of 256, 4 prompts of 512, 32 heads of 128, bf16
 // 37 whole, 47 in two.)
 template <int RT>
-constexpr int WHOLE = RT == TILE_ROWS ? 16 : 24;
+constexpr int WHOLE = RT == TILE_ROWS ? 16 : RT == 64 ? 20 : 24;
 template <int RT>
 __device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int Q) {
     Plan p;
@@ -109,98 +109,97 @@ struct Unit {
     Seq sq;
     int b, kvh, rt, beg, end, pieces, part;
 };
-// Unit u, or false if there are not that many.  SPLIT: u counts the split tiles instead, and the unit
-// is the tile's first piece.  SORT: XCD_RUN consecutive units (row tiles that read the same keys) go to one XCD's
-// workgroups (workgroup i runs on XCD i % 8), and those of sequences with few rows, which are short, come last.
+// A workgroup's place among the units by a plan's totals: the unit, and whether it is one of few rows.  False past the last.
+// SPLIT: the split tiles are counted instead.  SORT: XCD_RUN consecutive units (row tiles that read the same keys) go to one
+// XCD's workgroups (workgroup i runs on XCD i % 8), and those of sequences with few rows, which are short, come last.
 constexpr int XCD_RUN = 4;
-template <int RT, bool SPLIT, bool SORT>
-__device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, Unit& un) {
-    constexpr bool CLASSES = RT == TILE_ROWS;            // as the plan counts them
-    const int nkv = a.kv.n_kv_heads, lane = threadIdx.x & 63, n_seqs = a.chunk.n_seqs;
-    int Q, all[2], splits;
-    const bool lanes = n_seqs <= PLAN_LANES;
-    const int per_lane = (n_seqs + 63) / 64;             // sequences per_lane * lane + i
-    Seq mine[PER_LANE];
-    PlanRow row[PER_LANE], sum{0, 0, 0, 0};
-    if (lanes) {
-#pragma unroll
-        for (int i = 0; i < PER_LANE; ++i) {
-            const int b = per_lane * lane + i;
-            mine[i] = i < per_lane && b < n_seqs ? load_seq(a.chunk, b) : Seq{0, 0, 0, 0};
-        }
-        if (RT >= 64 && n_seqs == 1) {
-            Q = plan_one<RT>(a, lane_seq(mine[0], 0), G);
-        } else {
-            int64_t t = 0;                               // summed in halves of 24 bits
-            int tiles = 0;
-#pragma unroll
-            for (int i = 0; i < PER_LANE; ++i) {
-                if (i >= per_lane) break;
-                const Plan p = plan_seq<RT>(mine[i], G, 1);
-                t += (int64_t)p.tiles * p.blocks;
-                tiles += long_tiles<RT>(mine[i], G, p);
-            }
-            Q = plan_all<RT>(a, wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24),
-                             std::min(wave_total(tiles), 1 << 24));
-        }
-#pragma unroll
-        for (int i = 0; i < PER_LANE; ++i) {
-            row[i] = PlanRow{0, 0, 0, 0};
-            if (i >= per_lane) continue;
-            row[i] = plan_row<RT, CLASSES>(mine[i], G, nkv, Q);
-            sum.units += row[i].units;
-            sum.few += row[i].few;
-            sum.split += row[i].split;
-            sum.part += row[i].part;
-        }
-        all[0] = wave_total(sum.units);
-        all[1] = CLASSES ? wave_total(sum.few) : 0;
-        splits = SPLIT ? wave_total(sum.split) : 0;
-    } else {
-        Q = a.plan[PLAN_Q];
-        all[0] = a.plan[PLAN_UNITS];
-        all[1] = a.plan[PLAN_FEW];
-        splits = a.plan[PLAN_SPLIT];
-    }
-    int u = blockIdx.x;
-    bool last = false;                         // the sequences with few rows
+template <bool SPLIT, bool SORT>
+__device__ __forceinline__ bool place(int units, int few, int split, int& u, bool& last) {
+    u = blockIdx.x;
+    last = false;
     if constexpr (SORT) {
         constexpr int R = 8 * XCD_RUN;
-        const int first = (all[0] + R - 1) / R * R;
+        const int first = (units + R - 1) / R * R;
         last = u >= first;
         if (last) u -= first;
         u = u / R * R + u % 8 * XCD_RUN + u % R / 8;
     }
-    if (u < 0 || u >= (SPLIT ? splits : all[last])) return false;
-    int part;
-    if (lanes) {
-        auto count = [&](const PlanRow& w) { return SPLIT ? w.split : last ? w.few : w.units; };
-        const int c = count(sum), s = wave_scan(c);
-        const uint64_t past = __ballot(s > u);
-        if (past == 0) return false;
-        const int l = __builtin_ctzll(past);
-        u -= __builtin_amdgcn_readlane(s - c, l);
-        part = wave_total(lane < l ? sum.part : 0);
-        un.b = per_lane * l;
-        un.sq = lane_seq(mine[0], l);
-        bool here = true;                                // among the lane's sequences
+    return u >= 0 && u < (SPLIT ? split : last ? few : units);
+}
+template <bool SPLIT>
+__device__ __forceinline__ int counted(const PlanRow& w, bool last) { return SPLIT ? w.split : last ? w.few : w.units; }
+
+// Sequence, unit in it and pieces of the split tiles before it, for up to 64 PER sequences: lane l has PER l .. PER l + PER - 1.
+template <int RT, bool SPLIT, bool SORT, int PER>
+__device__ __forceinline__ bool find_by_lanes(const AttnChunkArgs& a, int G, Unit& un, int& Q, int& u, int& part) {
+    constexpr bool CLASSES = RT == TILE_ROWS;            // as the plan counts them
+    const int nkv = a.kv.n_kv_heads, lane = threadIdx.x & 63, n_seqs = a.chunk.n_seqs;
+    Seq mine[PER];
+    PlanRow row[PER], sum{0, 0, 0, 0};
+    int64_t t = 0;                                       // summed in halves of 24 bits
+    int tiles = 0;
 #pragma unroll
-        for (int i = 0; i + 1 < PER_LANE; ++i) {
-            if (i + 1 >= per_lane) break;
-            const int ci = __builtin_amdgcn_readlane(count(row[i]), l);
-            here = here && u >= ci;
-            if (!here) break;
-            u -= ci;
-            part += __builtin_amdgcn_readlane(row[i].part, l);
-            un.b = per_lane * l + i + 1;
-            un.sq = lane_seq(mine[i + 1], l);
-        }
+    for (int i = 0; i < PER; ++i) {
+        const int b = PER * lane + i;
+        mine[i] = b < n_seqs ? load_seq(a.chunk, b) : Seq{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const Plan p = plan_seq<RT>(mine[i], G, 1);
+        t += (int64_t)p.tiles * p.blocks;
+        tiles += long_tiles<RT>(mine[i], G, p);
+    }
+    if (PER == 1 && RT >= 64 && n_seqs == 1) Q = plan_one<RT>(a, lane_seq(mine[0], 0), G);
+    else Q = plan_all<RT>(a, wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24),
+                          std::min(wave_total(tiles), 1 << 24));
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        row[i] = plan_row<RT, CLASSES>(mine[i], G, nkv, Q);
+        sum.units += row[i].units;
+        sum.few += row[i].few;
+        sum.split += row[i].split;
+        sum.part += row[i].part;
+    }
+    bool last;
+    if (!place<SPLIT, SORT>(SPLIT ? 0 : wave_total(sum.units), SORT ? wave_total(sum.few) : 0, SPLIT ? wave_total(sum.split) : 0, u, last))
+        return false;
+    const int c = counted<SPLIT>(sum, last), s = wave_scan(c);
+    const uint64_t past = __ballot(s > u);
+    if (past == 0) return false;
+    const int l = __builtin_ctzll(past);
+    u -= __builtin_amdgcn_readlane(s - c, l);
+    part = wave_total(lane < l ? sum.part : 0);
+    un.b = PER * l;
+    un.sq = lane_seq(mine[0], l);
+#pragma unroll
+    for (int i = 0; i + 1 < PER; ++i) {                  // among the lane's sequences
+        const int ci = __builtin_amdgcn_readlane(counted<SPLIT>(row[i], last), l);
+        if (u < ci) break;
+        u -= ci;
+        part += __builtin_amdgcn_readlane(row[i].part, l);
+        un.b = PER * l + i + 1;
+        un.sq = lane_seq(mine[i + 1], l);
+    }
+    return true;
+}
+
+// The workgroup's unit, or false if it has none.  SPLIT: its split tile instead, as the tile's first piece.
+template <int RT, bool SPLIT, bool SORT>
+__device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, Unit& un) {
+    const int nkv = a.kv.n_kv_heads, n_seqs = a.chunk.n_seqs;
+    int Q, u, part;
+    if (__builtin_expect(n_seqs <= 64, 1)) {
+        if (!find_by_lanes<RT, SPLIT, SORT, 1>(a, G, un, Q, u, part)) return false;
+    } else if (n_seqs <= PLAN_LANES) {
+        if (!find_by_lanes<RT, SPLIT, SORT, PER_LANE>(a, G, un, Q, u, part)) return false;
     } else {
+        bool last;
+        if (!place<SPLIT, SORT>(a.plan[PLAN_UNITS], a.plan[PLAN_FEW], a.plan[PLAN_SPLIT], u, last)) return false;
         const PlanRow* rows = (const PlanRow*)(a.plan + PLAN_HEAD);
-        auto before = [&](int b) { return SPLIT ? rows[b].split : last ? rows[b].few : rows[b].units; };
-        un.b = last_at_most(n_seqs, u, before);
+        un.b = last_at_most(n_seqs, u, [&](int b) { return counted<SPLIT>(rows[b], last); });
         if (un.b < 0) return false;
-        u -= before(un.b);
+        Q = a.plan[PLAN_Q];
+        u -= counted<SPLIT>(rows[un.b], last);
         part = rows[un.b].part;
         un.sq = load_seq(a.chunk, un.b);
     }
