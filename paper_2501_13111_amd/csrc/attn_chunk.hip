@@ -22,8 +22,8 @@
 //     m = max m_i,  l = sum l_i 2^(m_i - m),  o = sum o_i 2^(m_i - m) / l.
 // The plan depends on the inputs alone, so results repeat bit for bit.
 //
-// Next tokens of 32 sequences of 4096, 8 kv heads of 128 (268 MB of cache): bf16, 8 rows 51 us (5.2 TB/s, the
-// rate of a large copy), 24 rows 53, 48 rows 70; int8 34, 37, 83.  One sequence of 331 positions, 32 kv heads: 9.7 us, of
+// Next tokens of 32 sequences of 4096, 8 kv heads of 128 (268 MB of cache): bf16, 8 rows 50 us (5.3 TB/s, the
+// rate of a large copy), 24 rows 53, 48 rows 70; int8 31, 37, 68.  One sequence of 331 positions, 32 kv heads: 9.7 us, of
 // which 1.4 are the plan, 1.3 the first loads, 4 three blocks a wave and 1.8 the merge (a chain of memory latencies
 // and of code fetched for the first time: a second copy of the block's code cost 1 us).
 #include <climits>
@@ -170,22 +170,29 @@ __global__ void __launch_bounds__(256) attn_chunk_join_kernel(AttnChunkArgs a) {
     store4(a.out + ((int64_t)(un.sq.row0 + rho / G) * a.n_heads + un.kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
 }
 
-// Rows of a tile, by what a sequence can bring to a kv head and by the call's size.  Up to 64 rows stream (tiles of
-// 16, 32 or 64).  More stream too, in tiles of 64, while those tiles times the blocks that they can see are few: the
-// tiles of 256, where the matrix cores bound, need as many to fill the GPU and their longer start to pay.  us streamed
-// and tiled, at (new tokens after context), 8 heads a kv head:
+// Rows of a tile, by what a sequence can bring to a kv head and by the call's size: 64-row tiles times the blocks that
+// they can see.  us at (new tokens after context), 8 heads a kv head, unless said otherwise.
+//   More than 64 rows: tiles of 256, where the matrix cores bound, once they fill the GPU and their longer start pays.
+// Streamed and in tiles of 256:
 //     d 128, bf16   up to 2^13: 512 after 0 21, 34; 512 after 512 32, 35    above: 1024 after 0 61, 49; 1024 after 31744 831, 521
 //     d 64, bf16    up to 2^15: 1024 after 0 32, 35; 128 after 16000 40, 46    above: 2048 after 0 74, 63; 1024 after 31744 402, 375
 //     d 64, int8    always: 512 after 0 14, 33; 2048 after 0 77, 83; 8 sequences of 2048 after 2000 505, 551; 1024 after
 //                   31744 554, 523 (the tiles' unpacking costs as much as their products)
-// (a power of two either way changes a case near the border by a few percent).  32 rows of 64 would be cheaper as 64 with
-// d 64 only: 24 rows of 32 sequences of 4096, d 128, bf16 53, as 64 68; int8 37, 79.
+//   Streamed, more than 32 rows: tiles of 64 read the cache once for them all, tiles of 32 start and end sooner and
+// two or three waves a SIMD hide each other's waits.  In tiles of 64 and of 32:
+//     small calls, or up to 8 blocks: 256 after 0 d 128 16, 11; d 64 11, 8; 5 after 2000 d 128 bf16 23, 16
+//     int8 of 128 dims, up to 64 rows: 5 of 64 sequences after up to 2000 84, 75; 4 after 300, 16 heads a kv head 16, 10
+//     others: 5 of 16 sequences after up to 4000, d 128 bf16 36, 52; 512 after 512 32, 47; 6 of 32 after up to 4096, d 64 int8
+//     37, 42
 int tile_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
     const int64_t G = n_heads / kv.n_kv_heads, R = std::min(c.max_new, c.n_rows) * G;
-    if (R <= 64) return R <= 16 ? 16 : R <= 32 ? 32 : 64;
-    if (kv.head_dim == 64 && kv.format == FP_KV_INT8) return 64;
-    const double work = (double)((c.n_rows * G + 63) / 64) * kv.n_kv_heads * ((c.max_len - 1) / VT_BLK + 1);
-    return work <= (kv.head_dim == 128 ? 8192.0 : 32768.0) ? 64 : TILE_ROWS;
+    if (R <= 32) return R <= 16 ? 16 : 32;
+    const int blocks = (c.max_len - 1) / VT_BLK + 1;
+    const double work = (double)((c.n_rows * G + 63) / 64) * kv.n_kv_heads * blocks;
+    const bool i8 = kv.format == FP_KV_INT8;
+    if (R > 64 && !(kv.head_dim == 64 && i8) && work > (kv.head_dim == 128 ? 8192.0 : 32768.0)) return TILE_ROWS;
+    if (i8 && kv.head_dim == 128 && R <= 64) return 32;
+    return blocks <= 8 || work <= (i8 ? 4096.0 : 2048.0) ? 32 : 64;
 }
 
 // log2 of the workgroups that run at a time (those of few rows: a half more), and the least number of blocks

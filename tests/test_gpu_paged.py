@@ -633,3 +633,22 @@ def test_many_sequences_captured():
         assert torch.equal(out[:n], again[:n]) and not out[n:].any()
         want, mag = _gpu_attention(kv, table, lens, q[:n])
         assert ((out[:n].double() - want).abs() <= HALF_BF16 * want.abs() + (HALF_BF16 + 1e-4) * mag * (1 + HALF_BF16)).all()
+
+
+@pytest.mark.parametrize("nkv,G,d,kvq,lens,bound", [
+    (2, 8, 128, "int8", [(1000, 40), (700, 30), (0, 1)], 9600), (2, 8, 128, "int8", [(64, 70)], 9600),
+    (2, 8, 128, "bf16", [(1000, 40), (700, 30), (0, 1)], 9600), (1, 16, 128, "bf16", [(2100, 4), (30, 3)], 60000),
+    (2, 3, 64, "int8", [(900, 100), (20, 33)], 60000), (2, 3, 64, "bf16", [(900, 100), (20, 33)], 20000),
+    (4, 8, 64, "int8", [(900, 6), (1300, 8), (7, 5)], 30000),
+])
+def test_bounds_of_tiles_of_64_rows(nkv, G, d, kvq, lens, bound):
+    """Bounds on the positions for which the call streams in tiles of 64 rows."""
+    fp = _fp()
+    g, pool, table = _case(lens, 64, nkv, d, kvq, 151)
+    _fill(pool, table, lens, g, upto=lambda c, n: c + n)
+    table = torch.nn.functional.pad(table, (0, bound // 64 + 1 - table.shape[1]), value=-7)
+    chunk, starts = _chunk(lens, table, max_len=bound)
+    q = torch.randn(starts[-1], nkv * G, d, generator=g).bfloat16()
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    fp.attn_chunk(pool.device(), chunk, q.cuda(), out)
+    _check_attention(pool, table, lens, q, out)
