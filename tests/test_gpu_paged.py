@@ -585,7 +585,7 @@ def test_many_sequences_append_and_read(B, longest, new, nkv, d, kvq):
 @pytest.mark.parametrize("B,longest,new,nkv,G,d,kvq", [
     (64, 3000, 1, 2, 4, 64, "bf16"), (65, 9000, 1, 2, 4, 128, "int8"), (200, 2000, 6, 1, 5, 64, "bf16"), (130, 2000, 9, 2, 8, 128, "bf16"),
     (300, 900, 30, 1, 8, 64, "int8"), (100, 4000, 40, 1, 4, 128, "bf16"), (4096, 60, 2, 1, 1, 64, "int8"), (1000, 200, 1, 1, 16, 128, "bf16"),
-    (70, 4000, 30, 1, 8, 128, "int8"),
+    (70, 4000, 30, 1, 8, 128, "int8"), (300, 900, 30, 1, 8, 128, "bf16"), (257, 3000, 20, 2, 4, 128, "int8"), (256, 500, 70, 1, 2, 64, "bf16"),
 ])
 def test_many_sequences_attention(B, longest, new, nkv, G, d, kvq, loose):
     fp = _fp()
@@ -602,10 +602,11 @@ def test_many_sequences_attention(B, longest, new, nkv, G, d, kvq, loose):
     assert ((out[:-1].double() - want).abs() <= HALF_BF16 * want.abs() + (HALF_BF16 + 1e-4) * mag * (1 + HALF_BF16)).all()
 
 
-def test_many_sequences_captured():
+@pytest.mark.parametrize("B", [150, 300])
+def test_many_sequences_captured(B):
     """The plan of many sequences is made in the graph, for the lengths at the time of the replay."""
     fp = _fp()
-    B, nkv, G, d, page = 150, 2, 4, 64, 64
+    nkv, G, d, page = 2, 4, 64, 64
     kv, table, g = _fill_gpu([(2500, 0)] * B, page, nkv, d, "int8", 141)
     rs = torch.zeros(B + 1, dtype=torch.int32).cuda()
     cl = torch.zeros(B, dtype=torch.int32).cuda()
