@@ -35,7 +35,7 @@ __device__ __forceinline__ int find_block(const fp_chunk& c, int& u, Seq& sq) {
     if (b < 0) return -1;
     u -= before(b);
     sq = load_seq(c, b);
-    return u < seq_blocks(sq) ? b : -1;
+    return u >= 0 && u < seq_blocks(sq) ? b : -1;      // below 0: starts that decrease
 }
 
 // The workgroup's block and kv head.  Workgroup i runs on XCD i % 8: the heads of a block follow each other on one,

@@ -653,3 +653,39 @@ def test_bounds_of_tiles_of_64_rows(nkv, G, d, kvq, lens, bound):
     out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
     fp.attn_chunk(pool.device(), chunk, q.cuda(), out)
     _check_attention(pool, table, lens, q, out)
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("B,max_new,G,d", [(5, 3, 4, 64), (40, 40, 4, 128), (100, 2, 8, 128), (300, 60, 2, 64), (300, 1, 2, 128)])
+def test_contents_without_any_order_stay_inside_the_buffers(B, max_new, G, d, kvq):
+    """Row starts and contexts of any values at all: rows past the buffers' end and pages of no table keep what
+    they hold."""
+    fp = _fp()
+    nkv, page, width, N, extra = 2, 32, 4, 60, 4
+    g = torch.Generator().manual_seed(161)
+    big = torch.Generator(device="cuda").manual_seed(161)
+    perm = torch.randperm(B * width + 7, generator=g)
+    table, spare = perm[:B * width].int().view(B, width), perm[B * width:].cuda()
+    kv = fp.PagedKV.empty(B * width + 7, page, nkv, d, kvq)
+    pools = [kv.k, kv.v] + ([kv.k_scales, kv.v_scales] if kvq == "int8" else [])
+    for t in pools:
+        t.fill_(1)
+    rs, cl = torch.zeros(B + 1, dtype=torch.int32).cuda(), torch.zeros(B, dtype=torch.int32).cuda()
+    around = torch.zeros(B * width + 8192, dtype=torch.int32)          # pages on both sides of the table's
+    around[4096:4096 + B * width] = table.flatten()
+    held = around.cuda()
+    chunk = fp.Chunk(rs, cl, held[4096:4096 + B * width].view(B, width), max_new=max_new, max_len=width * page - 3)
+    q, out, k, v, ko, vo = (torch.full((N + extra, h, d), 7.0, dtype=torch.bfloat16, device="cuda") for h in (nkv * G,) * 2 + (nkv,) * 4)
+    for t in (q, k, v):
+        t[:N] = torch.randn(N, t.shape[1], d, generator=big, device="cuda").bfloat16()
+    for lo, hi in ((-20, 100), (0, N + 1), (-2**31, 2**31 - 1), (N - 2, N + 2)):
+        rs.copy_(torch.randint(lo, hi, (B + 1,), generator=g).int())
+        cl.copy_(torch.randint(max(lo, -2**31), min(4 * hi, 2**31 - 1), (B,), generator=g).int())
+        fp.kv_append(kv, chunk, k[:N], v[:N])
+        fp.kv_read(kv, chunk, ko[:N], vo[:N])
+        fp.attn_chunk(kv, chunk, q[:N], out[:N])
+        torch.cuda.synchronize()
+        for t in (out, ko, vo):
+            assert (t[N:] == 7.0).all()
+        for t in pools:
+            assert (t[spare] == 1).all()
