@@ -63,6 +63,7 @@ __global__ void __launch_bounds__(PLAN_T) attn_plan_kernel(AttnChunkArgs a) {
         total += (int64_t)p.tiles * p.blocks;
         tiles = std::min(tiles + long_tiles<RT>(sq[i], G, p), 1 << 20);
     }
+    total = std::min(total, TOTAL_MAX);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
         total += __shfl_xor(total, o, 64);

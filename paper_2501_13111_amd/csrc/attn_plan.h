@@ -70,15 +70,17 @@ __device__ __forceinline__ int plan_one(const AttnChunkArgs& a, const Seq& s, in
     }
     return best;
 }
+// A count of TOTAL_MAX leaves every tile whole, as a larger one does: rows that overlap cannot overflow the sums.
+constexpr int64_t TOTAL_MAX = (int64_t)1 << 40;
 // total: tiles times blocks of all sequences; tiles: those not of few rows.  Both of one kv head.
 template <int RT>
 __device__ __forceinline__ int plan_all(const AttnChunkArgs& a, int64_t total, int tiles) {
-    total *= a.kv.n_kv_heads;
     const float round = (float)(1 << a.target), nt = (float)tiles * (float)a.kv.n_kv_heads;
     float aim = fmaxf(round - 0.5f * nt, 0.5f * round);
     if (RT < 64 && a.chunk.n_seqs == 1) aim = round;
     if (RT < 64 && nt >= round) aim = 2.f * round;
-    return std::max(a.min_blocks, (int)fminf((float)total / aim, 2.5e8f) + 1);      // above any sequence's blocks
+    const float q = (float)total * (float)a.kv.n_kv_heads / aim;
+    return std::max(a.min_blocks, (int)fminf(q, 2.5e8f) + 1);        // above any sequence's blocks
 }
 template <int RT>
 __device__ __forceinline__ int long_tiles(const Seq& s, int G, const Plan& p) {
@@ -149,6 +151,7 @@ __device__ __forceinline__ bool find_by_lanes(const AttnChunkArgs& a, int G, Uni
         t += (int64_t)p.tiles * p.blocks;
         tiles += long_tiles<RT>(mine[i], G, p);
     }
+    t = std::min(t, TOTAL_MAX);
     if (PER == 1 && RT >= 64 && n_seqs == 1) Q = plan_one<RT>(a, lane_seq(mine[0], 0), G);
     else Q = plan_all<RT>(a, wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24),
                           std::min(wave_total(tiles), 1 << 24));
