@@ -21,7 +21,8 @@
 //
 // int8: keys and values are unpacked to fp16 with their scales (code * scale rounded to 11 bits, so that
 // none may reach 65520: half the error that bf16's 8 bits leave in the output, and the matrix cores take no
-// scale); queries are fp16 too, a row of large ones scaled by a power of two.
+// scale); queries are fp16 too, each row brought to the top of its range by a power of two that the scale takes
+// back, so that only elements 2^-29 of the row's largest and smaller lose bits.
 //
 // 1024 tokens after 31744, 32 heads on 4 of 128: bf16 555 us, 0.98 PFLOP/s of the 1.31 that a large library matrix
 // product reaches; int8 640, 0.83 (its unpacking takes the instructions that the longer trip shows); heads of 64, bf16
@@ -269,8 +270,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                 for (int x = 0; x < 4; ++x)
                     m = fmaxf(m, fmaxf(fabsf(__uint_as_float(qf[c][j][x] << 16)), fabsf(__uint_as_float(qf[c][j][x] & 0xFFFF0000u))));
             m = fmaxf(m, __shfl_xor(m, 32, 64));
-            const int e = live && m >= 32768.f ? __builtin_amdgcn_frexp_expf(m) - 15 : 0;
-            sl2[c] = __builtin_amdgcn_ldexpf(sl2[c], e);
+            // the row's largest to 2^14 .. 2^15 (2^-e stays finite: bf16's least, 2^-133, comes to 2^-7, exact); the
+            // scale takes 2^e and stays a number above zero, which turns a masked score's -infinity into no NaN
+            const int e = live && m > 0.f ? max(__builtin_amdgcn_frexp_expf(m) - 15, -126) : 0;
+            sl2[c] = fminf(fmaxf(__builtin_amdgcn_ldexpf(sl2[c], e), 1.2e-38f), 3.4e38f);
             const float f = __builtin_amdgcn_ldexpf(1.f, -e);
 #pragma unroll
             for (int j = 0; j < NKC; ++j)

@@ -1,0 +1,34 @@
+"""Chunk attention at the ends of the number ranges that its entry accepts."""
+import math
+
+import pytest
+import torch
+
+import test_gpu_paged as paged
+
+pytestmark = pytest.mark.gpu
+
+# (rows of every tile size; with a loose bound more than 64 rows take the tiles of 256)
+CALLS = [(1, 8, 1, 0), (2, 8, 5, 0), (2, 4, 60, 0), (2, 4, 60, 64), (1, 1, 300, 64)]
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("nkv,G,new,loose", CALLS)
+@pytest.mark.parametrize("size", [1e-30, 1e-10, 1e-8, 1e-6, 1e-3, 1e6, 1e30])
+def test_queries_of_any_size(size, nkv, G, new, loose, kvq):
+    """Queries of one size and a scale that makes ordinary scores of them; rows of zeros and rows 2^20 smaller
+    beside them."""
+    fp = paged._fp()
+    d, page, lens = 128, 64, [(900, new), (70, new)]
+    g, pool, table = paged._case(lens, page, nkv, d, kvq, 171)
+    paged._fill(pool, table, lens, g, upto=lambda c, n: c + n)
+    chunk, starts = paged._chunk(lens, table, loose=loose)
+    q = size * torch.randn(starts[-1], nkv * G, d, generator=g)
+    q[1::5] = 0
+    q[3::5] *= 2.0 ** -20
+    q = q.bfloat16()
+    scale = 2.0 / math.sqrt(d) / size
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    fp.attn_chunk(pool.device(), chunk, q.cuda(), out, scale=scale)
+    # int8 in tiles of 256 rows: keys, values and queries meet the matrix cores as fp16
+    paged._check_attention(pool, table, lens, q, out, scale, fp16=kvq == "int8" and bool(loose))
