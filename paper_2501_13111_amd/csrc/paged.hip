@@ -79,8 +79,9 @@ __device__ __forceinline__ void load8(const void* base, int64_t off, int ks, int
     }
 }
 
+// x / s rounded.  Under a scale that is zero, infinite or NaN codes are zero: the last two read back as NaN.
 __device__ __forceinline__ int8_t code8(float x, float s) {
-    return s == 0.f ? (int8_t)0 : (int8_t)(int)fminf(fmaxf(rintf(__fdiv_rn(x, s)), -127.f), 127.f);
+    return s > 0.f && s < INFINITY ? (int8_t)(int)fminf(fmaxf(rintf(__fdiv_rn(x, s)), -127.f), 127.f) : (int8_t)0;
 }
 __device__ __forceinline__ u32x2 codes8(const float (&x)[8], float s) {
     uint32_t w[2] = {0u, 0u};
@@ -143,12 +144,13 @@ __global__ void __launch_bounds__(T) kv_append_paged_kernel(KvAppendArgs a) {
         }
         float sc = 0.f;
         if constexpr (KV8) {
-            float m = 0.f;
+            // the largest magnitude by its bits, in which a NaN is above all others (fmaxf would drop it)
+            uint32_t m = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m = fmaxf(m, fmaxf(fabsf(lo[e]), fabsf(hi[e])));
+            for (int e = 0; e < 8; ++e) m = max(m, max(__float_as_uint(fabsf(lo[e])), __float_as_uint(fabsf(hi[e]))));
 #pragma unroll
-            for (int o = 1; o < NP; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, NP));
-            const uint16_t sh = f2h(__fdiv_rn(m, 127.0f));
+            for (int o = 1; o < NP; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, NP));
+            const uint16_t sh = f2h(__fdiv_rn(__uint_as_float(m), 127.0f));
             sc = h2f(sh);
             if (j == 0 && pb >= 0) (what == 0 ? a.kv.k_scales : a.kv.v_scales)[(int64_t)pb * VT_BLK + t] = sh;
         }
