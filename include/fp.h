@@ -323,8 +323,8 @@ fp_status fp_kv_read(const fp_paged_kv* kv, const fp_chunk* chunk, void* k_out, 
  * bf16 [n_rows, n_heads, head_dim]; both 16-byte aligned.  Query group n_heads / n_kv_heads from
  * 1 to 16.  Scores, softmax statistics and sums are fp32; probabilities enter the product with V as bf16
  * (int8 caches: fp16).  Keys and values that are NaN or infinite reach the rows that see them and no
- * others.  int8: keys and values below 65504 in magnitude (calls of more than 64 rows per sequence
- * and kv head unpack them to fp16).
+ * others.  bf16: values below 2^127 in magnitude over up to 2^24 positions cannot overflow the sums.  int8: keys
+ * and values below 65504 in magnitude (calls of more than 64 rows per sequence and kv head unpack them to fp16).
  * workspace: device memory of at least fp_attn_chunk_workspace bytes, 16-byte aligned, which
  * the call may use until the stream has passed it (calls that can overlap need one each); enough
  * for one chunk's bounds is enough for any chunk of smaller ones.  FP_ERR_CAPACITY if workspace_bytes

@@ -16,7 +16,9 @@ __device__ __forceinline__ float max_groups(float v) {
 }
 
 // The softmax's reference moves only when a score passes it by 2^SLACK, so that few blocks rescale the sums.
-constexpr float SLACK = 8.f;
+// bf16 caches: and then to 2^(SLACK + ROOM) above that score, so that probabilities are at most 2^-ROOM and values up to
+// 2^127 cannot overflow the sums of 2^24 positions (bf16 and fp32 have exponents enough below).
+constexpr float SLACK = 8.f, ROOM = 24.f;
 
 template <int D, bool KV8>
 struct Chunk {
@@ -150,7 +152,7 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
     // only long bf16 batches, bound by memory, gain 2 %.)
     auto compute = [&](int i, int next) {
         const int base = (beg + w + 4 * i) * VT_BLK;
-        float ksc[2][4], vsc[2][4], lk = 0.f;
+        float ksc[2][4], vsc[2][4], lk = SLACK + ROOM;       // lk: from the block's largest score to its reference
         const bool edge = base + VT_BLK > sq.ctx + 1;        // some row may not see all of the block
         if (edge) {
             uint32_t bad = 0;

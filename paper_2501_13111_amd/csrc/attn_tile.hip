@@ -16,8 +16,8 @@
 //
 // The softmax's reference m moves only when a score passes it by 2^LAZY, and then to 2^-BELOW of that
 // score; the accumulators are rescaled then, outside the inner loop.  Probabilities are taken relative to m:
-// at most 2^(LAZY + BELOW), 2^15, so that in fp16 those down to 2^-21 of the largest keep all their bits
-// (smaller ones are off by 2^-32 of it at most).
+// at most 2^(LAZY + BELOW).  int8: 2^15, so that in fp16 those down to 2^-21 of the largest keep all their bits
+// (smaller ones are off by 2^-32 of it at most).  bf16: 2^-ROOM (attn_stream.h), for values of any size.
 //
 // int8: keys and values are unpacked to fp16 with their scales (code * scale rounded to 11 bits, so that
 // none may reach 65520: half the error that bf16's 8 bits leave in the output, and the matrix cores take no
@@ -39,7 +39,9 @@ namespace fpk {
 
 namespace {
 
-constexpr float LAZY = 8.f, BELOW = 7.f;
+constexpr float LAZY = 8.f;
+template <bool KV8>
+constexpr float BELOW = KV8 ? 7.f : -(LAZY + ROOM);
 constexpr int RING = 8;                    // LDS slots
 constexpr int AHEAD = 4;                   // blocks on their way (int8: in registers, two; unpacked two ahead)
 constexpr int FD = 4;                      // fragments read ahead
@@ -355,7 +357,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
             t[c][0] = max3(t[c][0], t[c][1], t[c][2]);
             t[c][1] = max3(t[c][3], t[c][4], cur.s[c][15]);
         };
-        auto max_c = [&](int c) { t[c][0] = fmaf(fmaxf(t[c][0], t[c][1]), sl2[c], -BELOW); };
+        auto max_c = [&](int c) { t[c][0] = fmaf(fmaxf(t[c][0], t[c][1]), sl2[c], -BELOW<KV8>); };
         auto ref_a = [&](int c) {          // the other half's keys belong to the same rows
             const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(t[c][0]), __float_as_uint(t[c][0]), false, false);
             t[c][0] = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));

@@ -32,3 +32,25 @@ def test_queries_of_any_size(size, nkv, G, new, loose, kvq):
     fp.attn_chunk(pool.device(), chunk, q.cuda(), out, scale=scale)
     # int8 in tiles of 256 rows: keys, values and queries meet the matrix cores as fp16
     paged._check_attention(pool, table, lens, q, out, scale, fp16=kvq == "int8" and bool(loose))
+
+
+@pytest.mark.parametrize("nkv,G,d,lens,loose", [
+    (1, 8, 128, [(900, 1), (5000, 1)], 0), (2, 8, 64, [(3000, 3), (31, 4)], 0), (2, 4, 128, [(300, 20), (0, 64)], 0),
+    (2, 4, 128, [(2000, 64), (0, 300)], 64), (1, 2, 64, [(700, 200), (5, 1)], 64), (1, 1, 128, [(0, 1000)], 64),
+])
+@pytest.mark.parametrize("top", [2.0 ** 126, 2.0 ** 112, 2.0 ** -60])
+def test_values_of_any_size(top, nkv, G, d, lens, loose):
+    """bf16 values of one sign, so that nothing cancels in the sums: finite outputs for all that are below 2^127."""
+    fp = paged._fp()
+    page = 64
+    g, pool, table = paged._case(lens, page, nkv, d, "bf16", 181)
+    for b, (c, n) in enumerate(lens):
+        m = c + n
+        pool.write(table[b], torch.arange(m), torch.randn(m, nkv, d, generator=g).bfloat16().float(),
+                   (top * (0.5 + 0.5 * torch.rand(m, nkv, d, generator=g))).bfloat16().float())
+    chunk, starts = paged._chunk(lens, table, loose=loose)
+    q = torch.randn(starts[-1], nkv * G, d, generator=g).bfloat16()
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    fp.attn_chunk(pool.device(), chunk, q.cuda(), out)
+    assert torch.isfinite(out.float()).all()
+    paged._check_attention(pool, table, lens, q, out)
