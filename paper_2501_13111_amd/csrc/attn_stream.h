@@ -154,6 +154,20 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
         const int base = (beg + w + 4 * i) * VT_BLK;
         float ksc[2][4], vsc[2][4], lk = SLACK + ROOM;       // lk: from the block's largest score to its reference
         const bool edge = base + VT_BLK > sq.ctx + 1;        // some row may not see all of the block
+        // positions past the sequence hold anything: their values must not meet a zero probability (cleared before the
+        // look for values that are not finite, which would take them for the sequence's)
+        if (base + VT_BLK > sq.len) {
+            const int nk = sq.len - base;
+            if constexpr (KV8) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) c.vs[t] &= u32x2{slots_below(g, 2 * t, nk), slots_below(g, 2 * t + 1, nk)};
+            } else {
+#pragma unroll
+                for (int dd = 0; dd < ND; ++dd)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) c.v[dd][x] &= slots_below(g, x, nk);
+            }
+        }
         if (edge) {
             uint32_t bad = 0;
             if constexpr (KV8) {
@@ -181,23 +195,6 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
                     ksc[t][e] = h2f((uint16_t)((e < 2 ? c.ks[t].x : c.ks[t].y) >> (16 * (e & 1)))) * sl2;
                     vsc[t][e] = h2f((uint16_t)((e < 2 ? c.vs[t].x : c.vs[t].y) >> (16 * (e & 1))));
                 }
-        }
-        // positions past the sequence hold anything: their values must not meet a zero probability
-        if (base + VT_BLK > sq.len) {
-            const int nk = sq.len - base;
-#pragma unroll
-            for (int dd = 0; dd < ND; ++dd) {
-                if constexpr (!KV8) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) c.v[dd][x] &= slots_below(g, x, nk);
-                }
-            }
-            if constexpr (KV8) {
-#pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) vsc[t][e] = 16 * t + 4 * g + e < nk ? vsc[t][e] : 0.f;
-            }
         }
         // P v_scale is at most 2^15: log2 of the block's largest value scale, less 15 and the reference's
         // slack.  Products down to 2^-21 of the largest keep fp16's full precision.

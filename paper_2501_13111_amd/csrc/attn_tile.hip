@@ -204,10 +204,18 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         for (int x = 0; x < 4; ++x) stage_v(i, r, x);
     };
 
-    // bf16: a block's values in LDS, each wave a quarter, before the barrier that ends the trip
+    // bf16: a block's values in LDS, each wave a quarter, before the barrier that ends the trip.  Those of positions
+    // past the sequence, which may be anything, become zeros first.
     auto scrub = [&](int i) {
         if constexpr (!KV8) {
             char* const v = smem + (i & (RING - 1)) * SB + NKC * 1024 + 16 * tid;
+            const int nk = uni(sq.len - (beg + i) * VT_BLK);
+            if (nk < VT_BLK) {
+                const u32x4 keep = {slots_below((tid >> 4) & 3, 0, nk), slots_below((tid >> 4) & 3, 1, nk),
+                                    slots_below((tid >> 4) & 3, 2, nk), slots_below((tid >> 4) & 3, 3, nk)};
+#pragma unroll
+                for (int x = 0; x < NVC / 4; ++x) *(u32x4*)(v + 4096 * x) &= keep;
+            }
             uint32_t bad = 0;
 #pragma unroll
             for (int x = 0; x < NVC / 4; ++x) {
@@ -559,16 +567,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
                 });
                 asm volatile("s_nop 4" ::: "memory");      // before a product adds to them
             }
-            // the last block's values; a sequence may end inside it, and what lies behind must not meet
-            // a zero probability (int8: its scales were cleared)
-            const int nk = sq.len - (beg + nw - 1) * VT_BLK;
+            // the last block's values
 #pragma unroll
             for (int x = 0; x < NVC; ++x) {
-                u32x4 v = vfrag((nw - 1) & (RING - 1), x);
-                if constexpr (!KV8) {
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) v[y] &= slots_below(2 * (x / NDT) + h32, y, nk);
-                }
+                const u32x4 v = vfrag((nw - 1) & (RING - 1), x);
                 oacc[0][x % NDT] = mfma32<PF>(v, pa.p[0][x / NDT], oacc[0][x % NDT]);
                 oacc[1][x % NDT] = mfma32<PF>(v, pa.p[1][x / NDT], oacc[1][x % NDT]);
             }

@@ -1,4 +1,5 @@
-"""Keys and values that are not finite on their way into an int8 cache and out of it."""
+"""Keys and values that are not finite on their way into an int8 cache and out of it, and the time that
+unwritten positions may take."""
 import math
 
 import pytest
@@ -67,3 +68,46 @@ def test_int8_appends_of_values_that_are_not_finite(nkv, G, d, lens, loose, rota
         # in: 2^-11 of the values' sum either way, fp32 sums, and both outputs' rounding)
         a, w = out[rows][~reach].double(), clean[2][rows][~reach].double()
         assert ((a - w).abs() <= 2 * (paged.HALF_BF16 * w.abs() * 1.01 + (2.0 ** -11 + 1e-5) * 1.01 * clean[1].abs().amax())).all()
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("nkv,G,d,lens,loose", [
+    (2, 4, 128, [(1500, 301), (0, 333)], 64),           # tiles of 256 rows
+    (2, 4, 64, [(1500, 301), (0, 333)], 64),
+    (2, 4, 64, [(0, 75)] * 4, 0),                       # streamed
+    (4, 8, 128, [(2000, 17)] * 8, 0),
+])
+def test_what_unwritten_positions_hold_takes_no_time(nkv, G, d, lens, loose, kvq):
+    """Sequences that end inside a block: NaN behind their ends costs nothing against zeros there.  (Looking
+    at each position again for each row costs tens of times the whole call.)"""
+    fp = paged._fp()
+    page = 64
+    g, pool, table = paged._case(lens, page, nkv, d, kvq, 201)
+    paged._fill(pool, table, lens, g, upto=lambda c, n: c + n)
+    chunk, starts = paged._chunk(lens, table, loose=loose)
+    q = torch.randn(starts[-1], nkv * G, d, generator=g).bfloat16().cuda()
+    odd = pool.device()
+    plain = [t.clone() for t in pool.tensors()]
+    if kvq == "bf16":
+        plain = [torch.nan_to_num(t, 0.0) for t in plain]
+    else:
+        plain[2:] = [torch.nan_to_num(t, 0.0) for t in plain[2:]]
+    even = fp.PagedKV(*[t.cuda() for t in plain])
+    out = {}
+    ws = fp.attn_chunk_workspace(odd, chunk, starts[-1], nkv * G)
+
+    def us(kv, name):
+        out[name] = torch.empty_like(q)
+        best = math.inf
+        for _ in range(12):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            fp.attn_chunk(kv, chunk, q, out[name], workspace=ws)
+            b.record()
+            b.synchronize()
+            best = min(best, 1e3 * a.elapsed_time(b))
+        return best
+
+    te, to = us(even, "even"), us(odd, "odd")
+    assert torch.equal(out["even"], out["odd"])
+    assert to < 2 * te, f"{to:.0f} us with NaN, {te:.0f} us with zeros"
