@@ -72,6 +72,19 @@ def _call(name, device, stream, *args):
         _check(rc, name)
 
 
+class _Fixed:
+    """Attributes that are set once: calls use the addresses and bounds taken from them when the object was
+    made.  Contents of tensors may change in place."""
+
+    def __setattr__(self, name, value):
+        if self.__dict__.get(name, value) is not value:
+            raise AttributeError(f"{name} cannot be replaced, make a new {type(self).__name__}")
+        self.__dict__[name] = value
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{name} cannot be taken out of a {type(self).__name__}")
+
+
 class PagedKV:
     """One layer's paged cache over the caller's pool tensors.
 
@@ -113,10 +126,11 @@ class PagedKV:
         return cls(k, v, *sc) if kvq == "int8" else cls(k, v)
 
 
-class Chunk:
+class Chunk(_Fixed):
     """A ragged batch of rows: row_start int32 [n_seqs + 1], ctx_len int32 [n_seqs], table int32
     [n_seqs, pages per sequence] on the device, and host bounds on a sequence's rows (max_new) and
-    on its positions with them (max_len; the table's whole width if not given)."""
+    on its positions with them (max_len; the table's whole width if not given).  The tensors' contents
+    may change between calls; other tensors or bounds make another Chunk."""
 
     def __init__(self, row_start, ctx_len, table, max_new: int, max_len: int | None = None):
         if not isinstance(table, torch.Tensor) or table.dim() != 2:
@@ -129,7 +143,7 @@ class Chunk:
         self._p = (_tensor(row_start, torch.int32, "row_start", (B + 1,), device=table.device),
                    _tensor(ctx_len, torch.int32, "ctx_len", (B,), device=table.device), _tensor(table, torch.int32, "table"))
         self.n_seqs = B
-        self._c = {}
+        self._c = {}             # the last C structures, by row count and page size
 
     def c(self, kv: PagedKV, n_rows: int):
         """The C structure for n_rows rows over kv's pages."""
@@ -138,6 +152,8 @@ class Chunk:
         key = (n_rows, kv.page_size)
         c = self._c.get(key)
         if c is None:
+            if len(self._c) >= 32:
+                self._c.clear()
             max_len = self.max_len if self.max_len is not None else min(self.width * kv.page_size, 2**31 - 1)
             c = self._c[key] = ctypes.byref(_Chunk(self.n_seqs, n_rows, self.max_new, max_len, self.width, *self._p))
         return c
