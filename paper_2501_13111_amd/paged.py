@@ -85,12 +85,12 @@ class _Fixed:
         raise AttributeError(f"{name} cannot be taken out of a {type(self).__name__}")
 
 
-class PagedKV:
+class PagedKV(_Fixed):
     """One layer's paged cache over the caller's pool tensors.
 
     k [n_pages, n_kv_heads, page_size, head_dim], v [n_pages, n_kv_heads, page_size / 32, head_dim,
     32], bfloat16 or int8; int8 also k_scales and v_scales, float16 [n_pages, n_kv_heads, page_size].
-    ``PagedKV.empty`` allocates them.
+    ``PagedKV.empty`` allocates them.  Other tensors make another PagedKV.
     """
 
     def __init__(self, k, v, k_scales=None, v_scales=None):

@@ -1,5 +1,5 @@
-"""What a chunk keeps of the tensors and bounds that it was made from (host tensors that pass for
-device ones: nothing is launched)."""
+"""What a chunk and a paged cache keep of the tensors and bounds that they were made from (host tensors that pass
+for device ones: nothing is launched)."""
 import ctypes
 
 import pytest
@@ -60,3 +60,17 @@ def test_a_chunk_keeps_few_structures():
             s = struct(c, kv, n)
             assert s.n_rows == n and s.max_len == 5 * page
     assert sum(len(x) for x in vars(c).values() if isinstance(x, dict)) <= 64
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.int8])
+def test_a_paged_cache_does_not_change_under_its_calls(dtype):
+    kv = cache(dtype=dtype)
+    before, held = bytes(kv.struct), [kv.k, kv.v, kv.k_scales, kv.v_scales]
+    for name, value in (("k", kv.k.clone()), ("v", kv.v.clone()), ("k_scales", dev(torch.zeros(1))), ("v_scales", dev(torch.zeros(1))),
+                        ("n_pages", 4), ("page_size", 32), ("n_kv_heads", 1), ("head_dim", 128), ("kvq", "none"),
+                        ("device", torch.device("cpu", 1))):
+        with pytest.raises(AttributeError, match=name):
+            setattr(kv, name, value)
+    assert bytes(kv.struct) == before and all(a is b for a, b in zip(held, [kv.k, kv.v, kv.k_scales, kv.v_scales]))
+    kv.k += 1                                          # contents may change
+    assert kv.struct.k == kv.k.data_ptr()
