@@ -345,7 +345,8 @@ fp_status fp_attn_chunk(const fp_paged_kv* kv, const fp_chunk* chunk, const void
  * weights and activations are used, its own cache, position and batch are not touched.
  * n_rows <= max_batch * max_prompt and max_len <= max_seq (FP_ERR_CAPACITY); up to max_batch
  * rows take the decode projections.  workspace: as for fp_attn_chunk (the largest of the
- * layers').  May be captured into a graph; allocates nothing.  The debug dumps are not written.
+ * layers').  May be captured into a graph; allocates nothing.  The debug dumps are not written.  Another
+ * current device than the handle's is refused (FP_ERR_INVALID_ARG).
  */
 fp_status fp_extend_workspace(const fp_layer* layer, const fp_paged_kv* kv, const fp_chunk* chunk, size_t* bytes);
 fp_status fp_extend(fp_layer* layer, const fp_paged_kv* kv, const fp_chunk* chunk, const void* x, void* y,

@@ -227,10 +227,6 @@ class Fingerprint:
                "fp_layer_create")
         self._h = h
         self.B = 0
-        self._device = None
-        if not unbacked:
-            import torch
-            self._device = torch.cuda.current_device()
 
     # lifetime ------------------------------------------------------------
     def close(self):
@@ -329,8 +325,6 @@ class Fingerprint:
             raise ValueError(f"{len(kvs)} paged caches for {self.shape.n_layers} layers")
         if any(kv.device != kvs[0].device or kv.page_size != kvs[0].page_size for kv in kvs):
             raise ValueError("the layers' pages must be on one device, of one size")
-        if self._device is not None and kvs[0].device.index != self._device:
-            raise ValueError(f"the pages are on {kvs[0].device}, the fingerprint on device {self._device}")
         return (_PagedKv * len(kvs))(*[kv.struct for kv in kvs])
 
     # blocks outside the hidden layers (vocab > 0) ------------------------

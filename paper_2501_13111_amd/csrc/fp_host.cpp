@@ -148,6 +148,7 @@ struct fp_layer {
     int wq = 0, kvq = 0;
     uint64_t seed = 0;
     bool unbacked = false;
+    int device = 0;               // that its storage is on
     int act_fmt = ACT_BF16;
     int q_dim = 0, kv_dim = 0, nqkv = 0;
     std::vector<LayerW> L;
@@ -1289,6 +1290,7 @@ static fp_status create_impl(const fp_shape* shape, fp_weight_quant wq, fp_kv_qu
         delete h;
         return fail(FP_ERR_UNSUPPORTED, "device %s is not gfx950", prop.gcnArchName);
     }
+    h->device = dev;
 
     auto bail = [&](fp_status code) {
         free_all(h);
@@ -1709,6 +1711,9 @@ fp_status fp_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, c
     if (!workspace || (uintptr_t)workspace % 16 != 0) return fail(FP_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device pointer");
     if (workspace_bytes < need) return fail(FP_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
     if (h->unbacked || chunk->n_rows == 0) return FP_OK;
+    int dev = 0;
+    HIPCHK(hipGetDevice(&dev));
+    if (dev != h->device) return fail(FP_ERR_INVALID_ARG, "the current device is %d, the fingerprint's %d", dev, h->device);
     return enqueue_extend(h, kv, *chunk, (const uint16_t*)x, (uint16_t*)y, (float*)workspace, (hipStream_t)stream);
 }
 
