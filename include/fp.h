@@ -321,8 +321,8 @@ fp_status fp_kv_read(const fp_paged_kv* kv, const fp_chunk* chunk, void* k_out, 
  * h * n_kv_heads / n_heads.  The chunk's own keys and values are read from the pages too:
  * append first.  q: device bf16, row r's head h at q + r * q_stride + h * head_dim; out: device
  * bf16 [n_rows, n_heads, head_dim]; both 16-byte aligned.  Query group n_heads / n_kv_heads from
- * 1 to 16.  Scores, softmax statistics and sums are fp32; probabilities enter the product with V as bf16
- * (int8 caches: fp16).  Keys and values that are NaN or infinite reach the rows that see them and no
+ * 1 to 16; scale below 2^127 in magnitude.  Scores, softmax statistics and sums are fp32; probabilities
+ * enter the product with V as bf16 (int8 caches: fp16).  Keys and values that are NaN or infinite reach the rows that see them and no
  * others.  bf16: values below 2^127 in magnitude over up to 2^24 positions cannot overflow the sums.  int8: keys
  * and values below 65504 in magnitude (calls of more than 64 rows per sequence and kv head unpack them to fp16).
  * workspace: device memory of at least fp_attn_chunk_workspace bytes, 16-byte aligned, which

@@ -164,7 +164,8 @@ fp_status fp_attn_chunk(const fp_paged_kv* kv, const fp_chunk* chunk, const void
     if ((s = check_rows("q", q, q_stride, qw)) || (s = check_rows("out", out, qw, qw))) return s;
     if (overlap(q, rows_bytes(chunk->n_rows, q_stride, qw), out, rows_bytes(chunk->n_rows, qw, qw)))
         return fail(FP_ERR_INVALID_ARG, "q and out overlap");
-    if (!std::isfinite(scale)) return fail(FP_ERR_INVALID_ARG, "scale is not finite");
+    // times log2 e it must stay finite
+    if (!(std::fabs(scale) < 0x1p127f)) return fail(FP_ERR_INVALID_ARG, "scale is not below 2^127 in magnitude");
     const size_t need = attn_chunk_ws_bytes(*kv, *chunk, n_heads);
     if (need > 0 && (!workspace || !aligned(workspace, 16))) return fail(FP_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device pointer");
     if (workspace_bytes < need) return fail(FP_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);

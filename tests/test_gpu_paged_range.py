@@ -54,3 +54,31 @@ def test_values_of_any_size(top, nkv, G, d, lens, loose):
     fp.attn_chunk(pool.device(), chunk, q.cuda(), out)
     assert torch.isfinite(out.float()).all()
     paged._check_attention(pool, table, lens, q, out)
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("nkv,G,new,loose", CALLS)
+def test_scales_of_any_size(nkv, G, new, loose, kvq):
+    """The largest scales, with queries of zeros (whose scores are zero) and queries whose scores lie some hundred
+    apart; beyond 2^127 the scale to base 2 would pass fp32's largest number, and is refused."""
+    fp = paged._fp()
+    d, page, lens = 128, 64, [(900, new), (70, new)]
+    g, pool, table = paged._case(lens, page, nkv, d, kvq, 175)
+    paged._fill(pool, table, lens, g, upto=lambda c, n: c + n)
+    chunk, starts = paged._chunk(lens, table, loose=loose)
+    q = 2.0 ** -123 * torch.randn(starts[-1], nkv * G, d, generator=g)
+    q[::3] = 0
+    q = q.bfloat16()
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    # int8: a probability (streamed: times its value's scale) enters the product as fp16, where it is off by up to 2^-25
+    # however small it is.  The row's largest is held at 2^7 or more (streamed: 2^7 over the largest scale) and the quotient's
+    # lower side is at least that: 2^-32 of the largest value for each key
+    n = max(c + m for c, m in lens)
+    floor = 2.0 ** -32 * n * max(float(pool.read(table[b], c + m)[1].abs().max()) for b, (c, m) in enumerate(lens)) * 1.01
+    floor = floor if kvq == "int8" else 0.0
+    for scale in (2.0 ** 127 * (1 - 2.0 ** -24), -2.0 ** 126):
+        fp.attn_chunk(pool.device(), chunk, q.cuda(), out, scale=scale)
+        paged._check_attention(pool, table, lens, q, out, scale, fp16=kvq == "int8" and bool(loose), floor=floor)
+    for scale in (2.0 ** 127, -3.3e38):
+        with pytest.raises(fp.FpError):
+            fp.attn_chunk(pool.device(), chunk, q.cuda(), out, scale=scale)
