@@ -277,7 +277,7 @@ typedef struct {
  *   n_rows   rows of the row buffers; rows from row_start[n_seqs] on belong to no sequence
  *            and are left as they are
  *   max_new  bound on a sequence's rows
- *   max_len  bound on ctx_len[b] + rows of b, at most table_stride * page_size
+ *   max_len  bound on ctx_len[b] + rows of b, at most table_stride * page_size and 2^31 - 1024
  * The bounds size the launches (tight ones are faster).  Contents that break them, or a page
  * number outside [0, n_pages), are no error and touch no memory outside the buffers: rows
  * beyond max_new are not computed, positions from max_len on are neither written nor read,

@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(T) kv_append_paged_kernel(KvAppendArgs a) {
     const int t0 = max(sq.ctx - blk * VT_BLK, 0), t1 = min(sq.len - blk * VT_BLK, VT_BLK);   // live positions
     const int np = t1 - t0;
     const int pb = pool_block(a.kv, a.chunk, b, kvh, blk);
-    const int row0 = sq.row0 + blk * VT_BLK + t0 - sq.ctx;
+    const int row0 = sq.row0 + (blk * VT_BLK + t0 - sq.ctx);
     const int G = a.q != nullptr ? a.n_heads / a.kv.n_kv_heads : 0;
 
     for (int it = tid; it < (2 + G) * np * NP; it += T) {
@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(T) kv_read_paged_kernel(KvReadArgs a) {
     const int t0 = max(sq.ctx - blk * VT_BLK, 0), t1 = min(sq.len - blk * VT_BLK, VT_BLK);
     const int np = t1 - t0;
     const int pb = pool_block(a.kv, a.chunk, b, kvh, blk);
-    const int64_t row0 = sq.row0 + blk * VT_BLK + t0 - sq.ctx;
+    const int64_t row0 = sq.row0 + (blk * VT_BLK + t0 - sq.ctx);
     const int64_t prow = (int64_t)pb * VT_BLK;
     if (pb >= 0) {
         const u32x4* src = (const u32x4*)((const char*)a.kv.v + (int64_t)pb * D * VT_BLK * ES);

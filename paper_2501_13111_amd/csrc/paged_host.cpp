@@ -26,6 +26,9 @@ fp_status done(hipError_t e, const char* what) {
     return e == hipSuccess ? FP_OK : fail(FP_ERR_HIP, "%s launch failed: %s", what, hipGetErrorString(e));
 }
 
+// Kernels count positions in int32, up to a few blocks past a sequence's last.
+constexpr int MAX_POSITIONS = INT32_MAX - 1023;
+
 fp_status check_shape(const fp_paged_kv* kv, const fp_chunk* c) {
     if (!kv || !c) return fail(FP_ERR_INVALID_ARG, "kv and chunk must not be NULL");
     if (kv->format != FP_KV_BF16 && kv->format != FP_KV_INT8)
@@ -45,6 +48,7 @@ fp_status check_shape(const fp_paged_kv* kv, const fp_chunk* c) {
     if (c->n_rows > 1 << 24) return fail(FP_ERR_UNSUPPORTED, "n_rows %d > 2^24", c->n_rows);
     if (c->max_len > (int64_t)c->table_stride * kv->page_size)
         return fail(FP_ERR_CAPACITY, "max_len %d passes the table's %d pages of %d", c->max_len, c->table_stride, kv->page_size);
+    if (c->max_len > MAX_POSITIONS) return fail(FP_ERR_UNSUPPORTED, "max_len %d > %d", c->max_len, MAX_POSITIONS);
     return FP_OK;
 }
 

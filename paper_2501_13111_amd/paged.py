@@ -14,6 +14,7 @@ import torch
 from .binding import KVQ, _check, load
 
 VT_BLK = 32      # positions per transposed block of values
+MAX_POSITIONS = 2**31 - 1024     # the largest max_len
 
 
 class _PagedKv(ctypes.Structure):
@@ -154,7 +155,7 @@ class Chunk(_Fixed):
         if c is None:
             if len(self._c) >= 32:
                 self._c.clear()
-            max_len = self.max_len if self.max_len is not None else min(self.width * kv.page_size, 2**31 - 1)
+            max_len = self.max_len if self.max_len is not None else min(self.width * kv.page_size, MAX_POSITIONS)
             c = self._c[key] = ctypes.byref(_Chunk(self.n_seqs, n_rows, self.max_new, max_len, self.width, *self._p))
         return c
 

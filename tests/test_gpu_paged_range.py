@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+import paged_reference as ref
 import test_gpu_paged as paged
 
 pytestmark = pytest.mark.gpu
@@ -82,3 +83,51 @@ def test_scales_of_any_size(nkv, G, new, loose, kvq):
     for scale in (2.0 ** 127, -3.3e38):
         with pytest.raises(fp.FpError):
             fp.attn_chunk(pool.device(), chunk, q.cuda(), out, scale=scale)
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("d,new", [(64, 1), (64, 70), (128, 300)])
+def test_the_longest_sequence(d, new, kvq):
+    """A sequence of the most positions that a call takes, nearly all of them in one shared page whose scores are far
+    below those of the last page; what lies behind its end is NaN."""
+    fp = paged._fp()
+    page, length = 65536, 2 ** 31 - 1024
+    last = length - 32767 * page                       # positions in the last page
+    pool = ref.Pool(2, page, 1, d, kvq)
+    g = torch.Generator().manual_seed(177)
+    two = torch.tensor([0, 1], dtype=torch.int32)
+    pool.write(two, torch.arange(page), torch.full((page, 1, d), -8.0), torch.full((page, 1, d), 5.0))
+    k, v = (torch.randn(last, 1, d, generator=g).bfloat16().float() for _ in range(2))
+    pool.write(two, page + torch.arange(last), k, v)
+    table = torch.zeros(1, 32768, dtype=torch.int32)
+    table[0, -1] = 1
+    kv = pool.device()
+    chunk = fp.Chunk(torch.tensor([0, new], dtype=torch.int32).cuda(), torch.tensor([length - new], dtype=torch.int32).cuda(),
+                     table.cuda(), max_new=new)
+    q = (1 + 0.25 * torch.rand(new, 2, d, generator=g)).bfloat16()
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+    fp.attn_chunk(kv, chunk, q.cuda(), out)
+    # the shared page's scores are below -8 sqrt(d), the last page's largest above 0: 2^31 times e^-64 is nothing
+    kd, vd = (t[page:, 0].cuda() for t in pool.read(two, page + last))
+    seen = last - new + 1 + torch.arange(new, device="cuda")
+    for h in range(2):
+        s = q[:, h].cuda().double() @ kd.t().contiguous() / math.sqrt(d)
+        s.masked_fill_(torch.arange(last, device="cuda")[None, :] >= seen[:, None], -math.inf)
+        p = torch.softmax(s, -1)
+        want, mag = p @ vd, p @ vd.abs()
+        err = (out[:, h].double() - want).abs()
+        # roundings of the output and the probabilities; int8 in tiles of 256 rows: keys and values in fp16, a key's share of
+        # the score on both sides of the quotient; fp32 scores and sums below 1e-3
+        smag = float((q[:, h].cuda().double().abs() @ kd.abs().t().contiguous()).max()) / math.sqrt(d)
+        f16 = 2.0 ** -11 * (1 + 2 * smag) if kvq == "int8" else 0.0
+        assert (err <= paged.HALF_BF16 * want.abs() + (paged.HALF_BF16 + f16 + 1e-3) * mag * 1.01).all()
+    # the rows' own positions, written and read back across the last blocks
+    rows = torch.randn(new, 1, d, generator=g).bfloat16().cuda()
+    fp.kv_append(kv, chunk, rows, rows)
+    ko, vo = torch.empty_like(rows), torch.empty_like(rows)
+    fp.kv_read(kv, chunk, ko, vo)
+    want = rows
+    if kvq == "int8":
+        code, scale = ref.quantise(rows.float().cpu())
+        want = (code.float() * scale.float()[..., None]).bfloat16().cuda()
+    assert torch.equal(ko, want) and torch.equal(vo, want)

@@ -9,3 +9,14 @@ from test_paged_cpu import CAPACITY, INVALID, UNSUPPORTED, append, attn, chunk, 
 def test_scales(lib, scale, code):  # noqa: F811
     # no rows: a call that is accepted launches nothing
     assert attn(lib, kv(), chunk(n_rows=0), scale=scale) == code
+
+
+@pytest.mark.parametrize("entry", [append, read, attn])
+def test_positions_up_to_the_end_of_32_bits(lib, entry):  # noqa: F811
+    """The kernels count positions up to a few blocks past a sequence's end."""
+    wide = dict(n_rows=0, table_stride=32768)
+    pool = kv(page_size=65536)
+    assert entry(lib, pool, chunk(max_len=2**31 - 1, **wide)) == UNSUPPORTED
+    assert entry(lib, pool, chunk(max_len=2**31 - 1023, **wide)) == UNSUPPORTED
+    assert entry(lib, pool, chunk(max_len=2**31 - 1024, **wide)) == 0
+    assert entry(lib, pool, chunk(max_len=2**31 - 1024, **dict(wide, table_stride=32767))) == CAPACITY

@@ -74,3 +74,11 @@ def test_a_paged_cache_does_not_change_under_its_calls(dtype):
     assert bytes(kv.struct) == before and all(a is b for a, b in zip(held, [kv.k, kv.v, kv.k_scales, kv.v_scales]))
     kv.k += 1                                          # contents may change
     assert kv.struct.k == kv.k.data_ptr()
+
+
+def test_a_chunks_default_bound_is_one_that_the_entries_take():
+    kv = fp.PagedKV(dev(torch.zeros(1, 1, 65536, 64, dtype=torch.int8)), dev(torch.zeros(1, 1, 2048, 64, 32, dtype=torch.int8)),
+                    *[dev(torch.zeros(1, 1, 65536, dtype=torch.float16)) for _ in range(2)])
+    i = dev(torch.zeros(2, dtype=torch.int32))
+    c = fp.Chunk(i, i[:1], dev(torch.zeros(1, 40000, dtype=torch.int32)), max_new=1)
+    assert struct(c, kv, 1).max_len == 2**31 - 1024
