@@ -26,8 +26,6 @@
 // rate of a large copy), 24 rows 53, 48 rows 70; int8 31, 37, 68.  One sequence of 331 positions, 32 kv heads: 9.7 us, of
 // which 1.4 are the plan, 1.3 the first loads, 4 three blocks a wave and 1.8 the merge (a chain of memory latencies
 // and of code fetched for the first time: a second copy of the block's code cost 1 us).
-#include <climits>
-
 #include "attn_stream.h"
 
 namespace fpk {
@@ -217,14 +215,16 @@ size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads
 template <int D, bool KV8, int RT>
 static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
-    const int64_t tiles = std::min<int64_t>((int64_t)a.chunk.n_rows * G, (int64_t)a.chunk.n_rows * G / RT + a.chunk.n_seqs) * nkv;
+    // rows that sequences own, which may be few of a padded batch's
+    const int64_t R = std::min<int64_t>(a.chunk.n_rows, (int64_t)a.chunk.n_seqs * a.chunk.max_new) * G;
+    const int64_t tiles = std::min(R, R / RT + a.chunk.n_seqs) * nkv;
     a.target = piece_target(RT, D);
     a.min_blocks = piece_min(RT);
     a.over = 10;
     a.join = 8;
     a.plan = (int*)(a.ws + 2 * piece_aim(RT, D) * RT * wst(D));
     const int64_t pieces = piece_aim(RT, D), n = std::max(tiles + pieces, 2 * pieces) + 16 * XCD_RUN;
-    if (n > INT_MAX) return hipErrorInvalidValue;
+    if (n > MAX_GRID) return hipErrorInvalidValue;
     // tiles that can be split: each has more than Q of the blocks
     const unsigned split = (a.chunk.max_len - 1) / VT_BLK < WHOLE<RT> ? 0u : (unsigned)std::min<int64_t>(tiles, pieces);
     if (a.chunk.n_seqs > PLAN_LANES) {

@@ -259,6 +259,9 @@ int head_logit_blocks(int V);
 hipError_t launch_logits_argmax(const float* part, int ks, int B, int V, float* logits, float* bval, int* bidx,
                                 int* out_ids, hipStream_t st);
 
+// Workgroups of 256 in one launch, whose threads count in 32 bits.
+constexpr int64_t MAX_GRID = UINT32_MAX / 256;
+
 // Paged cache (paged.hip).  ks fp32 partials pstride apart are summed by the append when its
 // launch says f32 (the layer stack's own qkv projection), else inputs are bf16.
 struct KvAppendArgs {

@@ -273,7 +273,7 @@ int64_t max_blocks(const fp_chunk& c) { return blocks_before(c.n_rows, c.n_seqs)
 
 hipError_t launch_kv_append(const KvAppendArgs& a, bool f32, hipStream_t st) {
     const int64_t n = (max_blocks(a.chunk) + 7) / 8 * 8 * a.kv.n_kv_heads;
-    if (n < 1 || n > INT_MAX) return hipErrorInvalidValue;
+    if (n < 1 || n > MAX_GRID) return hipErrorInvalidValue;
     const bool i8 = a.kv.format == FP_KV_INT8;
 #define FP_AP(D, I8, F32) FP_LAUNCH((kv_append_paged_kernel<D, I8, F32>), dim3((unsigned)n), dim3(T), 0, st, a)
 #define FP_AP_D(D)                                                                   \
@@ -291,7 +291,7 @@ hipError_t launch_kv_append(const KvAppendArgs& a, bool f32, hipStream_t st) {
 
 hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st) {
     const int64_t n = (max_blocks(a.chunk) + 7) / 8 * 8 * a.kv.n_kv_heads;
-    if (n < 1 || n > INT_MAX) return hipErrorInvalidValue;
+    if (n < 1 || n > MAX_GRID) return hipErrorInvalidValue;
     const dim3 grid((unsigned)n);
     const bool i8 = a.kv.format == FP_KV_INT8;
     if (a.kv.head_dim == 128) {

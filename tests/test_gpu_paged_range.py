@@ -131,3 +131,25 @@ def test_the_longest_sequence(d, new, kvq):
         code, scale = ref.quantise(rows.float().cpu())
         want = (code.float() * scale.float()[..., None]).bfloat16().cuda()
     assert torch.equal(ko, want) and torch.equal(vo, want)
+
+
+def test_rows_of_the_widest_buffer():
+    """Two sequences' next tokens in row buffers of 2^24 rows: the launch goes by the rows that they can own."""
+    fp = paged._fp()
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("needs 70 GB")
+    nkv, G, d, lens = 8, 2, 64, [(200, 1), (31, 1)]
+    kv, table, g = paged._fill_gpu(lens, 64, nkv, d, "bf16", 179)
+    chunk, starts = paged._chunk(lens, table)
+    q = torch.empty(1 << 24, nkv * G, d, dtype=torch.bfloat16, device="cuda")
+    out = torch.empty_like(q)
+    q[:2] = torch.randn(2, nkv * G, d, generator=g, device="cuda").bfloat16()
+    out[:4] = 7.0
+    out[-1] = 7.0
+    fp.attn_chunk(kv, chunk, q, out)
+    want, mag = paged._gpu_attention(kv, table, lens, q[:2])
+    got, untouched = out[:2].double(), (out[2:4] == 7.0).all() and (out[-1] == 7.0).all()
+    del q, out
+    torch.cuda.empty_cache()
+    assert ((got - want).abs() <= paged.HALF_BF16 * want.abs() + (paged.HALF_BF16 + 1e-4) * mag * 1.01).all()
+    assert untouched
