@@ -173,8 +173,8 @@ __global__ void __launch_bounds__(256) attn_chunk_join_kernel(AttnChunkArgs a) {
 // they can see.  us at (new tokens after context), 8 heads a kv head, unless said otherwise.
 //   More than 64 rows: tiles of 256, where the matrix cores bound, once they fill the GPU and their longer start pays.
 // Streamed and in tiles of 256:
-//     d 128, bf16   up to 2^13: 512 after 0 21, 34; 512 after 512 32, 35    above: 1024 after 0 61, 49; 1024 after 31744 831, 521
-//     d 64, bf16    up to 2^15: 1024 after 0 32, 35; 128 after 16000 40, 46    above: 2048 after 0 74, 63; 1024 after 31744 402, 375
+//     d 128, bf16   up to 2^13: 512 after 0 21, 34; 512 after 512 32, 35    above: 1024 after 0 61, 47; 1024 after 31744 832, 523
+//     d 64, bf16    up to 2^15: 1024 after 0 32, 35; 128 after 16000 40, 46    above: 2048 after 0 71, 60; 1024 after 31744 391, 360
 //     d 64, int8    always: 512 after 0 14, 33; 2048 after 0 77, 83; 8 sequences of 2048 after 2000 505, 551; 1024 after
 //                   31744 554, 523 (the tiles' unpacking costs as much as their products)
 //   Streamed, more than 32 rows: tiles of 64 read the cache once for them all, tiles of 32 start and end sooner and
@@ -198,7 +198,7 @@ int tile_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
 // worth a piece
 int piece_target(int RT, int D) { return RT == TILE_ROWS || (RT == 64 && D == 128) ? 8 : 9; }
 int piece_min(int RT) { return RT == TILE_ROWS ? 8 : 16; }
-// the most pieces that a call aims for (plan_q)
+// the most pieces that a call aims for (plan_one, plan_all)
 int64_t piece_aim(int RT, int D) { return (int64_t)1 << (piece_target(RT, D) + (RT < 64 ? 1 : 0)); }
 
 }  // namespace

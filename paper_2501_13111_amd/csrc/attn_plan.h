@@ -56,7 +56,7 @@ __device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int Q) {
 template <int RT>
 __device__ __forceinline__ int plan_one(const AttnChunkArgs& a, const Seq& s, int G) {
     const Plan p = plan_seq<RT>(s, G, 1);
-    const int tiles = std::max(1, p.tiles * a.kv.n_kv_heads);        // above 2^31 the launch is refused
+    const int tiles = std::max(1, p.tiles * a.kv.n_kv_heads);        // above MAX_GRID the launch is refused
     int best = std::max(1, p.blocks), cost = ((tiles - 1 >> a.target) + 1) * (p.blocks + a.over);
     for (int k = 0; k < 2; ++k) {
         const int cut = std::min((1 << (a.target + k)) / tiles, p.blocks / a.min_blocks);

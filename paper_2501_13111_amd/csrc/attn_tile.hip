@@ -24,9 +24,9 @@
 // scale); queries are fp16 too, each row brought to the top of its range by a power of two that the scale takes
 // back, so that only elements 2^-29 of the row's largest and smaller lose bits.
 //
-// 1024 tokens after 31744, 32 heads on 4 of 128: bf16 555 us, 0.98 PFLOP/s of the 1.31 that a large library matrix
-// product reaches; int8 640, 0.83 (its unpacking takes the instructions that the longer trip shows); heads of 64, bf16
-// 375, 0.72 (half the products, the same softmax).  A trip of 36 products is 1152 cycles of matrix core and takes some
+// 1024 tokens after 31744, 32 heads on 4 of 128, in a loop of 20 calls: bf16 523 us, 1.03 PFLOP/s of the 1.31 that a
+// large library matrix product reaches; int8 633, 0.85 (its unpacking takes the instructions that the longer trip
+// shows); heads of 64, bf16 360, 0.75 (half the products, the same softmax).  A trip of 36 products is 1152 cycles of matrix core and takes some
 // 2000 (int8 2600).  A unit's fixed part is 6 us before the first trip (the plan 1.5, the rest the first blocks and
 // queries at the memory's rate when every unit starts at once) and 2.5 after the last.
 #include <type_traits>

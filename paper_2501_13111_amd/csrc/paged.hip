@@ -7,8 +7,8 @@
 // with; the 8 (d = 64: 4) threads of a position find its largest magnitude by shuffles.  In an
 // append the workgroup also rotates the queries of its kv head's group for the block's positions,
 // whose cosines and sines it has just read.  Bound by memory: a long chunk's rows move once in, once
-// out.  Appending 16 chunks of up to 4096, 32 heads on 8 of 128, bf16 (1.2 GB): 276 us, 4.9 TB/s; 64 single tokens, 64 heads on 8,
-// int8: 6.5 us, a chain of latencies.  Reading 8 sequences of up to 16000 back, 8 heads of 128, int8 (473 MB): 97 us, 4.9 TB/s.
+// out.  Appending 16 chunks of up to 4096, 32 heads on 8 of 128, bf16 (40,604 rows, 1.02 GB): 214 us, 4.8 TB/s; 64 single tokens on
+// 8 heads, int8: 6.2 us, a chain of latencies.  Reading 8 sequences of up to 16000 back, 8 heads of 128, int8 (473 MB): 97 us, 4.9 TB/s.
 #include "paged.h"
 
 namespace fpk {
@@ -90,8 +90,7 @@ __device__ __forceinline__ u32x2 codes8(const float (&x)[8], float s) {
     return u32x2{w[0], w[1]};
 }
 
-// contraction off: products and sums are rounded one by one, as the definition's fp32 says
-#pragma clang fp contract(off)
+// rotate_pair rounds one product and fuses the other with the sum, whatever the compiler contracts
 __device__ __forceinline__ void rotate8(float (&lo)[8], float (&hi)[8], const float* c, const float* s) {
     const f32x4 c0 = *(const f32x4*)c, c1 = *(const f32x4*)(c + 4), s0 = *(const f32x4*)s, s1 = *(const f32x4*)(s + 4);
 #pragma unroll
@@ -196,7 +195,6 @@ __global__ void __launch_bounds__(T, KV8 && !F32 ? 8 : 1) kv_append_paged_kernel
         }
     }
 }
-#pragma clang fp contract(on)
 
 template <int D, bool KV8>
 __global__ void __launch_bounds__(T) kv_read_paged_kernel(KvReadArgs a) {
