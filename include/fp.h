@@ -296,7 +296,7 @@ typedef struct {
  * k + r * kv_stride + h * head_dim (the stride in elements, so that k and v may be columns of
  * one fused projection).  FP_KV_INT8: s = fp16(absmax / 127), code = rint(x / s) clamped to
  * +-127 per (position, kv head), in fp32 with ties to even; a zero scale gives zero codes.  A NaN, an
- * infinity or an absmax beyond 127 * 65504 leaves a scale that is not finite: that position and head reads
+ * infinity or an absmax of 127 * 65520 and more leaves a scale that is not finite: that position and head reads
  * back as NaN throughout, and so do the rows of an attention that see it.
  * With cos and sin (device fp32 [n_pos, head_dim / 2], n_pos >= max_len; both or neither)
  * keys are first rotated by their position (rotate-half: i pairs with i + d / 2), in fp32.
