@@ -382,6 +382,91 @@ fp_status fp_verify_draft(const float* logits, int64_t row_stride, int32_t n_seq
                           int32_t* out_ids, int32_t* n_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Drafted trees.  Several continuations of a sequence can be checked in one call: its rows are then nodes,
+ * row i (at position ctx_len + i of the cache) the child of row parent[row i] of the same sequence.  parent: device int32
+ * [n_rows], indices within the sequence; one that is no earlier row of it (-1, say) is none: the node follows the context.
+ * A node sees the context, its ancestors and itself, and is rotated by ctx_len + its depth.  Sequences have up to 64
+ * nodes: max_new above 64 is refused (FP_ERR_UNSUPPORTED).  The rest is as for chunks: a call takes parent's contents when
+ * its kernels run.
+ *
+ * fp_kv_append_tree, fp_attn_tree and fp_extend_tree are fp_kv_append, fp_attn_chunk and fp_extend for such rows;
+ * workspaces are those of fp_attn_chunk_workspace and fp_extend_workspace.  Without cos and sin an append does not
+ * depend on parent.  In a tree that is one line, node i the child of node i - 1, results are those of the chunk's calls.
+ */
+fp_status fp_kv_append_tree(const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* k, const void* v,
+                            int64_t kv_stride, const void* q, int64_t q_stride, int32_t n_heads, void* q_out,
+                            const float* cos_t, const float* sin_t, int32_t n_pos, void* stream);
+fp_status fp_attn_tree(const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* q, int64_t q_stride,
+                       int32_t n_heads, float scale, void* out, void* workspace, size_t workspace_bytes, void* stream);
+fp_status fp_extend_tree(fp_layer* layer, const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* x, void* y,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Decide over drafted trees.  Node 0 of a sequence is its root, the last token that is certain; node_ids[row i] (device
+ * int32 [n_rows], the root's is not read) is the token that node i holds, and row i of logits (fp32 [n_rows, vocab],
+ * row_stride elements apart) gives the distribution p_i = softmax(logits / temperature) of the token after it.  A token
+ * y_i is drawn from each p_i: the lowest id whose running sum exceeds u[row i] times the total (u uniform in [0, 1), the
+ * caller's; temperature 0: the argmax, the lowest id among equal ones, u is not read and may be NULL).  From the
+ * root on, the first child that holds its parent's y is accepted, and the first node without such a child ends the path.
+ * The tokens y along it are those that the target alone would have drawn, whatever the tree.  Sums and comparisons are in 64 bits.
+ * out_ids: device int32 [n_seqs, max_rows], sequence b's accepted tokens and then the last draw, -1 behind; path: the same
+ * shape, the nodes of the path from the root (0) on, -1 behind; n_out: device int32 [n_seqs], the number of either (a
+ * sequence without rows: 0).  fp_kv_keep takes path and n_out as they are, and ctx_len grows by n_out.
+ * Logits, row_start and the limits are as for fp_verify_draft; a row without any probability draws -1, which no child holds.
+ */
+fp_status fp_verify_tree_workspace(int32_t n_seqs, int32_t n_rows, int32_t vocab, size_t* bytes);
+fp_status fp_verify_tree(const float* logits, int64_t row_stride, int32_t n_seqs, int32_t n_rows, int32_t max_rows, int32_t vocab,
+                         const int32_t* row_start, const int32_t* parent, const int32_t* node_ids, const float* u,
+                         float temperature, int32_t* out_ids, int32_t* path, int32_t* n_out, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
+ * Keep a path of a tree: in each of n_layers caches (kv: host array; pages of one geometry, formats of their own)
+ * position ctx_len[b] + path[b * path_stride + j] of sequence b moves to position ctx_len[b] + j, for j < n_keep[b].
+ * Keys are not rotated again: node j of a path is at depth j already.  path entries are nodes of the sequence, in any order
+ * (all are read before any is written); a negative one, or one past its rows, leaves its position as it is, and so do j from
+ * path_stride or the sequence's rows on.  chunk: that of the append (max_new up to 64), read when the kernel runs: ctx_len
+ * grows afterwards.
+ */
+fp_status fp_kv_keep(const fp_paged_kv* kv, int32_t n_layers, const fp_chunk* chunk, const int32_t* path, int32_t path_stride,
+                     const int32_t* n_keep, void* stream);
+
+/*
+ * Beam search's selection.  Group g has n_beams beams, row g * n_beams + b of logits (fp32, row_stride elements apart)
+ * and of scores (fp32) belonging to its beam b.  The continuation of beam b by id v scores
+ *   scores[b] + logits[b, v] - log sum_v exp(logits[b, v]),
+ * a finished beam (finished: NULL or device uint8, not 0) has the one continuation pad_id, which scores scores[b].
+ * The n_best best of a group, in order (the larger score; of equal ones the lower beam, in it the larger logit, then the
+ * lower id), go to out_scores (fp32), out_parent (int32, the beam), out_ids (int32) and, unless NULL, out_finished (uint8: its beam was
+ * finished or its id is eos_id; eos_id -1: no id is), all [n_groups, n_best]; where there are fewer, -inf, -1, -1 and 0.
+ * Sums and comparisons are in 64 bits.  -inf and NaN logits are no continuation, +inf ones share the whole; a beam of
+ * score -inf or NaN has none.  With n_beams 1 and n_best the beams to come, a request's first step.
+ * 1 <= n_beams, n_best <= 64, n_groups * n_beams <= 65535, 1 <= vocab <= 2^20.  Outputs do not overlap inputs.
+ */
+fp_status fp_beam_select_workspace(int32_t n_groups, int32_t n_beams, int32_t n_best, int32_t vocab, size_t* bytes);
+fp_status fp_beam_select(const float* logits, int64_t row_stride, int32_t n_groups, int32_t n_beams, int32_t n_best, int32_t vocab,
+                         const float* scores, const uint8_t* finished, int32_t eos_id, int32_t pad_id, float* out_scores,
+                         int32_t* out_parent, int32_t* out_ids, uint8_t* out_finished, void* workspace, size_t workspace_bytes,
+                         void* stream);
+
+/*
+ * Beams go on from other beams' caches: beam b of a group from beam parent[b] (device int32 [n_groups, n_beams]; out of
+ * range: from itself).  table: device int32, row g * n_beams + b the pages of beam b of group g; ctx_len: device int32 [n_groups * n_beams],
+ * of which a group's first is read: its beams have one length.  Row b of table_out (table itself, or apart from it):
+ *   full pages        those of parent[b]: they are shared from then on, and nothing writes them any more;
+ *   the last page     if it is partly filled, parent[b]'s for the first of the beams that go on from it; the others take, in
+ *                     order, the last pages of the beams that none goes on from, and parent[b]'s page is copied there
+ *                     in each of the n_layers caches (kv: host array; one geometry, formats of their own);
+ *   pages behind      row b's own.
+ * So a group's last pages and those behind stay its own, one each a beam, and nothing is allocated; full pages that no row
+ * names any more are the caller's to use again.  Before the call the last pages of a group's rows are different pages.
+ * A missing page is as for chunks.  Limits as for fp_beam_select; width pages a row, table_stride and out_stride apart.
+ */
+fp_status fp_beam_reorder(const fp_paged_kv* kv, int32_t n_layers, int32_t n_groups, int32_t n_beams, const int32_t* table,
+                          int32_t table_stride, int32_t width, const int32_t* ctx_len, const int32_t* parent,
+                          int32_t* table_out, int32_t out_stride, void* stream);
+
+/*
  * Latency and memory estimation from fingerprints (host arithmetic, no device).
  *
  * Eq. 1 (Sec. 5.3): latency = TTFT + output_length * TPOT.  fp_fit_ttft_tpot solves the

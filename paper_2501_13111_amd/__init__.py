@@ -7,6 +7,8 @@ from .binding import Fingerprint, FpShape, FpError, fill_normal, load, lib_path 
 try:
     from .paged import (Chunk, PagedKV, attn_chunk, attn_chunk_workspace, kv_append, kv_read,  # noqa: F401
                         verify_draft, verify_draft_workspace)
+    from .branches import (attn_tree, beam_reorder, beam_select, beam_select_workspace, kv_keep,  # noqa: F401
+                           verify_tree, verify_tree_workspace)
 except ModuleNotFoundError as e:
     if e.name != "torch":
         raise

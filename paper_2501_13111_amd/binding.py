@@ -107,6 +107,15 @@ def load(path: str | None = None):
         "fp_attn_chunk": [vp, vp, vp, i64, i32, ctypes.c_float, vp, vp, ctypes.c_size_t, vp],
         "fp_extend_workspace": [vp, vp, vp, ctypes.POINTER(ctypes.c_size_t)],
         "fp_extend": [vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
+        "fp_kv_append_tree": [vp, vp, vp, vp, vp, i64, vp, i64, i32, vp, vp, vp, i32, vp],
+        "fp_attn_tree": [vp, vp, vp, vp, i64, i32, ctypes.c_float, vp, vp, ctypes.c_size_t, vp],
+        "fp_extend_tree": [vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
+        "fp_verify_tree_workspace": [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
+        "fp_verify_tree": [vp, i64, i32, i32, i32, i32, vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, ctypes.c_size_t, vp],
+        "fp_kv_keep": [vp, i32, vp, vp, i32, vp, vp],
+        "fp_beam_select_workspace": [i32, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
+        "fp_beam_select": [vp, i64, i32, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp],
+        "fp_beam_reorder": [vp, i32, i32, i32, vp, i32, i32, vp, vp, vp, i32, vp],
         "fp_verify_draft_workspace": [i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)],
         "fp_verify_draft": [vp, i64, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, ctypes.c_float, vp, vp, vp,
                             ctypes.c_size_t, vp],
@@ -296,8 +305,9 @@ class Fingerprint:
                "fp_extend_workspace")
         return torch.empty(max(n.value, 16), dtype=torch.uint8, device=kvs[0].device)
 
-    def extend(self, kvs, chunk, x, y, workspace=None, stream=None):
-        """The layer stack over a chunk's rows: x, y bf16 [rows, hidden], kvs one PagedKV per layer.
+    def extend(self, kvs, chunk, x, y, workspace=None, stream=None, parent=None):
+        """The layer stack over a chunk's rows: x, y bf16 [rows, hidden], kvs one PagedKV per layer.  With parent
+        (int32 [rows]) the rows are nodes of drafted trees, as for ``attn_tree``.
         Without a workspace the call takes one from torch's allocator, on the current stream, so it
         refuses another `stream` then."""
         import torch
@@ -314,7 +324,12 @@ class Fingerprint:
                 raise ValueError("another stream than the current one needs a workspace of its own")
             workspace = self.extend_workspace(kvs, chunk, N)
         wp = _tensor(workspace, torch.uint8, "workspace", device=dev)
+        if parent is not None:
+            pp = _tensor(parent, torch.int32, "parent", (N,), device=dev)
         if N == 0:
+            return
+        if parent is not None:
+            _call("fp_extend_tree", dev, stream, self._h, self._pages(kvs), chunk.c(kvs[0], N), pp, xp, yp, wp, workspace.numel())
             return
         _call("fp_extend", dev, stream, self._h, self._pages(kvs), chunk.c(kvs[0], N), xp, yp, wp, workspace.numel())
 

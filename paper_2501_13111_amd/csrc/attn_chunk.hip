@@ -32,12 +32,12 @@ namespace fpk {
 
 namespace {
 
-template <int D, bool KV8, int NT>
+template <int D, bool KV8, int NT, bool TREE>
 __global__ void __launch_bounds__(256, NT == 1 ? 3 : NT == 4 && D == 128 ? 1 : 2) attn_chunk_kernel(AttnChunkArgs a) {
-    __shared__ StreamLds<D, NT> lds;
+    __shared__ StreamLds<D, NT, TREE> lds;
     Unit un;
     if (!find_unit<16 * NT, false, false>(a, a.n_heads / a.kv.n_kv_heads, un)) return;
-    stream_unit<D, KV8, NT, false>(a, un, lds);
+    stream_unit<D, KV8, NT, false, TREE>(a, un, lds);
 }
 
 // The plan of more than 256 sequences (attn_plan.h), by one workgroup: PER sequences a thread, their sums and running
@@ -235,7 +235,8 @@ static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     if constexpr (RT == TILE_ROWS) {
         return launch_attn_tile(a, (unsigned)n, split, st);
     } else {
-        FP_LAUNCH((attn_chunk_kernel<D, KV8, RT / 16>), dim3((unsigned)n), dim3(256), 0, st, a);
+        if (a.parent != nullptr) FP_LAUNCH((attn_chunk_kernel<D, KV8, RT / 16, true>), dim3((unsigned)n), dim3(256), 0, st, a);
+        else FP_LAUNCH((attn_chunk_kernel<D, KV8, RT / 16, false>), dim3((unsigned)n), dim3(256), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || split == 0) return e;
         FP_LAUNCH((attn_chunk_join_kernel<D, RT>), dim3(split, RT * D / 1024), dim3(256), 0, st, a);

@@ -2,7 +2,7 @@
 #pragma once
 #include <algorithm>
 
-#include "paged.h"
+#include "tree.h"
 
 namespace fpk {
 
@@ -243,11 +243,13 @@ __device__ __forceinline__ uint32_t finite_halves(uint32_t w) {
 
 // Infinite and NaN values that some rows of a tile do not see would make NaN of their zero probabilities.
 // The kernels take them out of the products; this is what they are to a row that sees them: the sum of those of
-// dim d at positions first .. last, 0 if there are none (rare, and not quick).
-template <int D, bool KV8>
-__device__ __forceinline__ float stray_sum(const AttnChunkArgs& a, int b, int kvh, int d, int first, int last) {
+// dim d at positions first .. last, 0 if there are none (rare, and not quick).  TREE: at those of them that a node
+// with this line sees.
+template <int D, bool KV8, bool TREE>
+__device__ __forceinline__ float stray_sum(const AttnChunkArgs& a, int b, int kvh, int d, int first, int last, int ctx, uint64_t line) {
     float sum = 0.f;
     for (int p = first; p <= last; ++p) {
+        if (TREE && p >= ctx && !(line >> (p - ctx) & 1)) continue;
         const int pb = pool_block(a.kv, a.chunk, b, kvh, p / VT_BLK), t = p % VT_BLK;
         if (pb < 0) continue;
         const int64_t at = ((int64_t)pb * D + d) * VT_BLK + vt_slot(t);

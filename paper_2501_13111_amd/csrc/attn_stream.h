@@ -44,17 +44,28 @@ __device__ __forceinline__ u32x4 i8x8_to_bf16(uint32_t lo, uint32_t hi) {
 }
 
 // LDS of a unit of 16 NT rows
-template <int D, int NT>
+template <int D, int NT, bool TREE>
 struct StreamLds {
     static constexpr int RT = 16 * NT, RS = D + 4;
     __attribute__((aligned(16))) float ow[4][RT * RS];
     float mw[4][RT], lw[4][RT];
     int sw[4];
 };
+template <int D, int NT>
+struct StreamLds<D, NT, true> : StreamLds<D, NT, false> {
+    uint64_t line[TREE_MAX];
+};
 
-// One unit of at most 16 NT rows.  TILE: its partial result is laid out as those of the 256-row tiles.
-template <int D, bool KV8, int NT, bool TILE>
-__device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& un, StreamLds<D, NT>& lds) {
+template <int D, int NT, bool TREE>
+__device__ __forceinline__ uint64_t lds_line(const StreamLds<D, NT, TREE>& lds, int node) {
+    if constexpr (TREE) return lds.line[node];
+    else return 0;
+}
+
+// One unit of at most 16 NT rows.  TILE: its partial result is laid out as those of the 256-row tiles.  TREE: rows are
+// nodes of a tree, which see the context and their line (tree.h); the causal mask of their positions, with holes.
+template <int D, bool KV8, int NT, bool TILE, bool TREE>
+__device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& un, StreamLds<D, NT, TREE>& lds) {
     constexpr int NJ = D / 32, ND = D / 16, RT = 16 * NT;
     constexpr int NK = Chunk<D, KV8>::NK;
     constexpr int RS = D + 4;
@@ -121,14 +132,21 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
     // queries: column c of tile t is row row0 + 16 t + c.  Columns past the last row see no position, so
     // what they hold does not matter.
     u32x4 qf[NT][NJ];
-    int lim[NT];                                 // last position that the lane's row sees
+    int lim[TREE ? 1 : NT];                      // last position that the lane's row sees
+    uint64_t line[TREE ? NT : 1];                // nodes that it sees
+    uint64_t mine = 0;                           // those of node `lane`
+    if constexpr (TREE) {
+        if (end * VT_BLK > sq.ctx) mine = tree_lines(a.parent, sq);
+        if (w == 0) lds.line[lane] = mine;
+    }
     const QScale qs = q_scale(a.scale);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int rho = row0 + 16 * t + r;
         const bool live = 16 * t + r < rows;
         const int tok = live ? rho / G : 0, h = live ? rho % G : 0;
-        lim[t] = live ? sq.ctx + tok : -1;
+        if constexpr (TREE) line[t] = __shfl(mine, tok, 64);
+        else lim[t] = live ? sq.ctx + tok : -1;
         const uint16_t* q = a.q + (int64_t)(sq.row0 + tok) * a.q_stride + (kvh * G + h) * D;
 #pragma unroll
         for (int j = 0; j < NJ; ++j) qf[t][j] = (*(const u32x4*)(q + qdim<KV8>(j, g)) ^ qs.sign) & qs.keep;
@@ -153,7 +171,7 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
     auto compute = [&](int i, int next) {
         const int base = (beg + w + 4 * i) * VT_BLK;
         float ksc[2][4], vsc[2][4], lk = SLACK + ROOM;       // lk: from the block's largest score to its reference
-        const bool edge = base + VT_BLK > sq.ctx + 1;        // some row may not see all of the block
+        const bool edge = base + VT_BLK > sq.ctx + (TREE ? 0 : 1);        // some row may not see all of the block
         // positions past the sequence hold anything: their values must not meet a zero probability (cleared before the
         // look for values that are not finite, which would take them for the sequence's)
         if (base + VT_BLK > sq.len) {
@@ -233,11 +251,17 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[t][e] = KV8 ? acc[e] * ksc[t][e] : acc[e];
             }
-            if (edge) {
+            if (TREE && edge) {
+                const uint32_t sees = tree_sees(line[TREE ? q : 0], base - sq.ctx) >> (4 * g);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[t][e] = base + 16 * t + 4 * g + e <= lim[q] ? s[t][e] : -INFINITY;
+                    for (int e = 0; e < 4; ++e) s[t][e] = sees >> (16 * t + e) & 1 ? s[t][e] : -INFINITY;
+            } else if (edge) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[t][e] = base + 16 * t + 4 * g + e <= lim[TREE ? 0 : q] ? s[t][e] : -INFINITY;
             }
             float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])),
                              fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
@@ -328,8 +352,8 @@ __device__ __forceinline__ void stream_unit(const AttnChunkArgs& a, const Unit& 
         if (sw[0] | sw[1] | sw[2] | sw[3]) {
 #pragma unroll 1
             for (int e = 0; e < 4; ++e) {
-                const float x = stray_sum<D, KV8>(a, b, kvh, d0 + e, max(beg, (sq.ctx + 1) / VT_BLK) * VT_BLK,
-                                                  min(sq.ctx + rho / G, end * VT_BLK - 1));
+                const float x = stray_sum<D, KV8, TREE>(a, b, kvh, d0 + e, max(beg, (sq.ctx + (TREE ? 0 : 1)) / VT_BLK) * VT_BLK,
+                                                        min(sq.ctx + rho / G, end * VT_BLK - 1), sq.ctx, lds_line(lds, rho / G));
                 o += f32x4{e == 0 ? x : 0.f, e == 1 ? x : 0.f, e == 2 ? x : 0.f, e == 3 ? x : 0.f};
             }
         }

@@ -59,7 +59,7 @@ __device__ __forceinline__ void static_for(F&& f) {
 __device__ __forceinline__ uint32_t pk_mul(uint32_t x, uint32_t y) {
     return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, x) * __builtin_bit_cast(f16x2, y));
 }
-template <int D, bool KV8>
+template <int D, bool KV8, bool TREE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) attn_tile_kernel(AttnChunkArgs a) {
     constexpr int NKC = D / 16, NDT = D / 32, NVC = 2 * NDT, CH = NKC + NVC;
     constexpr int SB = CH * 1024;          // bytes of a slot: keys, then values
@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     Unit un;
     if (!find_unit<TILE_ROWS, false, true>(a, G, un)) return;
     if (few_rows(un.sq, G)) {
-        stream_unit<D, KV8, 1, true>(a, un, *(StreamLds<D, 1>*)smem);
+        stream_unit<D, KV8, 1, true, TREE>(a, un, *(StreamLds<D, 1, TREE>*)smem);
         return;
     }
     const Seq& sq = un.sq;
@@ -83,11 +83,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     // blocks that this wave's rows see, and that all of them see whole
     const int wr0 = row0 + 64 * w, wrows = min(max(rows - 64 * w, 0), 64);
     const int nw = uni(wrows > 0 ? min(n, (sq.ctx + (wr0 + wrows - 1) / G) / VT_BLK + 1 - beg) : 0);
-    const int wfull = uni((sq.ctx + wr0 / G + 1) / VT_BLK - beg);
+    const int wfull = uni((TREE ? sq.ctx : sq.ctx + wr0 / G + 1) / VT_BLK - beg);
     // From block `edge` on some row of the tile does not see every key.  Values there that are not finite
     // would make NaN of its zero probabilities: they are taken out, and what they are to the rows that
     // do see them is written at the end.
-    const int edge = uni((sq.ctx + row0 / G + 1) / VT_BLK - beg);
+    const int edge = uni((TREE ? sq.ctx : sq.ctx + row0 / G + 1) / VT_BLK - beg);
     __shared__ int sw[4];
     bool strays = false;                   // this wave has taken some out
 
@@ -259,6 +259,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
     // ---- queries: columns 32 c + l % 32 of the wave; a negative scale turns their signs
     u32x4 qf[2][NKC];
     int lim[2];                            // last position that the lane's row sees
+    uint64_t line[2] = {0, 0}, mine = 0;   // TREE: nodes that it sees; those of node `lane`
+    if constexpr (TREE) {
+        if (un.end * VT_BLK > sq.ctx) mine = tree_lines(a.parent, sq);
+    }
     float sl2[2];                          // scores to base 2
     const QScale qs = q_scale(a.scale);
 #pragma unroll
@@ -267,6 +271,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         const bool live = 32 * c + l32 < wrows;
         const int tok = live ? rho / G : 0, h = live ? rho % G : 0;
         lim[c] = live ? sq.ctx + tok : -1;
+        if constexpr (TREE) line[c] = __shfl(mine, tok, 64);
         sl2[c] = qs.sl2;
         const uint16_t* q = a.q + (int64_t)(sq.row0 + tok) * a.q_stride + (kvh * G + h) * D;
         const uint32_t keep = live ? qs.keep : 0u, sign = qs.sign;
@@ -354,9 +359,15 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
         auto max3 = [](float x, float y, float z) { return fmaxf(fmaxf(x, y), z); };
         auto max_a = [&](int c) {
             if constexpr (DM) {
-                const int lc = lim[c] - (beg + i) * VT_BLK - 4 * h32;
+                if constexpr (TREE) {
+                    const uint32_t sees = tree_sees(line[c], (beg + i) * VT_BLK - sq.ctx) >> (4 * h32);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) cur.s[c][e] = koff(e) <= lc ? cur.s[c][e] : -INFINITY;
+                    for (int e = 0; e < 16; ++e) cur.s[c][e] = sees >> koff(e) & 1 ? cur.s[c][e] : -INFINITY;
+                } else {
+                    const int lc = lim[c] - (beg + i) * VT_BLK - 4 * h32;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) cur.s[c][e] = koff(e) <= lc ? cur.s[c][e] : -INFINITY;
+                }
             }
 #pragma unroll
             for (int x = 0; x < 5; ++x) t[c][x] = max3(cur.s[c][3 * x], cur.s[c][3 * x + 1], cur.s[c][3 * x + 2]);
@@ -633,7 +644,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))
             const int c = x & 1, d = 8 * (x >> 3) + 4 * h32 + ((x >> 1) & 3), r = 32 * c + l32;
             if (r >= wrows) continue;
             const int seen = sq.ctx + (wr0 + r) / G;
-            const float sum = stray_sum<D, KV8>(a, b, kvh, d, (beg + max(edge, 0)) * VT_BLK, min(seen, (beg + n) * VT_BLK - 1));
+            const float sum = stray_sum<D, KV8, TREE>(a, b, kvh, d, (beg + max(edge, 0)) * VT_BLK, min(seen, (beg + n) * VT_BLK - 1),
+                                                      sq.ctx, line[c]);
             if (sum == 0.f) continue;
             // added to what the lane wrote there, which may be infinite or NaN too
             if (un.pieces == 1) {
@@ -701,9 +713,15 @@ hipError_t launch_attn_tile(const AttnChunkArgs& a, unsigned grid, unsigned spli
     const bool i8 = a.kv.format == FP_KV_INT8;
     const int D = a.kv.head_dim;
     if (D == 64 && i8) return hipErrorInvalidValue;
-    if (D == 64) FP_LAUNCH((attn_tile_kernel<64, false>), dim3(grid), dim3(256), 0, st, a);
-    else if (i8) FP_LAUNCH((attn_tile_kernel<128, true>), dim3(grid), dim3(256), 0, st, a);
-    else FP_LAUNCH((attn_tile_kernel<128, false>), dim3(grid), dim3(256), 0, st, a);
+#define FP_TILE(D, I8)                                                                                              \
+    do {                                                                                                            \
+        if (a.parent != nullptr) FP_LAUNCH((attn_tile_kernel<D, I8, true>), dim3(grid), dim3(256), 0, st, a);       \
+        else FP_LAUNCH((attn_tile_kernel<D, I8, false>), dim3(grid), dim3(256), 0, st, a);                          \
+    } while (0)
+    if (D == 64) FP_TILE(64, false);
+    else if (i8) FP_TILE(128, true);
+    else FP_TILE(128, false);
+#undef FP_TILE
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || split_tiles == 0) return e;
     if (D == 128) FP_LAUNCH(attn_tile_join_kernel<128>, dim3(split_tiles, D / 4), dim3(256), 0, st, a);

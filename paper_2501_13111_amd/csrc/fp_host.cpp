@@ -872,8 +872,9 @@ fp_status enqueue_decode_batch(fp_layer* h, const uint16_t* x, uint16_t* y, hipS
 
 // The layer stack over a chunk's rows, keys and values in the caller's pages.  Up to a batch of rows takes
 // the decode projections (weights streamed once past the rows), more the prefill's.
-fp_status enqueue_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk& chunk, const uint16_t* x, uint16_t* y,
-                         float* attn_ws, hipStream_t st) {
+// parent: NULL, or the rows are nodes of trees.
+fp_status enqueue_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk& chunk, const int32_t* parent, const uint16_t* x,
+                         uint16_t* y, float* attn_ws, hipStream_t st) {
     const fp_shape& s = h->s;
     const int M = chunk.n_rows, H = s.hidden;
     const bool few = M <= s.max_batch, one = M == 1 && h->wq != FP_WQ_BF16_2OF4;
@@ -922,6 +923,7 @@ fp_status enqueue_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk& chu
         ap.q_out = h->q16;
         ap.cos_t = h->cos_t;
         ap.sin_t = h->sin_t;
+        ap.parent = parent;
         HIPCHK(launch_kv_append(ap, true, st));
         AttnChunkArgs at{};
         at.kv = kv[l];
@@ -932,6 +934,7 @@ fp_status enqueue_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk& chu
         at.scale = (float)(1.0 / std::sqrt((double)s.head_dim));
         at.out = h->act_o;
         at.out_fmt = h->act_fmt;
+        at.parent = parent;
         at.ws = attn_ws;
         HIPCHK(launch_attn_chunk(at, st));
         if (!few) {
@@ -1701,9 +1704,8 @@ fp_status fp_extend_workspace(const fp_layer* h, const fp_paged_kv* kv, const fp
     return FP_OK;
 }
 
-fp_status fp_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, const void* x, void* y, void* workspace,
-                    size_t workspace_bytes, void* stream) {
-    if (const fp_status rc = check_extend(h, kv, chunk)) return rc;
+static fp_status extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* x, void* y,
+                        void* workspace, size_t workspace_bytes, void* stream) {
     if (!x || !y) return fail(FP_ERR_INVALID_ARG, "x and y must be device pointers");
     const size_t bytes = (size_t)chunk->n_rows * h->s.hidden * 2;
     if (overlap(x, bytes, y, bytes)) return fail(FP_ERR_INVALID_ARG, "x and y overlap");
@@ -1714,7 +1716,20 @@ fp_status fp_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, c
     int dev = 0;
     HIPCHK(hipGetDevice(&dev));
     if (dev != h->device) return fail(FP_ERR_INVALID_ARG, "the current device is %d, the fingerprint's %d", dev, h->device);
-    return enqueue_extend(h, kv, *chunk, (const uint16_t*)x, (uint16_t*)y, (float*)workspace, (hipStream_t)stream);
+    return enqueue_extend(h, kv, *chunk, parent, (const uint16_t*)x, (uint16_t*)y, (float*)workspace, (hipStream_t)stream);
+}
+
+fp_status fp_extend(fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, const void* x, void* y, void* workspace,
+                    size_t workspace_bytes, void* stream) {
+    if (const fp_status rc = check_extend(h, kv, chunk)) return rc;
+    return extend(h, kv, chunk, nullptr, x, y, workspace, workspace_bytes, stream);
+}
+
+fp_status fp_extend_tree(fp_layer* h, const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* x, void* y,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+    if (const fp_status rc = check_extend(h, kv, chunk)) return rc;
+    if (const fp_status rc = check_tree(chunk, parent, !h->unbacked)) return rc;
+    return extend(h, kv, chunk, parent, x, y, workspace, workspace_bytes, stream);
 }
 
 fp_status fp_set_decode_graph(fp_layer* h, int32_t enable) {

@@ -277,6 +277,7 @@ struct KvAppendArgs {
     uint16_t* q_out;          // bf16 [n_rows, n_heads, d]
     const float* cos_t;       // NULL: keys arrive rotated
     const float* sin_t;
+    const int* parent;        // NULL, or the rows are nodes of trees: rotated by their depth
 };
 struct KvReadArgs {
     fp_paged_kv kv;
@@ -285,6 +286,7 @@ struct KvReadArgs {
     uint16_t* v_out;
 };
 fp_status check_paged(const fp_paged_kv* kv, const fp_chunk* c, bool pointers);
+fp_status check_tree(const fp_chunk* c, const int32_t* parent, bool pointers);
 hipError_t launch_kv_append(const KvAppendArgs& a, bool f32, hipStream_t st);
 hipError_t launch_kv_read(const KvReadArgs& a, hipStream_t st);
 
@@ -298,6 +300,7 @@ struct AttnChunkArgs {
     float scale;
     uint16_t* out;            // [n_rows, n_heads, d], activation format out_fmt
     int out_fmt;
+    const int* parent;        // NULL: causal; else the rows are nodes of trees (tree.h)
     float* ws;
     int* plan;                // of many sequences, behind the partial results
     int target, min_blocks, over, join;   // set by the launcher: see attn_plan.h
@@ -324,6 +327,51 @@ struct VerifyArgs {
 };
 size_t verify_ws_bytes(int n_seqs, int n_rows, int V);
 hipError_t launch_verify(const VerifyArgs& a, hipStream_t st);
+
+// Verification of drafted trees (verify.hip): draft_ids are the nodes' own tokens, u_last and the drafts' probabilities
+// are not used.
+size_t verify_tree_ws_bytes(int n_rows, int V);
+hipError_t launch_verify_tree(const VerifyArgs& a, const int* parent, int* path, hipStream_t st);
+
+// Several layers' caches of one geometry and format in one launch (branch.hip).
+constexpr int KV_SET = 32;
+struct KvSet {
+    fp_paged_kv kv[KV_SET];
+    int n;
+};
+struct KvKeepArgs {
+    fp_chunk chunk;
+    const int* path;          // [n_seqs, path_stride]
+    const int* n_keep;
+    int path_stride;
+};
+hipError_t launch_kv_keep(const KvSet& kvs, const KvKeepArgs& a, hipStream_t st);
+struct ReorderArgs {
+    int n_groups, n_beams, width, table_stride, out_stride;
+    const int* table;
+    const int* ctx_len;
+    const int* parent;
+    int* table_out;           // table itself, or apart from it
+};
+hipError_t launch_beam_copy(const KvSet& kvs, const ReorderArgs& a, hipStream_t st);
+hipError_t launch_beam_table(int page_size, const ReorderArgs& a, hipStream_t st);
+
+// Selection over beams and vocabulary (beam.hip).
+struct BeamArgs {
+    const float* logits;
+    int64_t row_stride;
+    int n_groups, n_beams, n_best, V;
+    const float* scores;
+    const uint8_t* done;
+    int eos, pad;
+    float* out_scores;
+    int* out_parent;
+    int* out_ids;
+    uint8_t* out_done;
+    void* ws;
+};
+size_t beam_ws_bytes(int n_rows, int n_best, int V);
+hipError_t launch_beam_select(const BeamArgs& a, hipStream_t st);
 
 // Whether a single decode step launches its inner layers as one graph.
 bool decode_step_inner_graph(int n_layers, bool single, size_t layer_bytes);

@@ -9,7 +9,7 @@
 // whose cosines and sines it has just read.  Bound by memory: a long chunk's rows move once in, once
 // out.  Appending 16 chunks of up to 4096, 32 heads on 8 of 128, bf16 (40,604 rows, 1.02 GB): 214 us, 4.8 TB/s; 64 single tokens on
 // 8 heads, int8: 6.2 us, a chain of latencies.  Reading 8 sequences of up to 16000 back, 8 heads of 128, int8 (473 MB): 97 us, 4.9 TB/s.
-#include "paged.h"
+#include "tree.h"
 
 namespace fpk {
 
@@ -105,7 +105,8 @@ __device__ __forceinline__ void rotate8(float (&lo)[8], float (&hi)[8], const fl
 
 // int8 from bf16 inputs: the registers fit eight waves a SIMD only if the compiler is told (256 single tokens on 8 heads of
 // 64 7.8 us, with seven waves 8.8).  bf16 caches have eight without it (16 chunks of up to 4096 214 us, told so 221).
-template <int D, bool KV8, bool F32>
+// TREE: the rows are nodes of trees, rotated by the context's length and their depth.
+template <int D, bool KV8, bool F32, bool TREE>
 __global__ void __launch_bounds__(T, KV8 && !F32 ? 8 : 1) kv_append_paged_kernel(KvAppendArgs a) {
     constexpr int HALF = D / 2, NP = HALF / 8;             // threads per position
     constexpr int ES = KV8 ? 1 : 2;
@@ -123,11 +124,19 @@ __global__ void __launch_bounds__(T, KV8 && !F32 ? 8 : 1) kv_append_paged_kernel
     const int pb = pool_block(a.kv, a.chunk, b, kvh, blk);
     const int row0 = sq.row0 + (blk * VT_BLK + t0 - sq.ctx);
     const int G = a.q != nullptr ? a.n_heads / a.kv.n_kv_heads : 0;
+    __shared__ int turn[TREE ? VT_BLK : 1];                // the live positions' rotary positions
+    if constexpr (TREE) {
+        if (tid < 64) {
+            const int depth = __popcll(tree_lines(a.parent, sq)) - 1, i = tid - (row0 - sq.row0);
+            if (tid < sq.n && i >= 0 && i < np) turn[i] = sq.ctx + depth;
+        }
+        __syncthreads();
+    }
 
     for (int it = tid; it < (2 + G) * np * NP; it += T) {
         const int what = it / (np * NP), r = it % (np * NP);
         const int i = r / NP, j = 8 * (r % NP);
-        const int t = t0 + i, pos = blk * VT_BLK + t;
+        const int t = t0 + i;
         const int64_t row = row0 + i;
         const int h = what < 2 ? kvh : kvh * G + what - 2;
         const void* src = what == 0 ? a.k : what == 1 ? a.v : a.q;
@@ -135,8 +144,10 @@ __global__ void __launch_bounds__(T, KV8 && !F32 ? 8 : 1) kv_append_paged_kernel
         float lo[8], hi[8];
         load8<F32>(src, off, a.ks, a.pstride, lo);
         load8<F32>(src, off + HALF, a.ks, a.pstride, hi);
-        if (what != 1 && a.cos_t != nullptr)
+        if (what != 1 && a.cos_t != nullptr) {
+            const int pos = TREE ? turn[i] : blk * VT_BLK + t;
             rotate8(lo, hi, a.cos_t + (int64_t)pos * HALF + j, a.sin_t + (int64_t)pos * HALF + j);
+        }
         if (what >= 2) {
             uint16_t* q = a.q_out + (row * a.n_heads + h) * D + j;
             *(u32x4*)q = pack8(lo);
@@ -274,7 +285,12 @@ hipError_t launch_kv_append(const KvAppendArgs& a, bool f32, hipStream_t st) {
     const int64_t n = (max_blocks(a.chunk) + 7) / 8 * 8 * a.kv.n_kv_heads;
     if (n < 1 || n > MAX_GRID) return hipErrorInvalidValue;
     const bool i8 = a.kv.format == FP_KV_INT8;
-#define FP_AP(D, I8, F32) FP_LAUNCH((kv_append_paged_kernel<D, I8, F32>), dim3((unsigned)n), dim3(T), 0, st, a)
+    const bool tree = a.parent != nullptr && a.cos_t != nullptr;
+#define FP_AP(D, I8, F32)                                                                                          \
+    do {                                                                                                           \
+        if (tree) FP_LAUNCH((kv_append_paged_kernel<D, I8, F32, true>), dim3((unsigned)n), dim3(T), 0, st, a);     \
+        else FP_LAUNCH((kv_append_paged_kernel<D, I8, F32, false>), dim3((unsigned)n), dim3(T), 0, st, a);         \
+    } while (0)
 #define FP_AP_D(D)                                                                   \
     do {                                                                             \
         if (f32) { if (i8) FP_AP(D, true, true); else FP_AP(D, false, true); }       \

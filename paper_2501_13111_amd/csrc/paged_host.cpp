@@ -66,9 +66,45 @@ fp_status fpk::check_paged(const fp_paged_kv* kv, const fp_chunk* c, bool pointe
     return FP_OK;
 }
 
+// A tree's checks beside its chunk's.
+fp_status fpk::check_tree(const fp_chunk* c, const int32_t* parent, bool pointers) {
+    if (c->max_new > 64) return fail(FP_ERR_UNSUPPORTED, "max_new %d: trees have up to 64 nodes", c->max_new);
+    if (pointers && c->n_rows > 0 && !parent) return fail(FP_ERR_INVALID_ARG, "parent must be a device pointer");
+    return FP_OK;
+}
+
 namespace {
 
 fp_status check_chunk(const fp_paged_kv* kv, const fp_chunk* c) { return check_paged(kv, c, true); }
+
+// Several layers' caches behind one table: one geometry, formats of their own.
+fp_status check_layers(const fp_paged_kv* kv, int32_t n_layers, const fp_chunk* c) {
+    if (!kv) return fail(FP_ERR_INVALID_ARG, "kv must not be NULL");
+    if (n_layers < 1) return fail(FP_ERR_INVALID_ARG, "n_layers must be >= 1");
+    for (int l = 0; l < n_layers; ++l) {
+        if (const fp_status s = check_paged(&kv[l], c, true)) return s;
+        if (kv[l].page_size != kv->page_size || kv[l].n_kv_heads != kv->n_kv_heads || kv[l].head_dim != kv->head_dim)
+            return fail(FP_ERR_INVALID_ARG, "layer %d's pages hold %d positions of %d kv heads of %d, the first's %d of %d of %d", l,
+                        kv[l].page_size, kv[l].n_kv_heads, kv[l].head_dim, kv->page_size, kv->n_kv_heads, kv->head_dim);
+    }
+    return FP_OK;
+}
+
+// f(set) for runs of layers of one format, up to KV_SET each.
+template <class F>
+hipError_t each_set(const fp_paged_kv* kv, int n_layers, F f) {
+    KvSet set;
+    for (int l = 0; l < n_layers; l += set.n) {
+        set.n = 0;
+        while (set.n < KV_SET && l + set.n < n_layers && kv[l + set.n].format == kv[l].format) {
+            set.kv[set.n] = kv[l + set.n];
+            ++set.n;
+        }
+        const hipError_t e = f(set);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
 
 fp_status check_heads(const fp_paged_kv* kv, int n_heads) {
     if (n_heads < 1 || n_heads % kv->n_kv_heads != 0)
@@ -98,11 +134,10 @@ size_t rows_bytes(int64_t rows, int64_t stride, int64_t width) { return rows > 0
 
 extern "C" {
 
-fp_status fp_kv_append(const fp_paged_kv* kv, const fp_chunk* chunk, const void* k, const void* v, int64_t kv_stride,
-                       const void* q, int64_t q_stride, int32_t n_heads, void* q_out, const float* cos_t,
-                       const float* sin_t, int32_t n_pos, void* stream) {
-    fp_status s = check_chunk(kv, chunk);
-    if (s) return s;
+static fp_status append(const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* k, const void* v,
+                        int64_t kv_stride, const void* q, int64_t q_stride, int32_t n_heads, void* q_out, const float* cos_t,
+                        const float* sin_t, int32_t n_pos, void* stream) {
+    fp_status s;
     const int64_t kw = (int64_t)kv->n_kv_heads * kv->head_dim;
     if ((s = check_rows("k", k, kv_stride, kw)) || (s = check_rows("v", v, kv_stride, kw))) return s;
     if (!cos_t != !sin_t) return fail(FP_ERR_INVALID_ARG, "cos and sin come together");
@@ -133,7 +168,23 @@ fp_status fp_kv_append(const fp_paged_kv* kv, const fp_chunk* chunk, const void*
     a.q_out = (uint16_t*)q_out;
     a.cos_t = cos_t;
     a.sin_t = sin_t;
+    a.parent = parent;
     return done(launch_kv_append(a, false, (hipStream_t)stream), "kv append");
+}
+
+fp_status fp_kv_append(const fp_paged_kv* kv, const fp_chunk* chunk, const void* k, const void* v, int64_t kv_stride,
+                       const void* q, int64_t q_stride, int32_t n_heads, void* q_out, const float* cos_t,
+                       const float* sin_t, int32_t n_pos, void* stream) {
+    if (const fp_status s = check_chunk(kv, chunk)) return s;
+    return append(kv, chunk, nullptr, k, v, kv_stride, q, q_stride, n_heads, q_out, cos_t, sin_t, n_pos, stream);
+}
+
+fp_status fp_kv_append_tree(const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* k, const void* v,
+                            int64_t kv_stride, const void* q, int64_t q_stride, int32_t n_heads, void* q_out,
+                            const float* cos_t, const float* sin_t, int32_t n_pos, void* stream) {
+    fp_status s = check_chunk(kv, chunk);
+    if (s || (s = check_tree(chunk, parent, true))) return s;
+    return append(kv, chunk, parent, k, v, kv_stride, q, q_stride, n_heads, q_out, cos_t, sin_t, n_pos, stream);
 }
 
 fp_status fp_kv_read(const fp_paged_kv* kv, const fp_chunk* chunk, void* k_out, void* v_out, void* stream) {
@@ -160,10 +211,10 @@ fp_status fp_attn_chunk_workspace(const fp_paged_kv* kv, const fp_chunk* chunk, 
     return FP_OK;
 }
 
-fp_status fp_attn_chunk(const fp_paged_kv* kv, const fp_chunk* chunk, const void* q, int64_t q_stride, int32_t n_heads,
-                        float scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
-    fp_status s = check_chunk(kv, chunk);
-    if (s || (s = check_heads(kv, n_heads))) return s;
+static fp_status attn(const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* q, int64_t q_stride,
+                      int32_t n_heads, float scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    fp_status s;
+    if ((s = check_heads(kv, n_heads))) return s;
     const int64_t qw = (int64_t)n_heads * kv->head_dim;
     if ((s = check_rows("q", q, q_stride, qw)) || (s = check_rows("out", out, qw, qw))) return s;
     if (overlap(q, rows_bytes(chunk->n_rows, q_stride, qw), out, rows_bytes(chunk->n_rows, qw, qw)))
@@ -183,8 +234,22 @@ fp_status fp_attn_chunk(const fp_paged_kv* kv, const fp_chunk* chunk, const void
     a.scale = scale;
     a.out = (uint16_t*)out;
     a.out_fmt = ACT_BF16;
+    a.parent = parent;
     a.ws = (float*)workspace;
     return done(launch_attn_chunk(a, (hipStream_t)stream), "chunk attention");
+}
+
+fp_status fp_attn_chunk(const fp_paged_kv* kv, const fp_chunk* chunk, const void* q, int64_t q_stride, int32_t n_heads,
+                        float scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (const fp_status s = check_chunk(kv, chunk)) return s;
+    return attn(kv, chunk, nullptr, q, q_stride, n_heads, scale, out, workspace, workspace_bytes, stream);
+}
+
+fp_status fp_attn_tree(const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* q, int64_t q_stride,
+                       int32_t n_heads, float scale, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    fp_status s = check_chunk(kv, chunk);
+    if (s || (s = check_tree(chunk, parent, true))) return s;
+    return attn(kv, chunk, parent, q, q_stride, n_heads, scale, out, workspace, workspace_bytes, stream);
 }
 
 static fp_status check_verify(int32_t n_seqs, int32_t n_rows, int32_t vocab) {
@@ -238,6 +303,160 @@ fp_status fp_verify_draft(const float* logits, int64_t row_stride, int32_t n_seq
     a.n_out = n_out;
     a.ws = workspace;
     return done(launch_verify(a, (hipStream_t)stream), "draft verification");
+}
+
+fp_status fp_kv_keep(const fp_paged_kv* kv, int32_t n_layers, const fp_chunk* chunk, const int32_t* path, int32_t path_stride,
+                     const int32_t* n_keep, void* stream) {
+    if (!kv || !chunk) return fail(FP_ERR_INVALID_ARG, "kv and chunk must not be NULL");
+    fp_status s = check_layers(kv, n_layers, chunk);
+    if (s || (s = check_tree(chunk, nullptr, false))) return s;
+    if (!path || !n_keep) return fail(FP_ERR_INVALID_ARG, "path and n_keep must be device pointers");
+    if (path_stride < 1) return fail(FP_ERR_INVALID_ARG, "path_stride must be >= 1");
+    if ((int64_t)chunk->n_seqs * kv->n_kv_heads > MAX_GRID / KV_SET)
+        return fail(FP_ERR_UNSUPPORTED, "%d sequences of %d kv heads", chunk->n_seqs, kv->n_kv_heads);
+    if (chunk->n_rows == 0) return FP_OK;
+    KvKeepArgs a{};
+    a.chunk = *chunk;
+    a.path = path;
+    a.n_keep = n_keep;
+    a.path_stride = path_stride;
+    return done(each_set(kv, n_layers, [&](const KvSet& set) { return launch_kv_keep(set, a, (hipStream_t)stream); }), "kv keep");
+}
+
+fp_status fp_verify_tree_workspace(int32_t n_seqs, int32_t n_rows, int32_t vocab, size_t* bytes) {
+    if (!bytes) return fail(FP_ERR_INVALID_ARG, "bytes is NULL");
+    if (const fp_status s = check_verify(n_seqs, n_rows, vocab)) return s;
+    *bytes = verify_tree_ws_bytes(n_rows, vocab);
+    return FP_OK;
+}
+
+fp_status fp_verify_tree(const float* logits, int64_t row_stride, int32_t n_seqs, int32_t n_rows, int32_t max_rows, int32_t vocab,
+                         const int32_t* row_start, const int32_t* parent, const int32_t* node_ids, const float* u,
+                         float temperature, int32_t* out_ids, int32_t* path, int32_t* n_out, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+    if (const fp_status s = check_verify(n_seqs, n_rows, vocab)) return s;
+    if (max_rows < 1) return fail(FP_ERR_INVALID_ARG, "max_rows must be >= 1");
+    if (max_rows > 64) return fail(FP_ERR_UNSUPPORTED, "max_rows %d > 64", max_rows);
+    if (!std::isfinite(temperature) || temperature < 0.f) return fail(FP_ERR_INVALID_ARG, "temperature must be finite and >= 0");
+    if (!row_start || !out_ids || !path || !n_out) return fail(FP_ERR_INVALID_ARG, "row_start, out_ids, path and n_out must be device pointers");
+    if (n_rows > 0) {
+        if (!logits || !parent || !node_ids) return fail(FP_ERR_INVALID_ARG, "logits, parent and node_ids must be device pointers");
+        if (row_stride < vocab) return fail(FP_ERR_INVALID_ARG, "logits rows are %lld apart, vocab is %d", (long long)row_stride, vocab);
+        if (temperature > 0.f && !u) return fail(FP_ERR_INVALID_ARG, "u must be a device pointer");
+    }
+    const size_t need = verify_tree_ws_bytes(n_rows, vocab);
+    if (need > 0 && (!workspace || !aligned(workspace, 16))) return fail(FP_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device pointer");
+    if (workspace_bytes < need) return fail(FP_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    VerifyArgs a{};
+    a.logits = logits;
+    a.row_stride = row_stride;
+    a.n_seqs = n_seqs;
+    a.n_rows = n_rows;
+    a.max_rows = max_rows;
+    a.V = vocab;
+    a.row_start = row_start;
+    a.draft_ids = node_ids;
+    a.u = u;
+    a.c = temperature > 0.f ? 1.44269504088896340736 / (double)temperature : 0.0;
+    a.out_ids = out_ids;
+    a.n_out = n_out;
+    a.ws = workspace;
+    return done(launch_verify_tree(a, parent, path, (hipStream_t)stream), "tree verification");
+}
+
+static fp_status check_beams(int32_t n_groups, int32_t n_beams) {
+    if (n_groups < 1 || n_beams < 1) return fail(FP_ERR_INVALID_ARG, "n_groups and n_beams must be >= 1");
+    if (n_beams > 64 || n_groups > 65535 || (int64_t)n_groups * n_beams > 65535)
+        return fail(FP_ERR_UNSUPPORTED, "%d groups of %d beams: up to 64 beams, 65535 in all", n_groups, n_beams);
+    return FP_OK;
+}
+
+static fp_status check_select(int32_t n_groups, int32_t n_beams, int32_t n_best, int32_t vocab) {
+    if (const fp_status s = check_beams(n_groups, n_beams)) return s;
+    if (n_best < 1 || vocab < 1) return fail(FP_ERR_INVALID_ARG, "n_best and vocab must be >= 1");
+    if (n_best > 64 || vocab > 1 << 20) return fail(FP_ERR_UNSUPPORTED, "n_best %d > 64 or vocab %d > 2^20", n_best, vocab);
+    return FP_OK;
+}
+
+fp_status fp_beam_select_workspace(int32_t n_groups, int32_t n_beams, int32_t n_best, int32_t vocab, size_t* bytes) {
+    if (!bytes) return fail(FP_ERR_INVALID_ARG, "bytes is NULL");
+    if (const fp_status s = check_select(n_groups, n_beams, n_best, vocab)) return s;
+    *bytes = beam_ws_bytes(n_groups * n_beams, n_best, vocab);
+    return FP_OK;
+}
+
+fp_status fp_beam_select(const float* logits, int64_t row_stride, int32_t n_groups, int32_t n_beams, int32_t n_best, int32_t vocab,
+                         const float* scores, const uint8_t* finished, int32_t eos_id, int32_t pad_id, float* out_scores,
+                         int32_t* out_parent, int32_t* out_ids, uint8_t* out_finished, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+    if (const fp_status s = check_select(n_groups, n_beams, n_best, vocab)) return s;
+    if (!logits || !scores || !out_scores || !out_parent || !out_ids)
+        return fail(FP_ERR_INVALID_ARG, "logits, scores, out_scores, out_parent and out_ids must be device pointers");
+    if (row_stride < vocab) return fail(FP_ERR_INVALID_ARG, "logits rows are %lld apart, vocab is %d", (long long)row_stride, vocab);
+    const size_t rows = (size_t)n_groups * n_beams, best = (size_t)n_groups * n_best;
+    const struct {
+        const void* p;
+        size_t n;
+    } in[] = {{logits, 4 * ((rows - 1) * (size_t)row_stride + vocab)}, {scores, 4 * rows}, {finished, finished ? rows : 0}},
+      out[] = {{out_scores, 4 * best}, {out_parent, 4 * best}, {out_ids, 4 * best}, {out_finished, out_finished ? best : 0}};
+    for (const auto& o : out)
+        for (const auto& i : in)
+            if (overlap(o.p, o.n, i.p, i.n)) return fail(FP_ERR_INVALID_ARG, "an output overlaps an input");
+    const size_t need = beam_ws_bytes(n_groups * n_beams, n_best, vocab);
+    if (!workspace || !aligned(workspace, 16)) return fail(FP_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device pointer");
+    if (workspace_bytes < need) return fail(FP_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    BeamArgs a{};
+    a.logits = logits;
+    a.row_stride = row_stride;
+    a.n_groups = n_groups;
+    a.n_beams = n_beams;
+    a.n_best = n_best;
+    a.V = vocab;
+    a.scores = scores;
+    a.done = finished;
+    a.eos = eos_id;
+    a.pad = pad_id;
+    a.out_scores = out_scores;
+    a.out_parent = out_parent;
+    a.out_ids = out_ids;
+    a.out_done = out_finished;
+    a.ws = workspace;
+    return done(launch_beam_select(a, (hipStream_t)stream), "beam selection");
+}
+
+fp_status fp_beam_reorder(const fp_paged_kv* kv, int32_t n_layers, int32_t n_groups, int32_t n_beams, const int32_t* table,
+                          int32_t table_stride, int32_t width, const int32_t* ctx_len, const int32_t* parent,
+                          int32_t* table_out, int32_t out_stride, void* stream) {
+    if (const fp_status s = check_beams(n_groups, n_beams)) return s;
+    if (!table || !ctx_len || !parent || !table_out)
+        return fail(FP_ERR_INVALID_ARG, "table, ctx_len, parent and table_out must be device pointers");
+    if (width < 1 || table_stride < width || out_stride < width)
+        return fail(FP_ERR_INVALID_ARG, "table rows of %d pages are %d apart, table_out's %d", width, table_stride, out_stride);
+    // the caches' checks come with a chunk's
+    fp_chunk c{};
+    c.n_seqs = c.max_new = c.max_len = 1;
+    c.table_stride = table_stride;
+    c.row_start = c.ctx_len = ctx_len;
+    c.table = table;
+    if (const fp_status s = check_layers(kv, n_layers, &c)) return s;
+    const size_t last = (size_t)n_groups * n_beams - 1;
+    if (table_out == table ? table_stride != out_stride
+                           : overlap(table, 4 * (last * table_stride + width), table_out, 4 * (last * out_stride + width)))
+        return fail(FP_ERR_INVALID_ARG, "table_out is neither the table nor apart from it");
+    ReorderArgs a{};
+    a.n_groups = n_groups;
+    a.n_beams = n_beams;
+    a.width = width;
+    a.table_stride = table_stride;
+    a.out_stride = out_stride;
+    a.table = table;
+    a.ctx_len = ctx_len;
+    a.parent = parent;
+    a.table_out = table_out;
+    // the copies read the table as it was
+    hipError_t e = each_set(kv, n_layers, [&](const KvSet& set) { return launch_beam_copy(set, a, (hipStream_t)stream); });
+    if (e == hipSuccess) e = launch_beam_table(kv->page_size, a, (hipStream_t)stream);
+    return done(e, "beam reordering");
 }
 
 }  // extern "C"

@@ -15,15 +15,9 @@
 //   pick_kernel   per sequence: the CK ids that hold the draw, then the id; writes the tokens
 // Greedy decoding (T = 0) needs the maxima only: row_kernel, pick_kernel.
 //
-// exp(x) = 2^y, y = x log2 e = n / 256 + r, |r| <= 1 / 512: 2^(n / 256) from a table of 256 and the
-// exponent, 2^r by its power series to the fourth order (the rest is below 4e-17).
-//
 // 32 sequences of 6 rows of 32000, T = 0.8: 9.3 us for the rows (24.6 MB; the exponentials' 64-bit arithmetic is some 6 of
 // them), 10 for the masses and 8 for the draw, both chains of a dozen dependent loads.  One sequence of 4 rows, T = 0: 3.8 + 2.2.
-#include <climits>
-
-#include "fp_device.h"
-#include "fp_internal.h"
+#include "vocab.h"
 
 namespace fpk {
 
@@ -40,74 +34,6 @@ struct Part {                              // one block of a row
     float max;
     int arg;
 };
-
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double dpp_d(double v) {
-    return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, ROWS, 0xf, false),
-                            __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, ROWS, 0xf, false));
-}
-// Inclusive sums over the wave's lanes.
-__device__ __forceinline__ double wave_scan_d(double v) {
-    v += dpp_d<0x111, 0xf>(v);
-    v += dpp_d<0x112, 0xf>(v);
-    v += dpp_d<0x114, 0xf>(v);
-    v += dpp_d<0x118, 0xf>(v);
-    v += dpp_d<0x142, 0xa>(v);
-    v += dpp_d<0x143, 0xc>(v);
-    return v;
-}
-__device__ __forceinline__ double lane_d(double v, int l) {
-    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), l), __builtin_amdgcn_readlane(__double2loint(v), l));
-}
-__device__ __forceinline__ double wave_sum_d(double v) { return lane_d(wave_scan_d(v), 63); }
-
-// 2^(n / 256), made by the compiler from the power series; a workgroup copies it to LDS (a barrier follows).
-struct ExpTable {
-    double v[256];
-    constexpr ExpTable() : v() {
-        for (int n = 0; n < 256; ++n) {
-            const double x = n * 0.693147180559945309417 / 256.0;
-            double s = 0.0;
-            for (int k = 24; k >= 1; --k) s = (s + 1.0) * x / k;
-            v[n] = 1.0 + s;
-        }
-    }
-};
-__device__ constexpr ExpTable EXP_TABLE;
-__device__ __forceinline__ void exp_table(double* tab) { tab[threadIdx.x] = EXP_TABLE.v[threadIdx.x]; }
-__device__ __forceinline__ double exp2_d(double y, const double* tab) {
-    y = fmax(y, -1200.0);                  // 2^-1200 is zero
-    constexpr double R = 6755399441055744.0 / 256.0;        // 1.5 2^52 / 256: adding it rounds to 1 / 256
-    const double t = y + R;
-    const int n = __double2loint(t);
-    const double r = y - (t - R);
-    constexpr double L = 0.693147180559945309417;
-    double q = L * L * L * L / 24.0;
-    q = fma(q, r, L * L * L / 6.0);
-    q = fma(q, r, L * L / 2.0);
-    q = fma(q, r, L);
-    q = fma(q, r, 1.0);
-    return ldexp(tab[n & 255] * q, n >> 8);
-}
-// exp((z - m) / T) with the weight rules: NaN and -inf have none, +inf all of it
-__device__ __forceinline__ double weight(float z, float m, double c, const double* tab) {
-    const double e = exp2_d(((double)z - (double)m) * c, tab);
-    return z == m ? 1.0 : !(z > -INFINITY) || m == INFINITY ? 0.0 : e;
-}
-
-// The same for z that is no NaN and m < +inf, without the rules: -inf gives 2^-1200, zero, and m itself one.
-__device__ __forceinline__ double weight_below(float z, double m, double c, const double* tab) {
-    return exp2_d(((double)z - m) * c, tab);
-}
-__device__ __forceinline__ float no_nan(float z) { return fmaxf(z, -INFINITY); }
-
-// the larger value, the lower id among equal ones
-__device__ __forceinline__ void best_of(float& v, int& i, float ov, int oi) {
-    if (ov > v || (ov == v && oi < i)) {
-        v = ov;
-        i = oi;
-    }
-}
 
 __device__ __forceinline__ int seq_row0(const VerifyArgs& a, int b) { return min(max(a.row_start[b], 0), a.n_rows); }
 __device__ __forceinline__ int seq_rows(const VerifyArgs& a, int b) {
@@ -360,9 +286,151 @@ __global__ void __launch_bounds__(NT) pick_kernel(VerifyArgs a, int nb, const do
     if (tid == 0) a.n_out[b] = d.rows > 0 ? d.acc + 1 : 0;
 }
 
+// ---- trees
+//
+// A tree's decision is that of one draw: with y_i drawn from p_i, node by node from the root on, the child that holds
+// y_i is accepted and a node without such a child ends the path with y_i.  Whatever the tree is, the tokens are those
+// that the target alone would draw.  Every node's draw is independent of the path, so all are made at once and only the
+// walk remains:
+//   row_kernel    as above
+//   draw_kernel   per row: the block that holds the draw by the blocks' sums, then the id in it
+//   walk_kernel   per sequence, one wave, lane i its node i (T = 0: a node's token is its row's maximum)
+
+__global__ void __launch_bounds__(NT) draw_kernel(VerifyArgs a, int nb, int* __restrict__ drawn) {
+    __shared__ double tab[NT], sd[2][NT / 64], before;
+    __shared__ float sm[NT / 64];
+    __shared__ int first[2], last[2];
+    static_assert(NT >= (1 << 20) / VB, "a thread per block of the largest vocabulary");
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int64_t row = blockIdx.x;
+    exp_table(tab);
+    if (tid < 2) {
+        first[tid] = INT_MAX;
+        last[tid] = -1;
+    }
+    const Part p = tid < nb ? ((const Part*)a.ws)[row * nb + tid] : Part{0.0, -INFINITY, INT_MAX};
+    float m = wave_max(p.max);
+    if (lane == 0) sm[w] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    if (!(m > -INFINITY)) {
+        if (tid == 0) drawn[row] = -1;
+        return;
+    }
+    // the first block whose running sum passes the goal; rounding may leave the goal at the total: then the
+    // last block with any mass, and in it the last id with any
+    const double mass = tid < nb ? p.sum * weight(p.max, m, a.c, tab) : 0.0;
+    double inc = wave_scan_d(mass);
+    if (lane == 63) sd[0][w] = inc;
+    __syncthreads();
+    double total = 0.0;
+    for (int j = 0; j < NT / 64; ++j) {
+        if (j == w) inc += total;
+        total += sd[0][j];
+    }
+    const double goal = (double)a.u[row] * total;
+    if (mass > 0.0) {
+        if (inc > goal) atomicMin(&first[0], tid);
+        atomicMax(&last[0], tid);
+    }
+    __syncthreads();
+    const int blk = first[0] != INT_MAX ? first[0] : last[0];
+    if (tid == blk) before = inc - mass;
+    // EPT ids in a row per thread
+    const int v0 = blk * VB + EPT * tid;
+    const float* z = a.logits + row * a.row_stride;
+    float x[EPT];
+    double wt[EPT], s = 0.0;
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) x[i] = v0 + i < a.V ? z[v0 + i] : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) {
+        wt[i] = weight(x[i], m, a.c, tab);
+        s += wt[i];
+    }
+    inc = wave_scan_d(s);
+    if (lane == 63) sd[1][w] = inc;
+    __syncthreads();
+    double run = before + (inc - s);
+    for (int j = 0; j < w; ++j) run += sd[1][j];
+    int at = INT_MAX, hi = -1;
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) {
+        run += wt[i];
+        if (wt[i] > 0.0) {
+            hi = v0 + i;
+            if (run > goal) at = min(at, v0 + i);
+        }
+    }
+    if (at != INT_MAX) atomicMin(&first[1], at);
+    if (hi >= 0) atomicMax(&last[1], hi);
+    __syncthreads();
+    if (tid == 0) drawn[row] = first[1] != INT_MAX ? first[1] : last[1];
+}
+
+__global__ void __launch_bounds__(64) walk_kernel(VerifyArgs a, int nb, const int* __restrict__ drawn, const int* __restrict__ parent,
+                                                  int* __restrict__ path) {
+    const int b = blockIdx.x, lane = threadIdx.x, n = seq_rows(a, b);
+    const int64_t row = seq_row0(a, b) + lane;
+    int p = -1, id = -1, y = -1;
+    if (lane < n) {
+        p = parent[row];
+        id = a.draft_ids[row];
+        if (p >= lane) p = -1;
+        if (a.c > 0.0) {
+            y = drawn[row];
+        } else {
+            const Part* q = (const Part*)a.ws + row * nb;
+            float m = -INFINITY;
+            int mi = INT_MAX;
+            for (int j0 = 0; j0 < nb; j0 += 8) {
+                Part x[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = q[min(j0 + j, nb - 1)];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) best_of(m, mi, x[j].max, x[j].arg);
+            }
+            y = m > -INFINITY ? mi : -1;
+        }
+    }
+    int at = 0, k = 0, tok = -1, node = -1;
+    while (k < n) {
+        const int yc = __builtin_amdgcn_readlane(y, at);
+        if (lane == k) {
+            tok = yc;
+            node = at;
+        }
+        ++k;
+        const uint64_t hit = __ballot(p == at && id == yc && yc >= 0);
+        if (hit == 0) break;
+        at = __builtin_ctzll(hit);
+    }
+    if (lane < a.max_rows) {
+        a.out_ids[(int64_t)b * a.max_rows + lane] = tok;
+        path[(int64_t)b * a.max_rows + lane] = node;
+    }
+    if (lane == 0) a.n_out[b] = k;
+}
+
 int blocks_of(int V) { return (V + VB - 1) / VB; }
 
 }  // namespace
+
+size_t verify_tree_ws_bytes(int n_rows, int V) { return (size_t)n_rows * (blocks_of(V) * sizeof(Part) + sizeof(int)); }
+
+hipError_t launch_verify_tree(const VerifyArgs& a, const int* parent, int* path, hipStream_t st) {
+    const int nb = blocks_of(a.V);
+    int* drawn = (int*)((Part*)a.ws + (size_t)a.n_rows * nb);
+    if (a.n_rows > 0) FP_LAUNCH(row_kernel, dim3(nb, a.n_rows), dim3(NT), 0, st, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (a.c > 0.0 && a.n_rows > 0) {
+        FP_LAUNCH(draw_kernel, dim3(a.n_rows), dim3(NT), 0, st, a, nb, drawn);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    FP_LAUNCH(walk_kernel, dim3(a.n_seqs), dim3(64), 0, st, a, nb, drawn, parent, path);
+    return hipGetLastError();
+}
 
 size_t verify_ws_bytes(int n_seqs, int n_rows, int V) {
     return (size_t)n_rows * blocks_of(V) * sizeof(Part) + (size_t)n_seqs * (blocks_of(V) * (VB / CK) * sizeof(double) + sizeof(Decision));

@@ -176,10 +176,11 @@ def _heads(t, name, n_rows, head_dim, device):
     return p, rs if n > 1 else h * head_dim, h
 
 
-def kv_append(kv: PagedKV, chunk: Chunk, k, v, q=None, q_out=None, cos=None, sin=None, stream=None):
+def kv_append(kv: PagedKV, chunk: Chunk, k, v, q=None, q_out=None, cos=None, sin=None, stream=None, parent=None):
     """Write k and v (bf16 [rows, kv heads, head_dim], views of a fused projection included) to the
     chunk's positions.  With cos and sin (float32 [positions, head_dim / 2]) k is rotated first, and
-    q, if given, into q_out."""
+    q, if given, into q_out.  With parent (int32 [rows]) the rows are nodes of drafted trees
+    (``branches.attn_tree``), rotated by their depth."""
     N, d, dev = k.shape[0], kv.head_dim, kv.device
     kp, ks, kh = _heads(k, "k", N, d, dev)
     vp, vs, vh = _heads(v, "v", N, d, dev)
@@ -201,7 +202,12 @@ def kv_append(kv: PagedKV, chunk: Chunk, k, v, q=None, q_out=None, cos=None, sin
         cp = _tensor(cos, torch.float32, "cos", (n_pos, d // 2), device=dev)
     if sin is not None:
         sp = _tensor(sin, torch.float32, "sin", (n_pos, d // 2), device=dev)
+    if parent is not None:
+        pp = _tensor(parent, torch.int32, "parent", (N,), device=dev)
     if N == 0:
+        return
+    if parent is not None:
+        _call("fp_kv_append_tree", dev, stream, kv.c, chunk.c(kv, N), pp, kp, vp, ks, qp, qs, H, op, cp, sp, n_pos)
         return
     _call("fp_kv_append", dev, stream, kv.c, chunk.c(kv, N), kp, vp, ks, qp, qs, H, op,
           cp, sp, n_pos)
@@ -236,15 +242,20 @@ def attn_chunk(kv: PagedKV, chunk: Chunk, q, out, scale: float | None = None, wo
     fused projection included) over the cache, the chunk's own positions included.  scale defaults to
     1 / sqrt(head_dim); without a workspace the call takes one from torch's allocator, on the current
     stream, so it refuses another `stream` then."""
+    _attn("fp_attn_chunk", (), kv, chunk, q, out, scale, workspace, stream)
+
+
+def _attn(name, parent, kv, chunk, q, out, scale, workspace, stream):
     N = q.shape[0]
     qp, qs, H = _heads(q, "q", N, kv.head_dim, kv.device)
     op = _tensor(out, torch.bfloat16, "out", (N, H, kv.head_dim), device=kv.device)
+    parent = tuple(_tensor(p, torch.int32, "parent", (N,), device=kv.device) for p in parent)
     if N == 0:
         return
     if workspace is None and stream is not None and stream != torch.cuda.current_stream(kv.device):
         raise ValueError("another stream than the current one needs a workspace of its own")
     w, wp, wn = _workspace(workspace, lambda: attn_chunk_workspace(kv, chunk, N, H), kv.device)
-    _call("fp_attn_chunk", kv.device, stream, kv.c, chunk.c(kv, N), qp, qs, H,
+    _call(name, kv.device, stream, kv.c, chunk.c(kv, N), *parent, qp, qs, H,
           1.0 / math.sqrt(kv.head_dim) if scale is None else float(scale), op, wp, wn)
 
 
