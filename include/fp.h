@@ -391,7 +391,8 @@ fp_status fp_verify_draft(const float* logits, int64_t row_stride, int32_t n_seq
  *
  * fp_kv_append_tree, fp_attn_tree and fp_extend_tree are fp_kv_append, fp_attn_chunk and fp_extend for such rows;
  * workspaces are those of fp_attn_chunk_workspace and fp_extend_workspace.  Without cos and sin an append does not
- * depend on parent.  In a tree that is one line, node i the child of node i - 1, results are those of the chunk's calls.
+ * depend on parent.  A tree that is one line, node i the child of node i - 1, is a chunk: the append writes the same bits, and the attention
+ * is the same up to its rounding.
  */
 fp_status fp_kv_append_tree(const fp_paged_kv* kv, const fp_chunk* chunk, const int32_t* parent, const void* k, const void* v,
                             int64_t kv_stride, const void* q, int64_t q_stride, int32_t n_heads, void* q_out,

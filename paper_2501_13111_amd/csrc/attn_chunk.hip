@@ -125,12 +125,12 @@ __global__ void __launch_bounds__(PLAN_T) attn_plan_kernel(AttnChunkArgs a) {
 
 // Joins the pieces of split tiles: RPW rows of a tile per workgroup, a thread per four dims of a row.
 // Pieces' statistics and outputs load eight at a time.
-template <int D, int RT>
+template <int D, int TILE>
 __global__ void __launch_bounds__(256) attn_chunk_join_kernel(AttnChunkArgs a) {
-    constexpr int RPW = 1024 / D, NS = RT / RPW;         // rows per workgroup; workgroups per tile
+    constexpr int RT = tile_size(TILE), RPW = 1024 / D, NS = RT / RPW;         // rows per workgroup; workgroups per tile
     const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
     Unit un;
-    if (!find_unit<RT, true, false>(a, G, un)) return;
+    if (!find_unit<TILE, true, false>(a, G, un)) return;
     const int rows = min(RT, un.sq.n * G - un.rt * RT);
     const int c = blockIdx.y * RPW + threadIdx.x / (D / 4), d0 = threadIdx.x % (D / 4) * 4;
     static_assert(NS * RPW == RT, "rows of a tile divide evenly");
@@ -194,6 +194,16 @@ int tile_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
     return blocks <= 8 || work <= (i8 ? 4096.0 : 2048.0) ? 32 : 64;
 }
 
+// The same for trees: as chunks, but 65 to 128 rows of 128 dims in calls that are large enough for tiles of 256 take those of
+// attn_wide.hip.  us, 64 heads on 8, 16 nodes of 32 sequences of up to 8192: bf16 156, in tiles of 256 225, of 64 216; int8 164, 279, of 32
+// 202.  (256 rows and more, in pairs of such tiles or tiles of 256 made the same way: no faster than attn_tile.hip's, 8 sequences of up to 30001 with
+// 512 rows to a kv head, bf16 69 and 61 against 61.  48 rows: int8 183, in tiles of 32 94; bf16 161, in tiles of 64 134.)
+int tree_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
+    const int RT = tile_rows(kv, c, n_heads);
+    const int64_t R = (int64_t)std::min(c.max_new, c.n_rows) * (n_heads / kv.n_kv_heads);
+    return RT == TILE_ROWS && kv.head_dim == 128 && R <= 128 ? WIDE | 128 : RT;
+}
+
 // log2 of the workgroups that run at a time (those of few rows: a half more), and the least number of blocks
 // worth a piece
 int piece_target(int RT, int D) { return RT == TILE_ROWS || (RT == 64 && D == 128) ? 8 : 9; }
@@ -204,7 +214,8 @@ int64_t piece_aim(int RT, int D) { return (int64_t)1 << (piece_target(RT, D) + (
 }  // namespace
 
 // Split tiles have more than Q blocks, so their pieces number at most twice total / Q, twice the aim.  Enough for
-// calls of smaller bounds too, whose tiles may be smaller.
+// calls of smaller bounds too, whose tiles may be smaller, and for those of trees in wide tiles.
+static_assert(WIDE_PIECES * 128 <= 2 * TILE_ROWS * TILE_ROWS, "WIDE_PIECES fit where tiles of 256 rows do");
 size_t attn_chunk_ws_bytes(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
     int64_t rows = 0;
     for (const int RT : {16, 32, 64, TILE_ROWS})
@@ -244,8 +255,28 @@ static hipError_t launch_rt(AttnChunkArgs a, hipStream_t st) {
     }
 }
 
+// Trees in wide tiles.
+static hipError_t launch_wide(AttnChunkArgs a, hipStream_t st) {
+    constexpr int RT = WIDE | 128, D = 128;
+    const int64_t nkv = a.kv.n_kv_heads, R = std::min<int64_t>(a.chunk.n_rows, (int64_t)a.chunk.n_seqs * a.chunk.max_new) * (a.n_heads / nkv);
+    const int64_t tiles = std::min(R, R / 128 + a.chunk.n_seqs) * nkv, n = tiles + WIDE_PIECES + 8 * XCD_RUN;
+    a.min_blocks = 32;
+    a.plan = (int*)(a.ws + (int64_t)WIDE_PIECES * 128 * wst(D));
+    if (n > MAX_GRID) return hipErrorInvalidValue;
+    const unsigned split = (a.chunk.max_len - 1) / VT_BLK < WHOLE<RT> ? 0u : (unsigned)std::min<int64_t>(tiles, WIDE_PIECES);
+    hipError_t e;
+    if (a.chunk.n_seqs > PLAN_LANES) {
+        FP_LAUNCH(attn_plan_kernel<RT>, dim3(1), dim3(PLAN_T), 0, st, a);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if ((e = launch_attn_wide(a, (unsigned)n, st)) != hipSuccess || split == 0) return e;
+    FP_LAUNCH((attn_chunk_join_kernel<D, RT>), dim3(split, 128 * D / 1024), dim3(256), 0, st, a);
+    return hipGetLastError();
+}
+
 template <int D, bool KV8>
 static hipError_t launch_d(const AttnChunkArgs& a, hipStream_t st) {
+    if (a.parent != nullptr && tree_rows(a.kv, a.chunk, a.n_heads) & WIDE) return launch_wide(a, st);
     switch (tile_rows(a.kv, a.chunk, a.n_heads)) {
         case 16: return launch_rt<D, KV8, 16>(a, st);
         case 32: return launch_rt<D, KV8, 32>(a, st);

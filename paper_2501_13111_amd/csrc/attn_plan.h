@@ -9,6 +9,9 @@ namespace fpk {
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int TILE_ROWS = 256;             // rows per tile of attn_tile.hip
+// The tiles of attn_wide.hip, of 128 rows, whose work is split by other figures, have this flag in RT.
+constexpr int WIDE = 1 << 16;
+constexpr int tile_size(int RT) { return RT & (WIDE - 1); }
 constexpr float M0 = -3e38f;               // softmax reference before any score
 
 // Sequences with at most 16 rows to a kv head in a call of 256-row tiles (next tokens beside a prompt's chunk)
@@ -33,11 +36,11 @@ struct Plan {
 // 64 sequences 22 us whole, 26 in two pieces; one sequence of 1000 17, 15.  Tiles of 256, 4 prompts of 512, 32 heads of 128, bf16
 // 37 whole, 47 in two.)
 template <int RT>
-constexpr int WHOLE = RT == TILE_ROWS ? 16 : RT == 64 ? 20 : 24;
+constexpr int WHOLE = RT & WIDE ? 32 : RT == TILE_ROWS ? 16 : RT == 64 ? 20 : 24;
 template <int RT>
 __device__ __forceinline__ Plan plan_seq(const Seq& s, int G, int Q) {
     Plan p;
-    p.tiles = (s.n * G + RT - 1) / RT;
+    p.tiles = (s.n * G + tile_size(RT) - 1) / tile_size(RT);
     p.blocks = s.n > 0 ? (s.len - 1) / VT_BLK + 1 : 0;
     p.pieces = p.blocks <= WHOLE<RT> ? std::min(p.blocks, 1) : (p.blocks + Q - 1) / Q;
     return p;
@@ -70,12 +73,20 @@ __device__ __forceinline__ int plan_one(const AttnChunkArgs& a, const Seq& s, in
     }
     return best;
 }
+constexpr int WIDE_PIECES = 768;
 // A count of TOTAL_MAX leaves every tile whole, as a larger one does: rows that overlap cannot overflow the sums.
 constexpr int64_t TOTAL_MAX = (int64_t)1 << 40;
 // total: tiles times blocks of all sequences; tiles: those not of few rows.  Both of one kv head.
 template <int RT>
 __device__ __forceinline__ int plan_all(const AttnChunkArgs& a, int64_t total, int tiles) {
     const float round = (float)(1 << a.target), nt = (float)tiles * (float)a.kv.n_kv_heads;
+    if constexpr ((RT & WIDE) != 0) {
+        // Few tiles: one round of equal pieces.  Many: two rounds, so that a long tile does not outlast the others (32 sequences
+        // of up to 8192, 8 kv heads, int8, 16 nodes: 164 us; aiming for one round 208).  At most WIDE_PIECES come of it: the
+        // aim, and one more for each tile that is split.
+        const float aim = nt <= 128.f ? 256.f - 0.5f * nt : fmaxf(512.f - 0.5f * nt, 256.f);
+        return std::max(a.min_blocks, (int)fminf((float)total * (float)a.kv.n_kv_heads / aim, 2.5e8f) + 1);
+    }
     float aim = fmaxf(round - 0.5f * nt, 0.5f * round);
     if (RT < 64 && a.chunk.n_seqs == 1) aim = round;
     if (RT < 64 && nt >= round) aim = 2.f * round;
@@ -152,7 +163,7 @@ __device__ __forceinline__ bool find_by_lanes(const AttnChunkArgs& a, int G, Uni
         tiles += long_tiles<RT>(mine[i], G, p);
     }
     t = std::min(t, TOTAL_MAX);
-    if (PER == 1 && RT >= 64 && n_seqs == 1) Q = plan_one<RT>(a, lane_seq(mine[0], 0), G);
+    if (PER == 1 && RT >= 64 && !(RT & WIDE) && n_seqs == 1) Q = plan_one<RT>(a, lane_seq(mine[0], 0), G);
     else Q = plan_all<RT>(a, wave_total((int)(t & 0xFFFFFF)) + ((int64_t)wave_total((int)(t >> 24)) << 24),
                           std::min(wave_total(tiles), 1 << 24));
 #pragma unroll
@@ -215,7 +226,7 @@ __device__ __forceinline__ bool find_unit(const AttnChunkArgs& a, int G, Unit& u
     un.kvh = SPLIT ? v : v / pl.pieces;
     un.part = part + (SPLIT ? un.kvh * pl.pieces * pl.tiles + un.rt : u);
     // the blocks up to the tile's last row, in equal pieces
-    const int last_row = min((un.rt + 1) * RT, un.sq.n * G) - 1;
+    const int last_row = min((un.rt + 1) * tile_size(RT), un.sq.n * G) - 1;
     const int blocks = min(pl.blocks, (un.sq.ctx + last_row / G) / VT_BLK + 1), per = (blocks + pl.pieces - 1) / pl.pieces;
     un.beg = sp * per;
     un.end = min(un.beg + per, blocks);

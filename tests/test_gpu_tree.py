@@ -72,11 +72,65 @@ def test_attention_matches_the_reference(seqs, nkv, G, d, page, kvq, loose):
     assert torch.equal(ref.bits(again[:N]), ref.bits(out[:N]))
 
 
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("nkv,G,page", [(2, 8, 64), (1, 16, 32), (3, 5, 96), (1, 2, 256)])
+@pytest.mark.parametrize("seqs", ["one", "edge", "split", "ragged"])
+def test_tiles_of_128_rows(seqs, nkv, G, page, kvq):
+    """65 to 128 rows to a kv head of 128 dims, beside sequences with fewer."""
+    fp = _fp()
+    m, d = 128 // G, 128
+    lens = {"one": [(331, m)], "edge": [(31, 2), (32, 5), (63, m), (0, m), (0, m - 1), (95, 1), (96, m), (1, m)],
+            "split": [(4500, 6), (3, 1), (2100, m), (1700, m - 2)], "ragged": [(5, 3), (0, 0), (100, m), (64, 0), (33, m - 3), (0, 1)]}[seqs]
+    g, pool, table = paged._case(lens, page, nkv, d, kvq, 22)
+    paged._fill(pool, table, lens, g, upto=lambda c, n: c + n, scale=1.5)
+    parent = _trees(g, lens, forest=G == 8)
+    chunk, starts = paged._chunk(lens, table, loose=page)
+    N = starts[-1]
+    q = torch.randn(N + 2, nkv * G, d, generator=g).bfloat16()
+    out = torch.full((N + 2, nkv * G, d), 7.0, dtype=torch.bfloat16).cuda()
+    kv, pp = pool.device(), _int(parent + [0, 0])
+    for scale in (None, -0.05):
+        fp.attn_tree(kv, chunk, pp, q.cuda(), out, scale=scale)
+        assert (out[N:] == 7.0).all()
+        _check(pool, table, lens, parent, q[:N], out, scale, fp16=kvq == "int8", floor=2.0 ** -25 if kvq == "int8" else 0.0)
+    again = torch.empty_like(out)
+    fp.attn_tree(kv, chunk, pp, q.cuda(), again, scale=-0.05)
+    assert torch.equal(ref.bits(again[:N]), ref.bits(out[:N]))
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("G,new,loose", [(4, 5, 0), (4, 30, 0), (8, 14, 64), (8, 60, 64)])
+def test_scores_far_apart_and_rising(G, new, loose, kvq):
+    """As the chunk's test: the softmax's reference moves again and again, tiny and large values, a negative scale, large queries.
+    (5 rows streamed, then tiles of 64 or 32, 128 and 256.)"""
+    fp = _fp()
+    nkv, d, page, lens = 2, 128, 64, [(900, new), (333, new)]
+    for scale, qs in ((None, 1.0), (-0.05, 1.0), (1e-7, 3e5), (3.0, 0.2), (0.0, 1.0)):
+        g, pool, table = paged._case(lens, page, nkv, d, kvq, 41)
+        for b, (c, n) in enumerate(lens):
+            m = c + n
+            ramp = torch.linspace(0.1, 6, m)[:, None, None]
+            pool.write(table[b], torch.arange(m), (ramp * (1 + 0.2 * torch.randn(m, nkv, d, generator=g))).bfloat16().float(),
+                       (torch.randn(m, nkv, d, generator=g) * (10.0 ** (torch.arange(m) % 5 - 3))[:, None, None]).bfloat16().float())
+        parent = _trees(g, lens)
+        chunk, starts = paged._chunk(lens, table, loose=loose)
+        q = (qs * (0.3 + torch.randn(starts[-1], nkv * G, d, generator=g))).bfloat16()
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device="cuda")
+        fp.attn_tree(pool.device(), chunk, _int(parent), q.cuda(), out, scale=scale)
+        # int8, more than 64 rows: keys and values in fp16, of which the smallest are off by 2^-25; probabilities below 2^-21
+        # of the largest by 2^-32 of it, times at most all values' magnitudes
+        floor = 0.0
+        if kvq == "int8":
+            vmax = max(float(pool.read(table[b], c + n)[1].abs().sum(0).max()) for b, (c, n) in enumerate(lens))
+            floor = 2.0 ** -25 + 2.0 ** -32 * vmax
+        _check(pool, table, lens, parent, q, out, scale, fp16=kvq == "int8" and new * G > 64, floor=floor)
+
+
 @pytest.mark.parametrize("loose", [False, True])
 @pytest.mark.parametrize("kvq", ["bf16", "int8"])
 @pytest.mark.parametrize("nkv,G,d,page", [(2, 4, 128, 64), (1, 5, 64, 32)])
 def test_a_line_is_a_chunk(nkv, G, d, page, kvq, loose):
-    """Node i the child of node i - 1: the same bits as the chunk's calls, written and read."""
+    """Node i the child of node i - 1: the same bits as the chunk's append, the same attention up to rounding."""
     fp = _fp()
     lens = [(5, 3), (100, 17), (64, 0), (33, 64), (1500, 40), (0, 1)]
     g, pool, table = paged._case(lens, page, nkv, d, kvq, 23)
@@ -96,8 +150,11 @@ def test_a_line_is_a_chunk(nkv, G, d, page, kvq, loose):
         else:
             fp.attn_tree(kv, chunk, p, qo, out)
         got.append([out, qo, kv.k, kv.v] + ([kv.k_scales, kv.v_scales] if kvq == "int8" else []))
-    for a, b in zip(*got):
+    for a, b in zip(got[0][1:], got[1][1:]):
         assert torch.equal(ref.bits(a), ref.bits(b))
+    # each side: its output's rounding, and probabilities rounded before they meet v (keys and values through fp16 too)
+    a, b = got[0][0].double(), got[1][0].double()
+    assert ((a - b).abs() <= 2 * (HALF_BF16 * b.abs() * 1.01 + (HALF_BF16 + 2.0 ** -11 + 1e-3) * v.abs().max().double())).all()
 
 
 @pytest.mark.parametrize("nkv,G,d,page,kvq,lens,loose", [
@@ -141,12 +198,16 @@ def test_long_attention(nkv, G, d, page, kvq, lens, loose):
 
 
 @pytest.mark.parametrize("kvq", ["bf16", "int8"])
-@pytest.mark.parametrize("nkv,G,d,loose", [(2, 4, 64, 0), (2, 4, 64, 32), (1, 8, 128, 0), (1, 8, 128, 32)])
-def test_values_that_are_not_finite_reach_the_nodes_that_see_them(nkv, G, d, loose, kvq):
+@pytest.mark.parametrize("nkv,G,d,loose,lens,sick", [
+    (2, 4, 64, 0, [(70, 40), (0, 33), (31, 64)], [5, 7, 50]), (2, 4, 64, 32, [(70, 40), (0, 33), (31, 64)], [5, 7, 50]),
+    (1, 8, 128, 0, [(70, 40), (0, 33), (31, 64)], [5, 7, 50]), (1, 8, 128, 32, [(70, 40), (0, 33), (31, 64)], [5, 7, 50]),
+    (1, 8, 128, 32, [(70, 16), (0, 13), (31, 15)], [5, 7, 2]),
+])
+def test_values_that_are_not_finite_reach_the_nodes_that_see_them(nkv, G, d, loose, lens, sick, kvq):
     """An infinite or NaN value (and a NaN key) of one node makes its descendants' outputs what they are, and changes no
     bit of the others'."""
     fp = _fp()
-    page, lens = 32, [(70, 40), (0, 33), (31, 64)]
+    page = 32
     g, pool, table = paged._case(lens, page, nkv, d, kvq, 25)
     paged._fill(pool, table, lens, g, upto=lambda c, n: c + n)
     parent = _trees(g, lens)
@@ -155,7 +216,7 @@ def test_values_that_are_not_finite_reach_the_nodes_that_see_them(nkv, G, d, loo
     clean, out = torch.empty_like(q), torch.empty_like(q)
     fp.attn_tree(pool.device(), chunk, _int(parent), q, clean)
     for what in ("inf", "nan", "key"):
-        odd, sick = pool.device(), [5, 7, 50]
+        odd = pool.device()
         for b, node in enumerate(sick):
             pos = lens[b][0] + node
             pg, off = int(table[b, pos // page]), pos % page
