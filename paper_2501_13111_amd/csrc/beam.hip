@@ -7,7 +7,7 @@
 //
 // A block's candidates: of 64 groups of its ids (a lane's, of all waves) the n_best-th largest of the groups' maxima is
 // at most the n_best-th largest logit, as each of those groups has one as large.  What is not below it, some n_best to 2 n_best
-// logits unless many are equal, is collected and ranked by counting.
+// logits unless many are equal, is collected and ranked by counting.  The merge bounds its entries by the lists' heads in the same way.
 #include "vocab.h"
 
 namespace fpk {
@@ -29,30 +29,71 @@ struct Cand {
     int id;
 };
 
-// the larger logit, the lower id among equal ones
-__device__ __forceinline__ bool before(float za, int ia, float zb, int ib) { return za > zb || (za == zb && ia < ib); }
-
 int blocks_of(int V) { return (V + BV - 1) / BV; }
 
-__global__ void __launch_bounds__(NT) rows_kernel(BeamArgs a, BeamPart* __restrict__ parts, Cand* __restrict__ lists) {
-    __shared__ double tab[NT], sd[NW];
-    __shared__ float gm[NW][64], cz[CAP];
-    __shared__ int ci[CAP], count, tally[2];
+// Floats in an order that unsigned numbers have (no NaN), and back.
+__device__ __forceinline__ uint32_t order(float f) {
+    const uint32_t u = __float_as_uint(f);
+    return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float unorder(uint32_t t) { return __uint_as_float(t & 0x80000000u ? t & 0x7FFFFFFFu : ~t); }
+
+// Candidates as numbers in their order: the larger logit, of equal ones (0 and -0 too) the lower id.
+__device__ __forceinline__ uint64_t cand_key(float z, uint32_t id) { return (uint64_t)order(z + 0.f) << 32 | ~id; }
+
+// How many of n keys are larger (8 reads at a time: alone, each would wait for the one before).
+template <class T>
+__device__ __forceinline__ int rank_of(const T* keys, int n, const T& me) {
+    int r = 0, o = 0;
+    for (; o + 8 <= n; o += 8) {
+        T k[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) k[j] = keys[o + j];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) r += me < k[j] ? 1 : 0;
+    }
+    for (; o < n; ++o) r += me < keys[o] ? 1 : 0;
+    return r;
+}
+
+// A number that at least k of the wave's lanes are not below: the k-th largest with the bits under `low` cleared.
+__device__ __forceinline__ uint32_t kth_largest(uint32_t key, int k, int low) {
+    uint32_t t = 0;
+    for (int bit = 31; bit >= low; --bit) {
+        const uint32_t c = t | 1u << bit;
+        if (__popcll(__ballot(key >= c)) >= k) t = c;
+    }
+    return t;
+}
+
+// exp(z - m) for a sum that is off by some 1e-12: the power series to the fourth order.  NaN and -inf give 2^-900.
+__device__ __forceinline__ double exp_near(float z, double m, const double* tab) {
+    return exp2_series<4>(fmax(((double)z - m) * 1.44269504088896340736, -900.0), tab);
+}
+
+__global__ void __launch_bounds__(NT, 8) rows_kernel(BeamArgs a, BeamPart* __restrict__ parts, Cand* __restrict__ lists) {
+    __shared__ double tab[EXP_N], sd[NW];
+    __shared__ float gm[NW][64];
+    __shared__ uint64_t cand[CAP];
+    __shared__ int count, tally[2];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, K = a.n_best;
     const int64_t row = blockIdx.y, at = row * gridDim.x + blockIdx.x;
     if (a.done != nullptr && a.done[row]) return;
-    exp_table(tab);
     const int v0 = blockIdx.x * BV + tid;
-    const float* z = a.logits + row * a.row_stride;
+    // past the row's end a load gives zeros
+    const int here = min(a.V - (int)blockIdx.x * BV, BV);
+    const auto z = buf_rsrc(a.logits + row * a.row_stride + blockIdx.x * BV, 4 * here);
     float x[EPT];
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) x[i] = v0 + NT * i < a.V ? z[v0 + NT * i] : -INFINITY;
-    float mine = -INFINITY;
+    for (int i = 0; i < EPT; ++i) x[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(z, 4 * tid, 4 * NT * i, 0));
+    if (here < BV) {
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) {
-        x[i] = no_nan(x[i]);
-        mine = fmaxf(mine, x[i]);
+        for (int i = 0; i < EPT; ++i) x[i] = tid + NT * i < here ? x[i] : -INFINITY;
     }
+    exp_table(tab);
+    float mine = -INFINITY;                // (NaN is no maximum, and passes no comparison below)
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) mine = fmaxf(mine, x[i]);
     gm[w][lane] = mine;
     if (tid == 0) count = 0;
     __syncthreads();
@@ -64,51 +105,50 @@ __global__ void __launch_bounds__(NT) rows_kernel(BeamArgs a, BeamPart* __restri
         if (tid == 0) parts[at] = BeamPart{0.0, m, 0};
         return;
     }
-    // rank of the lane's group among the 64; the K-th largest maximum
-    int rank = 0;
-    for (int j = 0; j < 64; ++j) {
-        const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(grp), j));
-        rank += before(o, j, grp, lane) ? 1 : 0;
-    }
-    const uint64_t kth = __ballot(rank == K - 1);
-    float tau = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(grp), __builtin_ctzll(kth)));
-    auto collect = [&](bool equal) {
+    float tau = fmaxf(unorder(kth_largest(order(grp), K, 14)), -INFINITY);       // (NaN: fewer than K groups have any)
+    auto collect = [&](auto passes) {
 #pragma unroll
         for (int i = 0; i < EPT; ++i)
-            if (x[i] > -INFINITY && (equal ? x[i] >= tau : x[i] > tau)) {
+            if (x[i] > -INFINITY && passes(x[i])) {
                 const int c = atomicAdd(&count, 1);
-                if (c < CAP) {
-                    cz[c] = x[i];
-                    ci[c] = v0 + NT * i;
-                }
+                if (c < CAP) cand[c] = cand_key(x[i], v0 + NT * i);
             }
     };
-    collect(true);
+    if (mine >= tau) collect([&](float v) { return v >= tau; });
+    double s = 0.0;
+    if (m < INFINITY) {
+        const double md = m;
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) s += exp_near(x[i], md, tab);
+    } else {
+        int k = 0;
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) k += x[i] == m ? 1 : 0;
+        s = k;
+    }
+    s = wave_sum_d(s);
+    if (lane == 0) sd[w] = s;
     __syncthreads();
     int n = count;
     if (n > CAP) {
         // Many equal ones (or an order that fills few lanes): the K-th largest logit itself by bisection of its bits, those
         // above it, fewer than K, and then of the equal ones the lowest ids.
-        auto order = [](float f) {
-            const uint32_t u = __float_as_uint(f);
-            return u & 0x80000000u ? ~u : u | 0x80000000u;
-        };
         uint32_t t = 0;
         for (int bit = 31; bit >= 0; --bit) {
             const uint32_t c = t | 1u << bit;
             int k = 0;
 #pragma unroll
-            for (int i = 0; i < EPT; ++i) k += __popcll(__ballot(order(x[i]) >= c));
+            for (int i = 0; i < EPT; ++i) k += __popcll(__ballot(order(no_nan(x[i])) >= c));
             if (tid == 0) tally[bit & 1] = 0;
             __syncthreads();
             if (lane == 0) atomicAdd(&tally[bit & 1], k);
             __syncthreads();
             if (tally[bit & 1] >= K) t = c;
         }
-        tau = __uint_as_float(t & 0x80000000u ? t & 0x7FFFFFFFu : ~t);
+        tau = unorder(t);
         if (tid == 0) count = 0;
         __syncthreads();
-        collect(false);
+        collect([&](float v) { return v > tau; });
         __syncthreads();
         n = count;
 #pragma unroll
@@ -124,80 +164,76 @@ __global__ void __launch_bounds__(NT) rows_kernel(BeamArgs a, BeamPart* __restri
                 all += k;
             }
             c += __popcll(b & ((1ull << lane) - 1));
-            if (eq && c < K) {
-                cz[c] = x[i];
-                ci[c] = v0 + NT * i;
-            }
+            if (eq && c < K) cand[c] = cand_key(x[i], v0 + NT * i);
             n = min(n + all, K);
             __syncthreads();
         }
     }
-    for (int j = tid; j < n; j += NT) {
-        const float zj = cz[j];
-        const int ij = ci[j];
-        int r = 0;
-        for (int o = 0; o < n; ++o) r += before(cz[o], ci[o], zj, ij) ? 1 : 0;
-        if (r < K) lists[at * K + r] = Cand{zj, ij};
-    }
-    double s = 0.0;
-    if (m < INFINITY) {
-        const double md = m;
-#pragma unroll
-        for (int i = 0; i < EPT; ++i) s += weight_below(x[i], md, 1.44269504088896340736, tab);
-    } else {
-        int k = 0;
-#pragma unroll
-        for (int i = 0; i < EPT; ++i) k += x[i] == m ? 1 : 0;
-        s = k;
-    }
-    s = wave_sum_d(s);
-    if (lane == 0) sd[w] = s;
-    __syncthreads();
     if (tid == 0) parts[at] = BeamPart{(sd[0] + sd[1]) + (sd[2] + sd[3]), m, min(n, K)};
+    for (int j = tid; j < n; j += NT) {
+        const uint64_t me = cand[j];
+        const int r = rank_of(cand, n, me);
+        if (r < K) lists[at * K + r] = Cand{unorder(me >> 32), (int)~(uint32_t)me};
+    }
 }
 
 // ---- merge.  A workgroup per group.
 constexpr int MT = 1024;
 constexpr int ENT = 1024;                  // entries that are ranked at once
+// A continuation as a number in their order: the larger score; of equal ones the lower beam, in it the larger logit, then the
+// lower id.
 struct Entry {
-    double s;
-    float z;
-    uint32_t at;               // beam, id
+    uint64_t score, at;
+    __device__ __forceinline__ bool operator<(const Entry& o) const { return score < o.score || (score == o.score && at < o.at); }
 };
-// The larger score; of equal ones the lower beam, in it the larger logit, then the lower id.
-__device__ __forceinline__ bool better(const Entry& x, const Entry& y) {
-    if (x.s != y.s) return x.s > y.s;
-    if (x.at >> 20 != y.at >> 20) return x.at >> 20 < y.at >> 20;
-    return before(x.z, x.at & 0xFFFFF, y.z, y.at & 0xFFFFF);
+__device__ __forceinline__ uint64_t order(double v) {
+    const uint64_t u = __double_as_longlong(v);
+    return u ^ ((uint64_t)((int64_t)u >> 63) | 1ull << 63);
+}
+__device__ __forceinline__ double unorder(uint64_t t) { return __longlong_as_double(t >> 63 ? t & ~(1ull << 63) : ~t); }
+__device__ __forceinline__ Entry make_entry(double s, int b, float z, int id) {
+    return Entry{order(s + 0.0), (uint64_t)(BEST - 1 - b) << 52 | (uint64_t)order(z + 0.f) << 20 | (uint64_t)(0xFFFFF - id)};
 }
 
+// A chain of latencies: the lists' parts and heads are loaded together, and then all entries of the lists whose heads pass.
 __global__ void __launch_bounds__(MT) merge_kernel(BeamArgs a, int nb, const BeamPart* __restrict__ parts, const Cand* __restrict__ lists) {
     __shared__ Entry ent[ENT];
-    __shared__ double tab[256], base[BEST], head[MT], cut;
-    __shared__ float top[BEST];
-    __shared__ int count, won[MT / 64];
+    __shared__ double tab[EXP_N], base[BEST], ps[MT];
+    __shared__ uint64_t head[MT / 64][64];
+    __shared__ float top[BEST], pm[MT];
+    __shared__ int count, passed, won[MT / 64], pass[MT], length[MT];
     __shared__ uint8_t taken[BEST * ((1 << 20) / BV)];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = blockIdx.x, W = a.n_beams, K = a.n_best;
     const int64_t row0 = (int64_t)g * W;
-    if (tid < 256) exp_table(tab);
-    if (tid == 0) {
-        count = 0;
-        cut = -INFINITY;
+    const int L = W * nb;
+    auto is_done = [&](int b) { return a.done != nullptr && a.done[row0 + b]; };
+    // the thread's first list: its part and its head (those of a finished beam's rows are not written)
+    const bool mine = tid < L && !is_done(tid / nb);
+    BeamPart p0 = {0.0, -INFINITY, 0};
+    Cand c0 = {0.f, 0};
+    if (mine) {
+        p0 = parts[row0 * nb + tid];
+        c0 = lists[(row0 * nb + tid) * K];
     }
+    exp_table(tab);
+    ps[tid] = p0.sum;
+    pm[tid] = p0.max;
+    if (tid == 0) count = passed = 0;
     __syncthreads();
     // a row's sum: base + (z - m) is the score of a continuation (z - m first: of a row whose logits all are the type's
     // lowest value it is zero, and the sum's logarithm is not lost)
     for (int b = w; b < W; b += MT / 64) {
         const float sc = a.scores[row0 + b];
-        const bool done = a.done != nullptr && a.done[row0 + b];
+        const bool done = is_done(b);
         float m = -INFINITY;
         double s = 0.0;
         if (!done) {
-            const BeamPart* p = parts + (row0 + b) * nb;
-            for (int j = lane; j < nb; j += 64) m = fmaxf(m, p[j].max);
+            auto part_max = [&](int j) { return b * nb + j < MT ? pm[b * nb + j] : parts[(row0 + b) * nb + j].max; };
+            for (int j = lane; j < nb; j += 64) m = fmaxf(m, part_max(j));
             m = wave_max(m);
             if (m > -INFINITY)
-                for (int j = lane; j < nb; j += 64) s += p[j].sum * weight(p[j].max, m, 1.44269504088896340736, tab);
+                for (int j = lane; j < nb; j += 64)
+                    s += (b * nb + j < MT ? ps[b * nb + j] : parts[(row0 + b) * nb + j].sum) * weight(part_max(j), m, 1.44269504088896340736, tab);
             s = wave_sum_d(s);
         }
         if (lane == 0) {
@@ -209,86 +245,102 @@ __global__ void __launch_bounds__(MT) merge_kernel(BeamArgs a, int nb, const Bea
     }
     __syncthreads();
     // Entry r of list l (a row's blocks one after another; a finished beam has one list of itself).
-    const int L = W * nb;
-    auto entry = [&](int l, int r, Entry& e) {
+    auto entries = [&](int l) {
         const int b = l / nb;
-        if (!(base[b] > -INFINITY)) return false;
-        if (a.done != nullptr && a.done[row0 + b]) {
-            e = Entry{base[b], 0.f, (uint32_t)b << 20};
-            return l % nb == 0 && r == 0;
+        if (!(base[b] > -INFINITY)) return 0;
+        if (is_done(b)) return l % nb == 0 ? 1 : 0;
+        return l == tid ? p0.n : parts[row0 * nb + l].n;
+    };
+    auto make = [&](int l, const Cand& c, Entry& e) {
+        const int b = l / nb;
+        if (is_done(b)) {
+            e = make_entry(base[b], b, 0.f, 0);
+            return true;
         }
-        const int64_t at = row0 * nb + l;
-        if (r >= parts[at].n) return false;
-        const Cand c = lists[at * K + r];
         if (top[b] == INFINITY && c.z < INFINITY) return false;       // infinite logits share the whole
-        e = Entry{base[b] + (top[b] == INFINITY ? 0.0 : (double)c.z - (double)top[b]), c.z, (uint32_t)b << 20 | (uint32_t)c.id};
+        e = make_entry(base[b] + (top[b] == INFINITY ? 0.0 : (double)c.z - (double)top[b]), b, c.z, c.id);
         return true;
     };
+    auto load = [&](int l, int r) { return is_done(l / nb) ? Cand{0.f, 0} : l == tid && r == 0 ? c0 : lists[(row0 * nb + l) * K + r]; };
+    auto entry = [&](int l, int r, Entry& e) { return r < entries(l) && make(l, load(l, r), e); };
     auto emit = [&](int r, const Entry& e) {
-        const int b = e.at >> 20;
-        const bool was = a.done != nullptr && a.done[row0 + b];
-        const int id = was ? a.pad : (int)(e.at & 0xFFFFF);
+        const int b = BEST - 1 - (int)(e.at >> 52);
+        const bool was = is_done(b);
+        const int id = was ? a.pad : 0xFFFFF - (int)(e.at & 0xFFFFF);
         const int64_t o = (int64_t)g * K + r;
-        a.out_scores[o] = (float)e.s;
+        a.out_scores[o] = (float)unorder(e.score);
         a.out_parent[o] = b;
         a.out_ids[o] = id;
         if (a.out_done != nullptr) a.out_done[o] = was || id == a.eos;
     };
-    // The K-th largest of the threads' best heads is at most the K-th largest entry.
-    double best = -INFINITY;
+    // Of 64 groups of lists (a lane's, of all waves) the K-th largest of the groups' best heads is at most the K-th largest entry.
+    // (Scores are kept as numbers in their order; none is 0.)
+    uint64_t best = 0, first = 0;
     for (int l = tid; l < L; l += MT) {
         Entry e;
-        if (entry(l, 0, e)) best = fmax(best, e.s);
+        if (entry(l, 0, e)) best = max(best, e.score);
+        if (l == tid) first = best;
     }
-    head[tid] = best;
+    head[w][lane] = best;
     __syncthreads();
-    const int H = min(L, MT);
-    if (H >= K && tid < H) {
-        int r = 0;
-        for (int j = 0; j < H; ++j) r += head[j] > best || (head[j] == best && j < tid) ? 1 : 0;
-        if (r == K - 1) cut = best;
-    }
-    __syncthreads();
+    best = head[0][lane];
+#pragma unroll
+    for (int j = 1; j < MT / 64; ++j) best = max(best, head[j][lane]);
+    const uint64_t cut = max((uint64_t)kth_largest((uint32_t)(best >> 32), K, 8) << 32, (uint64_t)1);
     for (int l = tid; l < L; l += MT) {
+        uint64_t s = first;
+        if (l != tid) {
+            Entry e;
+            s = entry(l, 0, e) ? e.score : 0;
+        }
+        if (s >= cut) {
+            const int i = atomicAdd(&passed, 1);
+            if (i < MT) {
+                pass[i] = l;
+                length[i] = entries(l);
+            }
+        }
+    }
+    __syncthreads();
+    for (int it = tid; it < min(passed, MT) * K; it += MT) {
+        const int i = it / K, r = it % K;
         Entry e;
-        for (int r = 0; r < K && entry(l, r, e) && e.s >= cut; ++r) {
-            const int i = atomicAdd(&count, 1);
-            if (i < ENT) ent[i] = e;
+        if (r < length[i] && make(pass[i], load(pass[i], r), e) && e.score >= cut) {
+            const int j = atomicAdd(&count, 1);
+            if (j < ENT) ent[j] = e;
         }
     }
     __syncthreads();
     int n = count;
-    if (n <= ENT) {
+    if (n <= ENT && passed <= MT) {
         for (int i = tid; i < n; i += MT) {
-            const Entry e = ent[i];
-            int r = 0;
-            for (int j = 0; j < n; ++j) r += better(ent[j], e) ? 1 : 0;
-            if (r < K) emit(r, e);
+            const int r = rank_of(ent, n, ent[i]);
+            if (r < K) emit(r, ent[i]);
         }
     } else {
         // Many equal scores, or few long lists: the lists are merged head by head.
         for (int l = tid; l < L; l += MT) taken[l] = 0;
-        Entry mine;
+        Entry next;
         int from;
         auto heads = [&]() {               // the best head of the thread's lists
             from = -1;
             for (int l = tid; l < L; l += MT) {
                 Entry e;
-                if (taken[l] < K && entry(l, taken[l], e) && (from < 0 || better(e, mine))) {
-                    mine = e;
+                if (taken[l] < K && entry(l, taken[l], e) && (from < 0 || next < e)) {
+                    next = e;
                     from = l;
                 }
             }
         };
         heads();
         for (n = 0; n < K; ++n) {
-            Entry e = mine;
+            Entry e = next;
             int l = from;
 #pragma unroll
             for (int o = 32; o >= 1; o >>= 1) {
-                const Entry y = {__shfl_xor(e.s, o, 64), __shfl_xor(e.z, o, 64), __shfl_xor(e.at, o, 64)};
+                const Entry y = {__shfl_xor(e.score, o, 64), __shfl_xor(e.at, o, 64)};
                 const int yl = __shfl_xor(l, o, 64);
-                if (yl >= 0 && (l < 0 || better(y, e))) {
+                if (yl >= 0 && (l < 0 || e < y)) {
                     e = y;
                     l = yl;
                 }
@@ -302,7 +354,7 @@ __global__ void __launch_bounds__(MT) merge_kernel(BeamArgs a, int nb, const Bea
             e = ent[0];
             l = won[0];
             for (int j = 1; j < MT / 64; ++j)
-                if (won[j] >= 0 && (l < 0 || better(ent[j], e))) {
+                if (won[j] >= 0 && (l < 0 || e < ent[j])) {
                     e = ent[j];
                     l = won[j];
                 }

@@ -43,7 +43,7 @@ __device__ __forceinline__ int seq_rows(const VerifyArgs& a, int b) {
 __global__ void __launch_bounds__(NT) row_kernel(VerifyArgs a) {
     __shared__ float sm[NT / 64];
     __shared__ int si[NT / 64];
-    __shared__ double sd[NT / 64], tab[NT];
+    __shared__ double sd[NT / 64], tab[EXP_N];
     const int nb = gridDim.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t row = blockIdx.y;
     if (a.c > 0.0) exp_table(tab);
@@ -177,7 +177,7 @@ __device__ __forceinline__ void draw_weights(const VerifyArgs& a, const Decision
 }
 
 __global__ void __launch_bounds__(NT) mass_kernel(VerifyArgs a, double* __restrict__ mass, Decision* __restrict__ kept) {
-    __shared__ double tab[NT], sd[VB / CK][NT / 64];
+    __shared__ double tab[EXP_N], sd[VB / CK][NT / 64];
     const int nb = gridDim.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     exp_table(tab);
     __syncthreads();
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(NT) mass_kernel(VerifyArgs a, double* __restri
 
 // One workgroup per sequence.  The chunk that holds the draw from the chunks' masses, then the id in it.
 __global__ void __launch_bounds__(NT) pick_kernel(VerifyArgs a, int nb, const double* __restrict__ mass, const Decision* __restrict__ kept) {
-    __shared__ double tab[NT], sd[NT / 64];
+    __shared__ double tab[EXP_N], sd[NT / 64];
     __shared__ int found, top;
     const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     exp_table(tab);
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(NT) pick_kernel(VerifyArgs a, int nb, const do
 //   walk_kernel   per sequence, one wave, lane i its node i (T = 0: a node's token is its row's maximum)
 
 __global__ void __launch_bounds__(NT) draw_kernel(VerifyArgs a, int nb, int* __restrict__ drawn) {
-    __shared__ double tab[NT], sd[2][NT / 64], before;
+    __shared__ double tab[EXP_N], sd[2][NT / 64], before;
     __shared__ float sm[NT / 64];
     __shared__ int first[2], last[2];
     static_assert(NT >= (1 << 20) / VB, "a thread per block of the largest vocabulary");
