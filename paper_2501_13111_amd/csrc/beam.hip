@@ -66,13 +66,13 @@ __device__ __forceinline__ uint32_t kth_largest(uint32_t key, int k, int low) {
     return t;
 }
 
-// exp(z - m) for a sum that is off by some 1e-12: the power series to the fourth order.  NaN and -inf give 2^-900.
+// exp(z - m) for a sum that is off by some 1e-12, from a table whose entries lie in different banks of LDS.  NaN and -inf give 2^-900.
 __device__ __forceinline__ double exp_near(float z, double m, const double* tab) {
-    return exp2_series<4>(fmax(((double)z - m) * 1.44269504088896340736, -900.0), tab);
+    return exp2_series<32>(fmax(((double)z - m) * 1.44269504088896340736, -900.0), tab);
 }
 
 __global__ void __launch_bounds__(NT, 8) rows_kernel(BeamArgs a, BeamPart* __restrict__ parts, Cand* __restrict__ lists) {
-    __shared__ double tab[EXP_N], sd[NW];
+    __shared__ double tab[32], sd[NW];
     __shared__ float gm[NW][64];
     __shared__ uint64_t cand[CAP];
     __shared__ int count, tally[2];

@@ -40,32 +40,45 @@ __device__ __forceinline__ int seq_rows(const VerifyArgs& a, int b) {
     return min(max(min(max(a.row_start[b + 1], 0), a.n_rows) - seq_row0(a, b), 0), a.max_rows);
 }
 
-__global__ void __launch_bounds__(NT) row_kernel(VerifyArgs a) {
+// GREEDY: the maximum and its lowest id; else the maximum and the sum.
+template <bool GREEDY>
+__global__ void __launch_bounds__(NT, 8) row_kernel(VerifyArgs a) {
     __shared__ float sm[NT / 64];
     __shared__ int si[NT / 64];
     __shared__ double sd[NT / 64], tab[EXP_N];
     const int nb = gridDim.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t row = blockIdx.y;
-    if (a.c > 0.0) exp_table(tab);
-    const int v0 = blockIdx.x * VB;
-    const float* z = a.logits + row * a.row_stride;
+    // past the row's end a load gives zeros
+    const int v0 = blockIdx.x * VB, here = min(a.V - v0, VB);
+    const auto z = buf_rsrc(a.logits + row * a.row_stride + v0, 4 * here);
     float x[EPT];
+#pragma unroll
+    for (int i = 0; i < EPT; ++i) x[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(z, 4 * tid, 4 * NT * i, 0));
+    if (here < VB) {
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) x[i] = tid + NT * i < here ? x[i] : -INFINITY;
+    }
+    if (!GREEDY) exp_table(tab);
     float m = -INFINITY;
     int mi = INT_MAX;
 #pragma unroll
     for (int i = 0; i < EPT; ++i) {
-        const int v = v0 + tid + NT * i;
-        x[i] = v < a.V ? z[v] : -INFINITY;
-        if (x[i] > m) {
+        if (!GREEDY) {
+            m = fmaxf(m, x[i]);
+        } else if (x[i] > m) {
             m = x[i];
-            mi = v;
+            mi = v0 + tid + NT * i;
         }
     }
+    if constexpr (GREEDY) {
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const float ov = __shfl_xor(m, o, 64);
-        const int oi = __shfl_xor(mi, o, 64);
-        best_of(m, mi, ov, oi);
+        for (int o = 32; o >= 1; o >>= 1) {
+            const float ov = __shfl_xor(m, o, 64);
+            const int oi = __shfl_xor(mi, o, 64);
+            best_of(m, mi, ov, oi);
+        }
+    } else {
+        m = wave_max(m);
     }
     if (lane == 0) {
         sm[w] = m;
@@ -77,7 +90,7 @@ __global__ void __launch_bounds__(NT) row_kernel(VerifyArgs a) {
 #pragma unroll
     for (int j = 1; j < NT / 64; ++j) best_of(m, mi, sm[j], si[j]);
     double s = 0.0;
-    if (a.c > 0.0 && m > -INFINITY) {
+    if (!GREEDY && m > -INFINITY) {
         if (m < INFINITY) {
             const double md = m;
 #pragma unroll
@@ -296,35 +309,40 @@ __global__ void __launch_bounds__(NT) pick_kernel(VerifyArgs a, int nb, const do
 //   draw_kernel   per row: the block that holds the draw by the blocks' sums, then the id in it
 //   walk_kernel   per sequence, one wave, lane i its node i (T = 0: a node's token is its row's maximum)
 
-__global__ void __launch_bounds__(NT) draw_kernel(VerifyArgs a, int nb, int* __restrict__ drawn) {
-    __shared__ double tab[EXP_N], sd[2][NT / 64], before;
-    __shared__ float sm[NT / 64];
+constexpr int DT = 1024, DPT = VB / DT;     // threads of a draw, ids of one
+__global__ void __launch_bounds__(DT) draw_kernel(VerifyArgs a, int nb, int* __restrict__ drawn) {
+    __shared__ double tab[EXP_N], sd[2][DT / 64], before;
+    __shared__ float sm[DT / 64];
     __shared__ int first[2], last[2];
-    static_assert(NT >= (1 << 20) / VB, "a thread per block of the largest vocabulary");
+    static_assert(DT >= (1 << 20) / VB, "a thread per block of the largest vocabulary");
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int64_t row = blockIdx.x;
+    const Part p = tid < nb ? ((const Part*)a.ws)[row * nb + tid] : Part{0.0, -INFINITY, INT_MAX};
     exp_table(tab);
     if (tid < 2) {
         first[tid] = INT_MAX;
         last[tid] = -1;
     }
-    const Part p = tid < nb ? ((const Part*)a.ws)[row * nb + tid] : Part{0.0, -INFINITY, INT_MAX};
     float m = wave_max(p.max);
     if (lane == 0) sm[w] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    const int waves = (nb + 63) / 64;
+    m = sm[0];
+    for (int j = 1; j < waves; ++j) m = fmaxf(m, sm[j]);
     if (!(m > -INFINITY)) {
         if (tid == 0) drawn[row] = -1;
         return;
     }
     // the first block whose running sum passes the goal; rounding may leave the goal at the total: then the
     // last block with any mass, and in it the last id with any
-    const double mass = tid < nb ? p.sum * weight(p.max, m, a.c, tab) : 0.0;
-    double inc = wave_scan_d(mass);
-    if (lane == 63) sd[0][w] = inc;
+    double mass = 0.0, inc = 0.0, total = 0.0;
+    if (w < waves) {
+        mass = tid < nb ? p.sum * weight(p.max, m, a.c, tab) : 0.0;
+        inc = wave_scan_d(mass);
+        if (lane == 63) sd[0][w] = inc;
+    }
     __syncthreads();
-    double total = 0.0;
-    for (int j = 0; j < NT / 64; ++j) {
+    for (int j = 0; j < waves; ++j) {
         if (j == w) inc += total;
         total += sd[0][j];
     }
@@ -336,16 +354,16 @@ __global__ void __launch_bounds__(NT) draw_kernel(VerifyArgs a, int nb, int* __r
     __syncthreads();
     const int blk = first[0] != INT_MAX ? first[0] : last[0];
     if (tid == blk) before = inc - mass;
-    // EPT ids in a row per thread
-    const int v0 = blk * VB + EPT * tid;
-    const float* z = a.logits + row * a.row_stride;
-    float x[EPT];
-    double wt[EPT], s = 0.0;
+    // DPT ids in a row per thread
+    const int at0 = blk * VB, v0 = at0 + DPT * tid, here = min(a.V - at0, VB);
+    const auto z = buf_rsrc(a.logits + row * a.row_stride + at0, 4 * here);
+    float x[DPT];
+    double wt[DPT], s = 0.0;
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) x[i] = v0 + i < a.V ? z[v0 + i] : -INFINITY;
+    for (int i = 0; i < DPT; ++i) x[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(z, 4 * (DPT * tid + i), 0, 0));
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) {
-        wt[i] = weight(x[i], m, a.c, tab);
+    for (int i = 0; i < DPT; ++i) {
+        wt[i] = DPT * tid + i < here ? weight(x[i], m, a.c, tab) : 0.0;
         s += wt[i];
     }
     inc = wave_scan_d(s);
@@ -355,15 +373,17 @@ __global__ void __launch_bounds__(NT) draw_kernel(VerifyArgs a, int nb, int* __r
     for (int j = 0; j < w; ++j) run += sd[1][j];
     int at = INT_MAX, hi = -1;
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) {
+    for (int i = 0; i < DPT; ++i) {
         run += wt[i];
         if (wt[i] > 0.0) {
             hi = v0 + i;
             if (run > goal) at = min(at, v0 + i);
         }
     }
-    if (at != INT_MAX) atomicMin(&first[1], at);
-    if (hi >= 0) atomicMax(&last[1], hi);
+    // one lane of a wave has the wave's lowest, one its highest
+    const uint64_t past = __ballot(at != INT_MAX), any = __ballot(hi >= 0);
+    if (past != 0 && lane == __builtin_ctzll(past)) atomicMin(&first[1], at);
+    if (any != 0 && lane == 63 - __builtin_clzll(any)) atomicMax(&last[1], hi);
     __syncthreads();
     if (tid == 0) drawn[row] = first[1] != INT_MAX ? first[1] : last[1];
 }
@@ -414,6 +434,12 @@ __global__ void __launch_bounds__(64) walk_kernel(VerifyArgs a, int nb, const in
 
 int blocks_of(int V) { return (V + VB - 1) / VB; }
 
+hipError_t launch_rows(const VerifyArgs& a, int nb, hipStream_t st) {
+    if (a.n_rows > 0 && a.c > 0.0) FP_LAUNCH(row_kernel<false>, dim3(nb, a.n_rows), dim3(NT), 0, st, a);
+    else if (a.n_rows > 0) FP_LAUNCH(row_kernel<true>, dim3(nb, a.n_rows), dim3(NT), 0, st, a);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t verify_tree_ws_bytes(int n_rows, int V) { return (size_t)n_rows * (blocks_of(V) * sizeof(Part) + sizeof(int)); }
@@ -421,11 +447,10 @@ size_t verify_tree_ws_bytes(int n_rows, int V) { return (size_t)n_rows * (blocks
 hipError_t launch_verify_tree(const VerifyArgs& a, const int* parent, int* path, hipStream_t st) {
     const int nb = blocks_of(a.V);
     int* drawn = (int*)((Part*)a.ws + (size_t)a.n_rows * nb);
-    if (a.n_rows > 0) FP_LAUNCH(row_kernel, dim3(nb, a.n_rows), dim3(NT), 0, st, a);
-    hipError_t e = hipGetLastError();
+    hipError_t e = launch_rows(a, nb, st);
     if (e != hipSuccess) return e;
     if (a.c > 0.0 && a.n_rows > 0) {
-        FP_LAUNCH(draw_kernel, dim3(a.n_rows), dim3(NT), 0, st, a, nb, drawn);
+        FP_LAUNCH(draw_kernel, dim3(a.n_rows), dim3(DT), 0, st, a, nb, drawn);
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     FP_LAUNCH(walk_kernel, dim3(a.n_seqs), dim3(64), 0, st, a, nb, drawn, parent, path);
@@ -440,8 +465,7 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t st) {
     const int nb = blocks_of(a.V);
     double* mass = (double*)((Part*)a.ws + (size_t)a.n_rows * nb);
     Decision* kept = (Decision*)(mass + (size_t)a.n_seqs * nb * (VB / CK));
-    if (a.n_rows > 0) FP_LAUNCH(row_kernel, dim3(nb, a.n_rows), dim3(NT), 0, st, a);
-    hipError_t e = hipGetLastError();
+    hipError_t e = launch_rows(a, nb, st);
     if (e != hipSuccess) return e;
     if (a.c > 0.0) {
         FP_LAUNCH(mass_kernel, dim3(nb, a.n_seqs), dim3(NT), 0, st, a, mass, kept);

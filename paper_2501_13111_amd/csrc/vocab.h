@@ -1,9 +1,8 @@
 // Sums over a row of logits in 64 bits, for decisions that are borders between such sums: exponentials from a
 // table, sums over a wave, and the weight of a logit with its rules.
 //
-// exp(x) = 2^y, y = x log2 e = n / 32 + r, |r| <= 1 / 64: 2^(n / 32) from a table of 32 and the exponent, 2^r by its
-// power series to the sixth order (the rest is below 4e-18).  A table of 256 with the fourth order takes two operations less,
-// but its entries share the banks of LDS, and a wave's lookups wait for each other.
+// exp(x) = 2^y, y = x log2 e = n / N + r, |r| <= 1 / (2 N): 2^(n / N) from a table of N and the exponent, 2^r by its
+// power series.  N = 256 with the fourth order leaves less than 4e-17, N = 32 with it some 1e-12.
 #pragma once
 #include <climits>
 
@@ -32,38 +31,42 @@ __device__ __forceinline__ double lane_d(double v, int l) {
 }
 __device__ __forceinline__ double wave_sum_d(double v) { return lane_d(wave_scan_d(v), 63); }
 
-// 2^(n / 32), made by the compiler from the power series; a workgroup copies it to LDS (a barrier follows).
-constexpr int EXP_N = 32;
+// 2^(n / N), made by the compiler from the power series; a workgroup copies it to LDS (a barrier follows).
+template <int N>
 struct ExpTable {
-    double v[EXP_N];
+    double v[N];
     constexpr ExpTable() : v() {
-        for (int n = 0; n < EXP_N; ++n) {
-            const double x = n * 0.693147180559945309417 / EXP_N;
+        for (int n = 0; n < N; ++n) {
+            const double x = n * 0.693147180559945309417 / N;
             double s = 0.0;
             for (int k = 24; k >= 1; --k) s = (s + 1.0) * x / k;
             v[n] = 1.0 + s;
         }
     }
 };
-__device__ constexpr ExpTable EXP_TABLE;
-__device__ __forceinline__ void exp_table(double* tab) {
-    if (threadIdx.x < EXP_N) tab[threadIdx.x] = EXP_TABLE.v[threadIdx.x];
+template <int N>
+__device__ constexpr ExpTable<N> EXP_TABLE;
+template <int N>
+__device__ __forceinline__ void exp_table(double (&tab)[N]) {
+    if (threadIdx.x < N) tab[threadIdx.x] = EXP_TABLE<N>.v[threadIdx.x];
 }
-// 2^y for y >= -1022 with ORDER terms of the series
-template <int ORDER>
+constexpr int EXP_N = 256;
+// 2^y for y >= -1022 or so
+template <int N>
 __device__ __forceinline__ double exp2_series(double y, const double* tab) {
-    constexpr double R = 6755399441055744.0 / EXP_N;        // 1.5 2^52 / 32: adding it rounds to 1 / 32
-    constexpr double L = 0.693147180559945309417, C[] = {1.0, L, L * L / 2.0, L * L * L / 6.0, L * L * L * L / 24.0, L * L * L * L * L / 120.0,
-                                                         L * L * L * L * L * L / 720.0};
+    constexpr double R = 6755399441055744.0 / N;            // 1.5 2^52 / N: adding it rounds to 1 / N
     const double t = y + R;
     const int n = __double2loint(t);
     const double r = y - (t - R);
-    double q = C[ORDER];
-#pragma unroll
-    for (int k = ORDER - 1; k >= 0; --k) q = fma(q, r, C[k]);
-    return ldexp(tab[n & (EXP_N - 1)] * q, n >> 5);
+    constexpr double L = 0.693147180559945309417;
+    double q = L * L * L * L / 24.0;
+    q = fma(q, r, L * L * L / 6.0);
+    q = fma(q, r, L * L / 2.0);
+    q = fma(q, r, L);
+    q = fma(q, r, 1.0);
+    return ldexp(tab[n & (N - 1)] * q, n >> (N == 256 ? 8 : 5));
 }
-__device__ __forceinline__ double exp2_d(double y, const double* tab) { return exp2_series<6>(fmax(y, -1200.0), tab); }        // 2^-1200 is zero
+__device__ __forceinline__ double exp2_d(double y, const double* tab) { return exp2_series<EXP_N>(fmax(y, -1200.0), tab); }        // 2^-1200 is zero
 // exp((z - m) / T) with the weight rules: NaN and -inf have none, +inf all of it
 __device__ __forceinline__ double weight(float z, float m, double c, const double* tab) {
     const double e = exp2_d(((double)z - (double)m) * c, tab);
