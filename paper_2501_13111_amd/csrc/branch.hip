@@ -26,14 +26,15 @@ __global__ void __launch_bounds__(T) kv_keep_kernel(KvSet kvs, KvKeepArgs a) {
     const int tid = threadIdx.x, b = blockIdx.x / kv.n_kv_heads, kvh = blockIdx.x % kv.n_kv_heads;
     const Seq sq = load_seq(a.chunk, b);
     if (tid < 64) {
-        const int keep = min(min(a.n_keep[b], a.path_stride), sq.n);
-        const int src = tid < keep ? a.path[(int64_t)b * a.path_stride + tid] : -1;
-        const bool moves = src >= 0 && src < sq.n && src != tid;
-        int pt = -1, ps = -1;
-        if (moves) {
-            pt = pool_block(kv, a.chunk, b, kvh, (sq.ctx + tid) / VT_BLK);
-            ps = pool_block(kv, a.chunk, b, kvh, (sq.ctx + src) / VT_BLK);
-        }
+        // lengths and path together, then both pages of a move: positions below max_len are inside the table
+        const int src = tid < a.path_stride ? a.path[(int64_t)b * a.path_stride + tid] : -1;
+        const int keep = min(a.n_keep[b], sq.n), bpp = kv.page_size / VT_BLK;
+        const bool moves = tid < keep && src >= 0 && src < sq.n && src != tid;
+        const int bt = (sq.ctx + (moves ? tid : 0)) / VT_BLK, bs = (sq.ctx + (moves ? src : 0)) / VT_BLK;
+        const int* row = a.chunk.table + (int64_t)b * a.chunk.table_stride;
+        const int gt = moves ? row[bt / bpp] : -1, gs = moves ? row[bs / bpp] : -1;
+        const int pt = gt >= 0 && gt < kv.n_pages ? (gt * kv.n_kv_heads + kvh) * bpp + bt % bpp : -1;
+        const int ps = gs >= 0 && gs < kv.n_pages ? (gs * kv.n_kv_heads + kvh) * bpp + bs % bpp : -1;
         const uint64_t any = __ballot(pt >= 0);
         if (pt >= 0) {
             const int i = __popcll(any & ((1ull << tid) - 1));
@@ -118,65 +119,12 @@ __device__ __forceinline__ BeamMap beam_map(const ReorderArgs& a, int g) {
 // The group's positions: those of its first beam.
 __device__ __forceinline__ int group_len(const ReorderArgs& a, int g) { return max(a.ctx_len[(int64_t)g * a.n_beams], 0); }
 
-// The partly filled last page of the beam that an extra beam goes on from, copied into its own: workgroups per (extra
-// beam, layer) share its 32-position blocks.  Whole blocks: what lies behind the last position may be anything.
-template <int D, bool KV8>
-__global__ void __launch_bounds__(T) beam_copy_kernel(KvSet kvs, ReorderArgs a) {
-    constexpr int N = VT_BLK * D * (KV8 ? 1 : 2) / 16;     // 16-byte pieces of a block of keys, and of values
-    constexpr int X = (N + T - 1) / T;
-    const fp_paged_kv& kv = kvs.kv[blockIdx.z];
-    const int bpp = kv.page_size / VT_BLK, tid = threadIdx.x;
-    const int g = blockIdx.y / (a.n_beams - 1), e = blockIdx.y % (a.n_beams - 1);
-    const int len = group_len(a, g), col = len / kv.page_size, blocks = (len % kv.page_size + VT_BLK - 1) / VT_BLK;
-    if ((int)blockIdx.x >= blocks * kv.n_kv_heads || col >= a.width) return;
-    const BeamMap m = beam_map(a, g);
-    if (e >= __popcll(m.extra)) return;
-    uint64_t x = m.extra;
-    for (int i = 0; i < e; ++i) x &= x - 1;
-    const int b = __builtin_ctzll(x);
-    const int* t = a.table + (int64_t)g * a.n_beams * a.table_stride + col;
-    const int src = t[(int64_t)__builtin_amdgcn_readlane(m.from, b) * a.table_stride];
-    const int dst = t[(int64_t)__builtin_amdgcn_readlane(m.giver, b) * a.table_stride];
-    if (dst < 0 || dst >= kv.n_pages) return;
-    const bool ok = src >= 0 && src < kv.n_pages;          // a missing page reads as zeros
-    const u32x4 zero = {0u, 0u, 0u, 0u};
-    for (int u = blockIdx.x; u < blocks * kv.n_kv_heads; u += gridDim.x) {
-        const int in = u / blocks * bpp + u % blocks;      // of the page's blocks
-        const int64_t per = (int64_t)kv.n_kv_heads * bpp, from = (ok ? src * per : 0) + in, to = dst * per + in;
-        const u32x4 *ks = (const u32x4*)kv.k + from * N, *vs = (const u32x4*)kv.v + from * N;
-        u32x4 *kd = (u32x4*)kv.k + to * N, *vd = (u32x4*)kv.v + to * N;
-        u32x4 k[X], v[X];
-#pragma unroll
-        for (int i = 0; i < X; ++i) {
-            const int it = tid + T * i;
-            k[i] = ok && it < N ? ks[it] : zero;
-            v[i] = ok && it < N ? vs[it] : zero;
-        }
-#pragma unroll
-        for (int i = 0; i < X; ++i) {
-            const int it = tid + T * i;
-            if (it < N) {
-                kd[it] = k[i];
-                vd[it] = v[i];
-            }
-        }
-        if (KV8 && tid < 2 * VT_BLK / 8) {                 // scales: 64 bytes each
-            uint16_t* s = tid < VT_BLK / 8 ? kv.k_scales : kv.v_scales;
-            const int i = tid % (VT_BLK / 8);
-            ((u32x4*)s)[to * (VT_BLK / 8) + i] = ok ? ((const u32x4*)s)[from * (VT_BLK / 8) + i] : zero;
-        }
-    }
-}
-
-// The table: full pages from the beam that a beam goes on from, the last one from its giver, those behind it its own.
-// A wave takes the group's entries of some columns, all read before any is written: table_out may be the table.
-__global__ void __launch_bounds__(64) beam_table_kernel(int page_size, ReorderArgs a) {
-    const int W = a.n_beams, g = blockIdx.y, lane = threadIdx.x;
+// Sixty-four columns' worth of lanes of group g's table, by one wave: full pages from the beam that a beam goes on from, the
+// last one from its giver, those behind it its own.  All entries are read before any is written: table_out may be the table.
+__device__ __forceinline__ void table_wave(const ReorderArgs& a, int page_size, const BeamMap& m, int g, int chunk, int cols) {
+    const int W = a.n_beams, lane = threadIdx.x & 63;
     const int len = group_len(a, g), full = len / page_size, part = len % page_size != 0;
-    const BeamMap m = beam_map(a, g);
-    int cols = 64;                                         // columns of a wave: 64 / W to a power of two
-    while (cols * W > 64) cols >>= 1;
-    const int w = lane / cols, c = blockIdx.x * cols + lane % cols;
+    const int w = lane / cols, c = chunk * cols + lane % cols;
     const int from = __shfl(m.from, w, 64), giver = __shfl(m.giver, w, 64);
     const bool on = w < W && c < a.width;
     const int64_t row = (int64_t)g * W;
@@ -184,6 +132,87 @@ __global__ void __launch_bounds__(64) beam_table_kernel(int page_size, ReorderAr
     const int up = __shfl(own, from * cols + lane % cols, 64), last = __shfl(own, giver * cols + lane % cols, 64);
     const int v = c < full ? up : c == full && part ? last : own;
     if (on && (v != own || a.table_out != a.table)) a.table_out[(row + w) * a.out_stride + c] = v;
+}
+// Columns of a wave: 64 / n_beams to a power of two.
+__host__ __device__ __forceinline__ int table_cols(int n_beams) {
+    int cols = 64;
+    while (cols * n_beams > 64) cols >>= 1;
+    return cols;
+}
+
+__global__ void __launch_bounds__(64) beam_table_kernel(int page_size, ReorderArgs a) {
+    const BeamMap m = beam_map(a, blockIdx.y);
+    table_wave(a, page_size, m, blockIdx.y, blockIdx.x, table_cols(a.n_beams));
+}
+
+// The partly filled last page of the beam that an extra beam goes on from, copied into its own, and, as one layer more, the table if
+// that goes elsewhere.  The workgroups of a (group, layer) take shares of its copies in turn: 32-position blocks of keys or of
+// values, eight 16-byte loads a thread in flight.  Whole blocks: what lies behind the last position may be anything.  Parents, table
+// and data are a chain of three latencies, so there are no more workgroups than run at a time.  16 groups of 8 beams, 4 layers, int8,
+// 121 MB in random pages: 30 us, 4.0 TB/s (one workgroup for each pair of blocks that might have to be copied 41; the eight loads
+// under a mask, each waiting for the one before, 58).
+template <int D, bool KV8>
+__global__ void __launch_bounds__(T) beam_copy_kernel(KvSet kvs, ReorderArgs a) {
+    constexpr int N = VT_BLK * D * (KV8 ? 1 : 2) / 16;     // 16-byte pieces of a block of keys or of values
+    constexpr int TPB = N < T ? N : T, PX = N / TPB;       // threads of a block, pieces of a thread
+    constexpr int SIDE = T / TPB, X = 8 / PX;              // blocks side by side, and after each other
+    const int tid = threadIdx.x, ps = kvs.kv[0].page_size, bpp = ps / VT_BLK, g = blockIdx.y;
+    const int len = group_len(a, g), col = len / ps;
+    const BeamMap m = beam_map(a, g);
+    if ((int)blockIdx.z == kvs.n) {
+        const int cols = table_cols(a.n_beams);
+        for (int c = blockIdx.x * (T / 64) + (tid >> 6); c * cols < a.width; c += gridDim.x * (T / 64)) table_wave(a, ps, m, g, c, cols);
+        return;
+    }
+    const fp_paged_kv& kv = kvs.kv[blockIdx.z];
+    const int blocks = (len % ps + VT_BLK - 1) / VT_BLK, all = 2 * blocks * kv.n_kv_heads;      // of keys and values, of a copy
+    const int shares = (all + X * SIDE - 1) / (X * SIDE), items = __popcll(m.extra) * shares;
+    if ((int)blockIdx.x >= items || col >= a.width) return;
+    // lane b: the pages of beam b's copy
+    const int lane = tid & 63;
+    const int* t = a.table + (int64_t)g * a.n_beams * a.table_stride + col;
+    int from_page = -1, to_page = -1;
+    if (m.extra >> lane & 1) {
+        from_page = t[(int64_t)m.from * a.table_stride];
+        to_page = t[(int64_t)m.giver * a.table_stride];
+    }
+    for (int it = blockIdx.x; it < items; it += gridDim.x) {
+        uint64_t x = m.extra;
+        for (int i = it / shares; i > 0; --i) x &= x - 1;
+        const int b = __builtin_ctzll(x), i0 = it % shares * (X * SIDE);
+        const int src = __builtin_amdgcn_readlane(from_page, b), dst = __builtin_amdgcn_readlane(to_page, b);
+        if (dst < 0 || dst >= kv.n_pages) continue;
+        const bool ok = src >= 0 && src < kv.n_pages;      // a missing page reads as zeros
+        const int64_t per = (int64_t)kv.n_kv_heads * bpp, from = ok ? src * per : 0, to = dst * per;      // in blocks
+        // Block i of the copy, of keys if even: its data and scales at `page` of the pool, nothing past the last.  (Loads and stores
+        // past a resource's end do nothing: no branch around one, at whose end the loads before it would be waited for.)
+        auto data = [&](int i, int64_t page, bool on) {
+            const int64_t at = page + (i >> 1) / blocks * bpp + (i >> 1) % blocks;
+            return buf_rsrc((const u32x4*)(i & 1 ? kv.v : kv.k) + (on ? at * N : 0), on ? 16 * N : 0);
+        };
+        auto scale = [&](int i, int64_t page, bool on) {
+            const int64_t at = page + (i >> 1) / blocks * bpp + (i >> 1) % blocks;
+            return buf_rsrc((i & 1 ? kv.v_scales : kv.k_scales) + (on ? at * VT_BLK : 0), on ? 2 * VT_BLK : 0);
+        };
+        const int i1 = __builtin_amdgcn_readfirstlane(i0 + tid / TPB), q = tid % TPB;
+        u32x4 v[X][PX], sc[X];
+#pragma unroll
+        for (int k = 0; k < X; ++k) {
+            const int i = i1 + k * SIDE;
+            const auto r = data(i, from, ok && i < all);
+#pragma unroll
+            for (int y = 0; y < PX; ++y) v[k][y] = __builtin_amdgcn_raw_buffer_load_b128(r, 16 * (q + TPB * y), 0, 0);
+            if (KV8) sc[k] = __builtin_amdgcn_raw_buffer_load_b128(scale(i, from, ok && i < all), 16 * q, 0, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < X; ++k) {
+            const int i = i1 + k * SIDE;
+            const auto r = data(i, to, i < all);
+#pragma unroll
+            for (int y = 0; y < PX; ++y) __builtin_amdgcn_raw_buffer_store_b128(v[k][y], r, 16 * (q + TPB * y), 0, 0);
+            if (KV8) __builtin_amdgcn_raw_buffer_store_b128(sc[k], scale(i, to, i < all), 16 * q, 0, 0);
+        }
+    }
 }
 
 }  // namespace
@@ -206,19 +235,19 @@ hipError_t launch_kv_keep(const KvSet& kvs, const KvKeepArgs& a, hipStream_t st)
     return hipGetLastError();
 }
 
-hipError_t launch_beam_copy(const KvSet& kvs, const ReorderArgs& a, hipStream_t st) {
+hipError_t launch_beam_copy(const KvSet& kvs, const ReorderArgs& a, bool table, hipStream_t st) {
     const fp_paged_kv& kv = kvs.kv[0];
-    const int64_t y = (int64_t)a.n_groups * (a.n_beams - 1);
-    if (y == 0) return hipSuccess;
-    if (y > 65535) return hipErrorInvalidValue;
-    const int64_t x = std::min<int64_t>((int64_t)kv.n_kv_heads * (kv.page_size / VT_BLK), std::max<int64_t>(8, 16384 / y));
-    FP_SET(beam_copy_kernel, dim3((unsigned)x, (unsigned)y, kvs.n), a);
+    if (a.n_beams < 2) return hipErrorInvalidValue;
+    // eight blocks of 4 KB, four of 8, and so on, are what a workgroup takes at a time
+    const int64_t share = 32768 / (VT_BLK * kv.head_dim * (kv.format == FP_KV_INT8 ? 1 : 2));
+    const int64_t most = (2ll * kv.n_kv_heads * (kv.page_size / VT_BLK) + share - 1) / share * (a.n_beams - 1);
+    const int64_t x = std::min<int64_t>(most, std::max<int64_t>(1, 1280 / ((int64_t)a.n_groups * kvs.n)));
+    FP_SET(beam_copy_kernel, dim3((unsigned)x, a.n_groups, kvs.n + (table ? 1 : 0)), a);
     return hipGetLastError();
 }
 
 hipError_t launch_beam_table(int page_size, const ReorderArgs& a, hipStream_t st) {
-    int cols = 64;
-    while (cols * a.n_beams > 64) cols >>= 1;
+    const int cols = table_cols(a.n_beams);
     FP_LAUNCH(beam_table_kernel, dim3((a.width + cols - 1) / cols, a.n_groups), dim3(64), 0, st, page_size, a);
     return hipGetLastError();
 }

@@ -354,7 +354,7 @@ struct ReorderArgs {
     const int* parent;
     int* table_out;           // table itself, or apart from it
 };
-hipError_t launch_beam_copy(const KvSet& kvs, const ReorderArgs& a, hipStream_t st);
+hipError_t launch_beam_copy(const KvSet& kvs, const ReorderArgs& a, bool table, hipStream_t st);      // n_beams > 1; table: it too
 hipError_t launch_beam_table(int page_size, const ReorderArgs& a, hipStream_t st);
 
 // Selection over beams and vocabulary (beam.hip).

@@ -424,11 +424,11 @@ fp_status fp_beam_select(const float* logits, int64_t row_stride, int32_t n_grou
     return done(launch_beam_select(a, (hipStream_t)stream), "beam selection");
 }
 
-fp_status fp_beam_reorder(const fp_paged_kv* kv, int32_t n_layers, int32_t n_groups, int32_t n_beams, const int32_t* table,
+fp_status fp_beam_reorder(const fp_paged_kv* kv, int32_t n_layers, int32_t n_groups, int32_t n_beams, const int32_t* table_in,
                           int32_t table_stride, int32_t width, const int32_t* ctx_len, const int32_t* parent,
                           int32_t* table_out, int32_t out_stride, void* stream) {
     if (const fp_status s = check_beams(n_groups, n_beams)) return s;
-    if (!table || !ctx_len || !parent || !table_out)
+    if (!table_in || !ctx_len || !parent || !table_out)
         return fail(FP_ERR_INVALID_ARG, "table, ctx_len, parent and table_out must be device pointers");
     if (width < 1 || table_stride < width || out_stride < width)
         return fail(FP_ERR_INVALID_ARG, "table rows of %d pages are %d apart, table_out's %d", width, table_stride, out_stride);
@@ -437,11 +437,11 @@ fp_status fp_beam_reorder(const fp_paged_kv* kv, int32_t n_layers, int32_t n_gro
     c.n_seqs = c.max_new = c.max_len = 1;
     c.table_stride = table_stride;
     c.row_start = c.ctx_len = ctx_len;
-    c.table = table;
+    c.table = table_in;
     if (const fp_status s = check_layers(kv, n_layers, &c)) return s;
     const size_t last = (size_t)n_groups * n_beams - 1;
-    if (table_out == table ? table_stride != out_stride
-                           : overlap(table, 4 * (last * table_stride + width), table_out, 4 * (last * out_stride + width)))
+    if (table_out == table_in ? table_stride != out_stride
+                           : overlap(table_in, 4 * (last * table_stride + width), table_out, 4 * (last * out_stride + width)))
         return fail(FP_ERR_INVALID_ARG, "table_out is neither the table nor apart from it");
     ReorderArgs a{};
     a.n_groups = n_groups;
@@ -449,13 +449,20 @@ fp_status fp_beam_reorder(const fp_paged_kv* kv, int32_t n_layers, int32_t n_gro
     a.width = width;
     a.table_stride = table_stride;
     a.out_stride = out_stride;
-    a.table = table;
+    a.table = table_in;
     a.ctx_len = ctx_len;
     a.parent = parent;
     a.table_out = table_out;
-    // the copies read the table as it was
-    hipError_t e = each_set(kv, n_layers, [&](const KvSet& set) { return launch_beam_copy(set, a, (hipStream_t)stream); });
-    if (e == hipSuccess) e = launch_beam_table(kv->page_size, a, (hipStream_t)stream);
+    // the copies read the table as it was: written elsewhere, it is written beside the first of them, else after them
+    bool table = table_out != table_in;
+    hipError_t e = hipSuccess;
+    if (n_beams > 1)
+        e = each_set(kv, n_layers, [&](const KvSet& set) {
+            const hipError_t r = launch_beam_copy(set, a, table, (hipStream_t)stream);
+            table = false;
+            return r;
+        });
+    if (e == hipSuccess && (n_beams == 1 || table_out == table_in)) e = launch_beam_table(kv->page_size, a, (hipStream_t)stream);
     return done(e, "beam reordering");
 }
 
