@@ -195,7 +195,7 @@ int tile_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
 }
 
 // The same for trees: as chunks, but 65 to 128 rows of 128 dims in calls that are large enough for tiles of 256 take those of
-// attn_wide.hip.  us, 64 heads on 8, 16 nodes of 32 sequences of up to 8192: bf16 156, in tiles of 256 225, of 64 216; int8 164, 279, of 32
+// attn_wide.hip.  us, 64 heads on 8, 16 nodes of 32 sequences of up to 8192: bf16 149, in tiles of 256 225, of 64 216; int8 150, 279, of 32
 // 202.  (256 rows and more, in pairs of such tiles or tiles of 256 made the same way: no faster than attn_tile.hip's, 8 sequences of up to 30001 with
 // 512 rows to a kv head, bf16 69 and 61 against 61.  48 rows: int8 183, in tiles of 32 94; bf16 161, in tiles of 64 134.)
 int tree_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {

@@ -82,7 +82,7 @@ __device__ __forceinline__ int plan_all(const AttnChunkArgs& a, int64_t total, i
     const float round = (float)(1 << a.target), nt = (float)tiles * (float)a.kv.n_kv_heads;
     if constexpr ((RT & WIDE) != 0) {
         // Few tiles: one round of equal pieces.  Many: two rounds, so that a long tile does not outlast the others (32 sequences
-        // of up to 8192, 8 kv heads, int8, 16 nodes: 164 us; aiming for one round 208).  At most WIDE_PIECES come of it: the
+        // of up to 8192, 8 kv heads, int8, 16 nodes: 139 us; aiming for one round 160).  At most WIDE_PIECES come of it: the
         // aim, and one more for each tile that is split.
         const float aim = nt <= 128.f ? 256.f - 0.5f * nt : fmaxf(512.f - 0.5f * nt, 256.f);
         return std::max(a.min_blocks, (int)fminf((float)total * (float)a.kv.n_kv_heads / aim, 2.5e8f) + 1);

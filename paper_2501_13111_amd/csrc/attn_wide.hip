@@ -5,9 +5,10 @@
 // Rows, units and the join of their pieces are those of attn_chunk.hip, the mask is the tree's (tree.h).  A step takes two blocks
 // of 32 keys: wave w the rows 32 (w % 4) .. and of the two blocks the w / 4-th; the two sums of a row are merged at the end.
 //     S^T = K Q^T,   O^T += V^T P^T      on MFMA 32x32x16
-// Two waves share a SIMD, w and w + 4, half a step apart: one multiplies (P V of its last block, then S of this one) while the other
-// takes its softmax, a barrier after each half.  Blocks pass through registers into LDS, as 16-bit fragments (int8: codes times
-// scales in fp16), loaded two steps before they are stored.
+// Two waves share a SIMD, w and w + 4: one multiplies first (P V of its last block, then S of this one), stores and takes its softmax, the
+// other stores, takes the softmax of its last block and multiplies then.  One barrier a step (with one after each half, the waves
+// half a step apart: 32 sequences of 8192, 16 nodes, 64 heads on 8, int8 264 us, so 241; bf16 258 and 253).  Blocks pass
+// through registers into LDS, as 16-bit fragments (int8: codes times scales in fp16), loaded two steps before they are stored.
 #include <type_traits>
 
 #include "attn_stream.h"
@@ -283,12 +284,9 @@ __global__ void __launch_bounds__(512, 2) attn_wide_kernel(AttnChunkArgs a) {
     };
     auto meet = []() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-    // Step s sits in slot s % 3.  In the half in which waves 0 to 3 multiply step s the others (`late`) take the softmax of s - 1, in the
-    // next they multiply s.  So s + 1 may be stored by waves 0 to 3 while the others still multiply s and the values of s - 1, and
-    // s + 2 by the others once s - 1 is done with.
+    // Step s sits in slot s % 3, s + 1 is stored while s is multiplied: in a slot that was done with before the barrier.
     auto run = [&](auto late, auto keys) {
         constexpr bool LATE = decltype(late)::value;
-        constexpr int PH = LATE ? 1 : 0;
         auto put = [&](char* slot, int s, const Raw& r) {
             if (s * KP + KP > edge) store(slot, s, r, keys, Yes{});
             else store(slot, s, r, keys, No{});
@@ -296,34 +294,29 @@ __global__ void __launch_bounds__(512, 2) attn_wide_kernel(AttnChunkArgs a) {
         // the values before step 0: zeros, times zero probabilities
         for (int x = tid; x < KP * NKC * 64; x += 512) *(u32x4*)(lds.ring + 2 * ST + x / (NKC * 64) * SB + NKC * 1024 + x % (NKC * 64) * 16) = u32x4{0u, 0u, 0u, 0u};
         put(lds.ring, 0, r0);
-        if constexpr (LATE) {
-            fetch(2, r0, keys);
-            put(lds.ring + ST, 1, r1);
-            fetch(3, r1, keys);
-        } else {
-            fetch(2, r0, keys);
-        }
+        fetch(2, r0, keys);
         meet();
-        if constexpr (LATE) meet();
         int at = 0;                                            // of step s
         auto step = [&](int s, Raw& r) {
             const int before = at == 0 ? 2 * ST : at - ST, after = at == 2 * ST ? 0 : at + ST;
-            both(before, at);
-            meet();
-            if (s + 1 + PH < steps) put(lds.ring + (LATE ? before : after), s + 1 + PH, r);
-            fetch(s + 3 + PH, r, keys);
-            softmax(s * KP + kp);
+            if (!LATE) both(before, at);
+            if (s + 1 < steps) put(lds.ring + after, s + 1, r);
+            fetch(s + 3, r, keys);
+            if (!LATE) softmax(s * KP + kp);
+            if (LATE) {
+                if (s > 0) softmax((s - 1) * KP + kp);
+                both(before, at);
+            }
             meet();
             at = after;
         };
-        Raw &ra = LATE ? r0 : r1, &rb = LATE ? r1 : r0;        // of steps s + 1 + PH with s even, and odd
         int s = 0;
         for (; s + 1 < steps; s += 2) {
-            step(s, ra);
-            step(s + 1, rb);
+            step(s, r1);
+            step(s + 1, r0);
         }
-        if (s < steps) step(s, ra);
-        if constexpr (!LATE) meet();
+        if (s < steps) step(s, r1);
+        if (LATE) softmax((steps - 1) * KP + kp);
         values(at == 0 ? 2 * ST : at - ST);
     };
     if (n > 0) {
@@ -349,20 +342,24 @@ __global__ void __launch_bounds__(512, 2) attn_wide_kernel(AttnChunkArgs a) {
     int any = 0;
 #pragma unroll
     for (int x = 0; x < 8; ++x) any |= lds.sw[x];
+    // a row's factors once, by a thread: of its two sums, and the whole's reference and sum
+    float m = M0, l = 0.f;
+    if (tid < RT) {
+        const float m0 = lds.mw[tid], m1 = lds.mw[RT + tid];
+        m = fmaxf(m0, m1);
+        const float e0 = __builtin_amdgcn_exp2f(m0 - m), e1 = __builtin_amdgcn_exp2f(m1 - m);
+        l = lds.lw[tid] * e0 + lds.lw[RT + tid] * e1;
+        const float f = un.pieces == 1 && !any ? 1.f / l : 1.f;
+        lds.mw[tid] = e0 * f;
+        lds.mw[RT + tid] = e1 * f;
+        lds.lw[tid] = l;
+        if (un.pieces > 1 && tid < rows) *(f32x2*)(a.ws + ((int64_t)un.part * RT + tid) * wst(D) + D) = f32x2{m, l};
+    }
+    __syncthreads();
 #pragma unroll 4
     for (int it = tid; it < rows * (D / 4); it += 512) {
         const int c = it / (D / 4), d0 = it % (D / 4) * 4;
-        float m = M0;
-#pragma unroll
-        for (int v = 0; v < KP; ++v) m = fmaxf(m, lds.mw[v * RT + c]);
-        float l = 0.f;
-        f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int v = 0; v < KP; ++v) {
-            const float e = __builtin_amdgcn_exp2f(lds.mw[v * RT + c] - m);
-            l += lds.lw[v * RT + c] * e;
-            x += *(const f32x4*)&lds.ow[(v * RT + c) * RS + d0] * e;
-        }
+        f32x4 x = *(const f32x4*)&lds.ow[c * RS + d0] * lds.mw[c] + *(const f32x4*)&lds.ow[(RT + c) * RS + d0] * lds.mw[RT + c];
         const int r = row0 + c;
         if (any) {
 #pragma unroll 1
@@ -373,11 +370,10 @@ __global__ void __launch_bounds__(512, 2) attn_wide_kernel(AttnChunkArgs a) {
             }
         }
         if (un.pieces == 1) {
-            store4(a.out + ((int64_t)(sq.row0 + r / G) * a.n_heads + kvh * G + r % G) * D + d0, x * (1.f / l), a.out_fmt);
+            if (any) x *= 1.f / lds.lw[c];
+            store4(a.out + ((int64_t)(sq.row0 + r / G) * a.n_heads + kvh * G + r % G) * D + d0, x, a.out_fmt);
         } else {
-            float* dst = a.ws + ((int64_t)un.part * RT + c) * wst(D);
-            *(f32x4*)(dst + d0) = x;
-            if (d0 == 0) *(f32x2*)(dst + D) = f32x2{m, l};
+            *(f32x4*)(a.ws + ((int64_t)un.part * RT + c) * wst(D) + d0) = x;
         }
     }
 }
