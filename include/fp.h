@@ -414,6 +414,7 @@ fp_status fp_extend_tree(fp_layer* layer, const fp_paged_kv* kv, const fp_chunk*
  * shape, the nodes of the path from the root (0) on, -1 behind; n_out: device int32 [n_seqs], the number of either (a
  * sequence without rows: 0).  fp_kv_keep takes path and n_out as they are, and ctx_len grows by n_out.
  * Logits, row_start and the limits are as for fp_verify_draft; a row without any probability draws -1, which no child holds.
+ * Outputs overlap neither inputs nor each other.
  */
 fp_status fp_verify_tree_workspace(int32_t n_seqs, int32_t n_rows, int32_t vocab, size_t* bytes);
 fp_status fp_verify_tree(const float* logits, int64_t row_stride, int32_t n_seqs, int32_t n_rows, int32_t max_rows, int32_t vocab,
@@ -442,7 +443,8 @@ fp_status fp_kv_keep(const fp_paged_kv* kv, int32_t n_layers, const fp_chunk* ch
  * finished or its id is eos_id; eos_id -1: no id is), all [n_groups, n_best]; where there are fewer, -inf, -1, -1 and 0.
  * Sums and comparisons are in 64 bits.  -inf and NaN logits are no continuation, +inf ones share the whole; a beam of
  * score -inf or NaN has none.  With n_beams 1 and n_best the beams to come, a request's first step.
- * 1 <= n_beams, n_best <= 64, n_groups * n_beams <= 65535, 1 <= vocab <= 2^20.  Outputs do not overlap inputs.
+ * 1 <= n_beams, n_best <= 64, n_groups * n_beams <= 65535, 1 <= vocab <= 2^20.  Outputs overlap neither
+ * inputs nor each other.
  */
 fp_status fp_beam_select_workspace(int32_t n_groups, int32_t n_beams, int32_t n_best, int32_t vocab, size_t* bytes);
 fp_status fp_beam_select(const float* logits, int64_t row_stride, int32_t n_groups, int32_t n_beams, int32_t n_best, int32_t vocab,
@@ -453,7 +455,7 @@ fp_status fp_beam_select(const float* logits, int64_t row_stride, int32_t n_grou
 /*
  * Beams go on from other beams' caches: beam b of a group from beam parent[b] (device int32 [n_groups, n_beams]; out of
  * range: from itself).  table: device int32, row g * n_beams + b the pages of beam b of group g; ctx_len: device int32 [n_groups * n_beams],
- * of which a group's first is read: its beams have one length.  Row b of table_out (table itself, or apart from it):
+ * of which a group's first is read: its beams have one length.  Row b of table_out (table itself, or apart from it; apart from parent and ctx_len):
  *   full pages        those of parent[b]: they are shared from then on, and nothing writes them any more;
  *   the last page     if it is partly filled, parent[b]'s for the first of the beams that go on from it; the others take, in
  *                     order, the last pages of the beams that none goes on from, and parent[b]'s page is copied there

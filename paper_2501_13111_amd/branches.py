@@ -46,7 +46,8 @@ def kv_keep(kvs, chunk: Chunk, path, n_keep, stream=None):
 
 
 def verify_tree_workspace(n_rows: int, vocab: int, device="cuda"):
-    """A workspace for verify_tree calls of up to n_rows rows."""
+    """A workspace for verify_tree calls of up to n_rows rows.  Calls that may overlap (other streams, graphs
+    replayed side by side) need one each."""
     n = ctypes.c_size_t()
     _check(load().fp_verify_tree_workspace(1, int(n_rows), int(vocab), ctypes.byref(n)), "fp_verify_tree_workspace")
     return torch.empty(max(n.value, 16), dtype=torch.uint8, device=device)
@@ -87,7 +88,7 @@ def verify_tree(logits, row_start, parent, ids, u, out_ids, path, n_out, tempera
 
 
 def beam_select_workspace(n_groups: int, n_beams: int, n_best: int, vocab: int, device="cuda"):
-    """A workspace for beam_select calls of these sizes."""
+    """A workspace for beam_select calls of these sizes.  Calls that may overlap need one each."""
     n = ctypes.c_size_t()
     _check(load().fp_beam_select_workspace(int(n_groups), int(n_beams), int(n_best), int(vocab), ctypes.byref(n)),
            "fp_beam_select_workspace")

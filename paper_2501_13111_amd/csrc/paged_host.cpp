@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <initializer_list>
 
 #include "fp_internal.h"
 
@@ -125,6 +126,22 @@ fp_status check_rows(const char* name, const void* p, int64_t stride, int64_t wi
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     return (const char*)a < (const char*)b + nb && (const char*)b < (const char*)a + na;
+}
+
+// Whether every output is apart from the inputs and the other outputs.
+struct Bytes {
+    const void* p;
+    size_t n;
+};
+bool apart(std::initializer_list<Bytes> outs, std::initializer_list<Bytes> ins) {
+    auto meet = [](const Bytes& a, const Bytes& b) { return a.n > 0 && b.n > 0 && overlap(a.p, a.n, b.p, b.n); };
+    for (const Bytes& o : outs) {
+        for (const Bytes& i : ins)
+            if (meet(o, i)) return false;
+        for (const Bytes& i : outs)
+            if (&i != &o && meet(o, i)) return false;
+    }
+    return true;
 }
 
 // bytes from the first element of strided rows to the last one's end
@@ -344,6 +361,11 @@ fp_status fp_verify_tree(const float* logits, int64_t row_stride, int32_t n_seqs
         if (row_stride < vocab) return fail(FP_ERR_INVALID_ARG, "logits rows are %lld apart, vocab is %d", (long long)row_stride, vocab);
         if (temperature > 0.f && !u) return fail(FP_ERR_INVALID_ARG, "u must be a device pointer");
     }
+    const size_t rows = (size_t)n_rows, room = 4 * (size_t)n_seqs * max_rows;
+    if (!apart({{out_ids, room}, {path, room}, {n_out, 4 * (size_t)n_seqs}},
+               {{logits, rows > 0 ? 4 * ((rows - 1) * (size_t)row_stride + vocab) : 0}, {row_start, 4 * ((size_t)n_seqs + 1)},
+                {parent, 4 * rows}, {node_ids, 4 * rows}, {u, u ? 4 * rows : 0}}))
+        return fail(FP_ERR_INVALID_ARG, "an output overlaps an input or another output");
     const size_t need = verify_tree_ws_bytes(n_rows, vocab);
     if (need > 0 && (!workspace || !aligned(workspace, 16))) return fail(FP_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device pointer");
     if (workspace_bytes < need) return fail(FP_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
@@ -394,14 +416,9 @@ fp_status fp_beam_select(const float* logits, int64_t row_stride, int32_t n_grou
         return fail(FP_ERR_INVALID_ARG, "logits, scores, out_scores, out_parent and out_ids must be device pointers");
     if (row_stride < vocab) return fail(FP_ERR_INVALID_ARG, "logits rows are %lld apart, vocab is %d", (long long)row_stride, vocab);
     const size_t rows = (size_t)n_groups * n_beams, best = (size_t)n_groups * n_best;
-    const struct {
-        const void* p;
-        size_t n;
-    } in[] = {{logits, 4 * ((rows - 1) * (size_t)row_stride + vocab)}, {scores, 4 * rows}, {finished, finished ? rows : 0}},
-      out[] = {{out_scores, 4 * best}, {out_parent, 4 * best}, {out_ids, 4 * best}, {out_finished, out_finished ? best : 0}};
-    for (const auto& o : out)
-        for (const auto& i : in)
-            if (overlap(o.p, o.n, i.p, i.n)) return fail(FP_ERR_INVALID_ARG, "an output overlaps an input");
+    if (!apart({{out_scores, 4 * best}, {out_parent, 4 * best}, {out_ids, 4 * best}, {out_finished, out_finished ? best : 0}},
+               {{logits, 4 * ((rows - 1) * (size_t)row_stride + vocab)}, {scores, 4 * rows}, {finished, finished ? rows : 0}}))
+        return fail(FP_ERR_INVALID_ARG, "an output overlaps an input or another output");
     const size_t need = beam_ws_bytes(n_groups * n_beams, n_best, vocab);
     if (!workspace || !aligned(workspace, 16)) return fail(FP_ERR_INVALID_ARG, "workspace must be a 16-byte aligned device pointer");
     if (workspace_bytes < need) return fail(FP_ERR_CAPACITY, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
@@ -443,6 +460,8 @@ fp_status fp_beam_reorder(const fp_paged_kv* kv, int32_t n_layers, int32_t n_gro
     if (table_out == table_in ? table_stride != out_stride
                            : overlap(table_in, 4 * (last * table_stride + width), table_out, 4 * (last * out_stride + width)))
         return fail(FP_ERR_INVALID_ARG, "table_out is neither the table nor apart from it");
+    if (!apart({{table_out, 4 * (last * out_stride + width)}}, {{ctx_len, 4 * (last + 1)}, {parent, 4 * (last + 1)}}))
+        return fail(FP_ERR_INVALID_ARG, "table_out overlaps ctx_len or parent");
     ReorderArgs a{};
     a.n_groups = n_groups;
     a.n_beams = n_beams;

@@ -112,8 +112,8 @@ def test_tree_extends_that_are_refused(lib):
 
 
 def verify(lib, **kw):
-    a = dict(logits=P, stride=100, n_seqs=2, n_rows=6, max_rows=4, vocab=100, row_start=P, parent=P, ids=P, u=P, T=1.0, out=P, path=P,
-             n_out=P, ws=P, n=1 << 40)
+    a = dict(logits=P, stride=100, n_seqs=2, n_rows=6, max_rows=4, vocab=100, row_start=8 * P, parent=9 * P, ids=10 * P, u=11 * P, T=1.0,
+             out=12 * P, path=13 * P, n_out=14 * P, ws=P, n=1 << 40)
     a.update(kw)
     return lib.fp_verify_tree(*a.values(), None)
 
@@ -125,6 +125,8 @@ def verify(lib, **kw):
     (dict(logits=None), INVALID), (dict(row_start=None), INVALID), (dict(parent=None), INVALID), (dict(ids=None), INVALID),
     (dict(out=None), INVALID), (dict(path=None), INVALID), (dict(n_out=None), INVALID), (dict(u=None), INVALID), (dict(stride=99), INVALID),
     (dict(ws=None), INVALID), (dict(ws=P + 4), INVALID), (dict(n=16), CAPACITY),
+    (dict(out=10 * P), INVALID), (dict(path=9 * P + 20), INVALID), (dict(n_out=P + 4 * 599), INVALID), (dict(n_out=8 * P + 8), INVALID),
+    (dict(path=12 * P + 28), INVALID), (dict(n_out=12 * P), INVALID), (dict(out=11 * P), INVALID),
 ])
 def test_tree_verifications_that_are_refused(lib, bad, code):
     assert verify(lib, **bad) == code
@@ -149,7 +151,7 @@ def select(lib, **kw):
     (dict(groups=65536, beams=1), UNSUPPORTED), (dict(logits=None), INVALID), (dict(scores=None), INVALID), (dict(os=None), INVALID),
     (dict(op=None), INVALID), (dict(oi=None), INVALID), (dict(stride=999), INVALID), (dict(ws=None), INVALID), (dict(ws=P + 8), INVALID),
     (dict(n=256), CAPACITY), (dict(os=8 * P + 44), INVALID), (dict(oi=P + 4 * 11000), INVALID), (dict(od=9 * P + 11), INVALID),
-    (dict(op=9 * P), INVALID),
+    (dict(op=9 * P), INVALID), (dict(oi=10 * P + 92), INVALID), (dict(od=11 * P + 95), INVALID),
 ])
 def test_selections_that_are_refused(lib, bad, code):
     assert select(lib, **bad) == code
@@ -173,7 +175,7 @@ def reorder(lib, pools=None, **kw):
     (dict(groups=1024, beams=64), UNSUPPORTED), (dict(table=None), INVALID), (dict(ctx=None), INVALID), (dict(parent=None), INVALID),
     (dict(out=None), INVALID), (dict(width=0), INVALID), (dict(stride=3), INVALID), (dict(out_stride=3), INVALID),
     (dict(out=P), INVALID),                                     # the table, with other rows
-    (dict(out=P + 8, out_stride=5), INVALID),
+    (dict(out=P + 8, out_stride=5), INVALID), (dict(out=2 * P + 20), INVALID), (dict(out=3 * P - 92), INVALID),
     (dict(pools=[kv(), kv(page_size=32)]), INVALID), (dict(pools=[kv(k=None)]), INVALID), (dict(pools=[kv(head_dim=80)]), UNSUPPORTED),
 ])
 def test_reorderings_that_are_refused(lib, bad, code):

@@ -338,3 +338,33 @@ def test_captured_beams_follow_their_contents():
         for s in sides[:2]:
             for a, b in zip(s.state(), sides[2].state()):
                 assert torch.equal(ref.bits(a), ref.bits(b)), it
+
+
+def test_beams_on_another_stream():
+    """On a stream of the caller's, with a workspace of its own; without one another stream is refused."""
+    fp = _fp()
+    G, W, V, page = 2, 4, 5000, 32
+    g = torch.Generator().manual_seed(8)
+    z, s = torch.randn(G * W, V, generator=g).cuda(), torch.randn(G, W, generator=g).cuda()
+    kv = fp.PagedKV.empty(20, page, 2, 64, "int8")
+    for t in (kv.k, kv.v):
+        t.random_(-127, 127)
+    for t in (kv.k_scales, kv.v_scales):
+        t.uniform_(0.1, 1)
+    start = [t.clone() for t in (kv.k, kv.v, kv.k_scales, kv.v_scales)]
+    ctx, st = _int([40] * G * W), torch.cuda.Stream()
+    ws = fp.beam_select_workspace(G, W, W, V)
+    got = []
+    for stream in (None, st):
+        for t, x in zip((kv.k, kv.v, kv.k_scales, kv.v_scales), start):
+            t.copy_(x)
+        os, op, oi, table = torch.zeros(G, W).cuda(), _int([[7] * W] * G), _int([[7] * W] * G), _int([[2 * i, 2 * i + 1] for i in range(G * W)])
+        torch.cuda.synchronize()
+        fp.beam_select(z, s, os, op, oi, workspace=ws, stream=stream)
+        fp.beam_reorder(kv, table, ctx, op, stream=stream)
+        torch.cuda.synchronize()
+        got.append([os, op, oi, table] + [t.clone() for t in (kv.k, kv.v, kv.k_scales, kv.v_scales)])
+    for a, b in zip(*got):
+        assert torch.equal(ref.bits(a.cpu()), ref.bits(b.cpu()))
+    with pytest.raises(ValueError, match="workspace"):
+        fp.beam_select(z, s, os, op, oi, stream=st)

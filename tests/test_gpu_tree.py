@@ -653,3 +653,48 @@ def test_trees_on_another_stream():
         fp.verify_tree(lg, chunk.row_start, pp, ids, None, o, h, n, temperature=0, stream=st)
     with pytest.raises(ValueError, match="path"):
         fp.verify_tree(lg, chunk.row_start, pp, ids, None, o, h[:, 1:], n, temperature=0)
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
+def test_pages_past_32_bits_of_bytes(kvq):
+    """Append, attention (16 nodes: streamed, in tiles of 64 or 32, and of 128), the move and the beams' copies among the last pages of
+    a pool above 4 GiB leave the same bits as in a small pool."""
+    fp = _fp()
+    lens, page, nkv, d = [(700, 16), (300, 12), (0, 16), (1000, 7)], 256, 8, 128
+    g, pool, table = paged._case(lens, page, nkv, d, kvq, 71)
+    paged._fill(pool, table, lens, g, upto=lambda c, n: c + n)
+    parent = _int(_trees(g, lens))
+    N = sum(n for _, n in lens)
+    small = pool.device()
+    n = small.n_pages
+    big = fp.PagedKV.empty((9 << 29) // (nkv * page * d * small.k.element_size()), page, nkv, d, kvq)
+    assert big.k.nbytes > 1 << 32
+    hi = big.n_pages - n
+
+    def held(kv, at):
+        ts = [kv.k, kv.v] + ([kv.k_scales, kv.v_scales] if kvq == "int8" else [])
+        return [t[at:at + n] for t in ts]
+
+    for a, b in zip(held(small, 0), held(big, hi)):
+        b.copy_(a)
+    cos, sin = torch.rand(2, 1100, d // 2, generator=g).cuda()
+    k, v = torch.randn(2, N, nkv, d, generator=g).bfloat16().cuda()
+    out = []
+    for kv, at in ((small, 0), (big, hi)):
+        tab = torch.where((table >= 0) & (table < n), table + at, -1).int()
+        res = []
+        for G in (1, 2, 8):
+            q = torch.randn(N, nkv * G, d, generator=torch.Generator().manual_seed(G)).bfloat16().cuda()
+            qr = torch.empty_like(q)
+            fp.kv_append(kv, paged._chunk(lens, tab)[0], k, v, q=q, q_out=qr, cos=cos, sin=sin, parent=parent)
+            res.append(qr)
+            for loose in (0, page):
+                o = torch.empty_like(q)
+                fp.attn_tree(kv, paged._chunk(lens, tab, loose=loose)[0], parent, qr, o)
+                res.append(o)
+        fp.kv_keep(kv, paged._chunk(lens, tab)[0], _int([[0, 3, 5, 6]] * 4), _int([4, 3, 2, 4]))
+        tab = tab.cuda()
+        fp.beam_reorder(kv, tab, _int([700] * 4), _int([[1, 1, 0, 1]]))
+        out.append(res + held(kv, at) + [torch.where(tab >= 0, tab - at, -1).int()])
+    for a, b in zip(*out):
+        assert torch.equal(ref.bits(a.cpu()), ref.bits(b.cpu()))
