@@ -123,50 +123,60 @@ __global__ void __launch_bounds__(PLAN_T) attn_plan_kernel(AttnChunkArgs a) {
     }
 }
 
-// Joins the pieces of split tiles: RPW rows of a tile per workgroup, a thread per four dims of a row.
-// Pieces' statistics and outputs load eight at a time.
+// Joins the pieces of split tiles: RPW rows of a tile at a time, a thread per four dims of a row.  Pieces' statistics and
+// outputs load GRP at a time.  Wide tiles, whose pieces are two or three, four times per workgroup (each has to find its tile first)
+// and without a branch around a load (48 sequences of up to 3000, 14 nodes, 64 heads on 8, int8: with its attention 98.5 us, so 94.5;
+// 32 of up to 8192, 16 nodes 141, 138).
+constexpr int join_reps(int tile) { return tile & WIDE ? 4 : 1; }
 template <int D, int TILE>
 __global__ void __launch_bounds__(256) attn_chunk_join_kernel(AttnChunkArgs a) {
-    constexpr int RT = tile_size(TILE), RPW = 1024 / D, NS = RT / RPW;         // rows per workgroup; workgroups per tile
+    constexpr bool ALL = (TILE & WIDE) != 0;
+    constexpr int RT = tile_size(TILE), RPW = 1024 / D, REP = join_reps(TILE), GRP = ALL ? 4 : 8;
     const int nkv = a.kv.n_kv_heads, G = a.n_heads / nkv;
     Unit un;
     if (!find_unit<TILE, true, false>(a, G, un)) return;
     const int rows = min(RT, un.sq.n * G - un.rt * RT);
-    const int c = blockIdx.y * RPW + threadIdx.x / (D / 4), d0 = threadIdx.x % (D / 4) * 4;
-    static_assert(NS * RPW == RT, "rows of a tile divide evenly");
-    if (c >= rows) return;
+    const int c0 = blockIdx.y * (RPW * REP) + threadIdx.x / (D / 4), d0 = threadIdx.x % (D / 4) * 4;
+    static_assert(RT % (RPW * REP) == 0, "rows of a tile divide evenly");
     const int tiles = (un.sq.n * G + RT - 1) / RT;
-    const float* src = a.ws + ((int64_t)un.part * RT + c) * wst(D);
     const int64_t step = (int64_t)tiles * RT * wst(D);
-    float m = M0, l = 0.f;
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int i0 = 0; i0 < un.pieces; i0 += 8) {
-        float mi[8], li[8];
-        f32x4 oi[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool on = i0 + j < un.pieces;
-            const float* p = src + (i0 + j) * step;
-            mi[j] = on ? p[D] : M0;
-            li[j] = on ? p[D + 1] : 0.f;
-            oi[j] = on ? *(const f32x4*)(p + d0) : f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < REP; ++k) {
+        const int c = c0 + k * RPW;
+        if (c >= rows) return;
+        const float* src = a.ws + ((int64_t)un.part * RT + c) * wst(D);
+        float m = M0, l = 0.f;
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int i0 = 0; i0 < un.pieces; i0 += GRP) {
+            float mi[GRP], li[GRP];
+            f32x4 oi[GRP];
+#pragma unroll
+            for (int j = 0; j < GRP; ++j) {
+                const bool on = i0 + j < un.pieces;
+                const float* p = src + (ALL ? min(i0 + j, un.pieces - 1) : i0 + j) * step;
+                const f32x2 ml = ALL || on ? *(const f32x2*)(p + D) : f32x2{M0, 0.f};
+                const f32x4 x = ALL || on ? *(const f32x4*)(p + d0) : f32x4{0.f, 0.f, 0.f, 0.f};
+                mi[j] = on ? ml.x : M0;
+                li[j] = on ? ml.y : 0.f;
+                oi[j] = on ? x : f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+            float mn = m;
+#pragma unroll
+            for (int j = 0; j < GRP; ++j) mn = fmaxf(mn, mi[j]);
+            const float f = __builtin_amdgcn_exp2f(m - mn);
+            l *= f;
+            o *= f;
+            m = mn;
+#pragma unroll
+            for (int j = 0; j < GRP; ++j) {
+                const float e = __builtin_amdgcn_exp2f(mi[j] - m);
+                l += li[j] * e;
+                o += oi[j] * e;
+            }
         }
-        float mn = m;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) mn = fmaxf(mn, mi[j]);
-        const float f = __builtin_amdgcn_exp2f(m - mn);
-        l *= f;
-        o *= f;
-        m = mn;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float e = __builtin_amdgcn_exp2f(mi[j] - m);
-            l += li[j] * e;
-            o += oi[j] * e;
-        }
+        const int rho = un.rt * RT + c;
+        store4(a.out + ((int64_t)(un.sq.row0 + rho / G) * a.n_heads + un.kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
     }
-    const int rho = un.rt * RT + c;
-    store4(a.out + ((int64_t)(un.sq.row0 + rho / G) * a.n_heads + un.kvh * G + rho % G) * D + d0, o * (1.f / l), a.out_fmt);
 }
 
 // Rows of a tile, by what a sequence can bring to a kv head and by the call's size: 64-row tiles times the blocks that
@@ -195,7 +205,7 @@ int tile_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
 }
 
 // The same for trees: as chunks, but 65 to 128 rows of 128 dims in calls that are large enough for tiles of 256 take those of
-// attn_wide.hip.  us, 64 heads on 8, 16 nodes of 32 sequences of up to 8192: bf16 149, in tiles of 256 225, of 64 216; int8 150, 279, of 32
+// attn_wide.hip.  us, 64 heads on 8, 16 nodes of 32 sequences of up to 8192: bf16 140, in tiles of 256 225, of 64 216; int8 143, 279, of 32
 // 202.  (256 rows and more, in pairs of such tiles or tiles of 256 made the same way: no faster than attn_tile.hip's, 8 sequences of up to 30001 with
 // 512 rows to a kv head, bf16 69 and 61 against 61.  48 rows: int8 183, in tiles of 32 94; bf16 161, in tiles of 64 134.)
 int tree_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
@@ -270,7 +280,7 @@ static hipError_t launch_wide(AttnChunkArgs a, hipStream_t st) {
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if ((e = launch_attn_wide(a, (unsigned)n, st)) != hipSuccess || split == 0) return e;
-    FP_LAUNCH((attn_chunk_join_kernel<D, RT>), dim3(split, 128 * D / 1024), dim3(256), 0, st, a);
+    FP_LAUNCH((attn_chunk_join_kernel<D, RT>), dim3(split, 128 * D / 1024 / join_reps(RT)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 
