@@ -9,6 +9,10 @@
 // other stores, takes the softmax of its last block and multiplies then.  One barrier a step (with one after each half, the waves
 // half a step apart: 32 sequences of 8192, 16 nodes, 64 heads on 8, int8 264 us, so 241; bf16 258 and 253).  Blocks pass
 // through registers into LDS, as 16-bit fragments (int8: codes times scales in fp16), loaded two steps before they are stored.
+//
+// Those 32 sequences with lengths spread up to 8192 (290 MB of int8 cache): 127 us, and 10 for the join.  A step of two blocks of keys takes
+// some 2300 cycles: 1030 of products on each SIMD, 1300 of LDS (a fragment serves the 32 rows of a wave, 128 KB a step, and
+// 32 KB stored), 200 vector instructions a wave; a unit's prologue and merge 12 us.
 #include <type_traits>
 
 #include "attn_stream.h"

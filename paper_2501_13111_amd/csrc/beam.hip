@@ -8,6 +8,9 @@
 // A block's candidates: of 64 groups of its ids (a lane's, of all waves) the n_best-th largest of the groups' maxima is
 // at most the n_best-th largest logit, as each of those groups has one as large.  What is not below it, some n_best to 2 n_best
 // logits unless many are equal, is collected and ranked by counting.  The merge bounds its entries by the lists' heads in the same way.
+//
+// 24 groups of 8 beams over 128000 ids, 16 best, some beams finished: 25 us for the rows (98 MB if none were, 3.9 TB/s), 9 for the merge. One
+// group of 4 over 32000: 5.0 + 6.5, both chains of latencies.
 #include "vocab.h"
 
 namespace fpk {
