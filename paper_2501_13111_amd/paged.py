@@ -51,6 +51,8 @@ def _tensor(t, dtype, name, shape=None, contiguous=True, device=None):
 _fn = {}
 # the current stream's handle without a Stream object (about a microsecond less a call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+# tensors on a device have initialised torch's side of it
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _call(name, device, stream, *args):
@@ -64,7 +66,7 @@ def _call(name, device, stream, *args):
         if stream.device != device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
         s = stream.cuda_stream
-    if torch.cuda.current_device() == device.index:
+    if _device() == device.index:
         rc = f(*args, s)
     else:
         with torch.cuda.device(device):
