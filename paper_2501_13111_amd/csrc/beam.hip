@@ -9,8 +9,8 @@
 // at most the n_best-th largest logit, as each of those groups has one as large.  What is not below it, some n_best to 2 n_best
 // logits unless many are equal, is collected and ranked by counting.  The merge bounds its entries by the lists' heads in the same way.
 //
-// 24 groups of 8 beams over 128000 ids, 16 best, some beams finished: 25 us for the rows (98 MB if none were, 3.9 TB/s), 9 for the merge. One
-// group of 4 over 32000: 5.0 + 6.5, both chains of latencies.
+// 24 groups of 8 beams over 128000 ids, 16 best, some beams finished: 25 us for the rows (98 MB if none were, 3.9 TB/s), 8 for the merge. One
+// group of 4 over 32000: 5.0 + 5.3, both chains of latencies.
 #include "vocab.h"
 
 namespace fpk {
@@ -180,8 +180,7 @@ __global__ void __launch_bounds__(NT, 8) rows_kernel(BeamArgs a, BeamPart* __res
     }
 }
 
-// ---- merge.  A workgroup per group.
-constexpr int MT = 1024;
+// ---- merge.  A workgroup of MT threads per group.
 constexpr int ENT = 1024;                  // entries that are ranked at once
 // A continuation as a number in their order: the larger score; of equal ones the lower beam, in it the larger logit, then the
 // lower id.
@@ -199,34 +198,37 @@ __device__ __forceinline__ Entry make_entry(double s, int b, float z, int id) {
 }
 
 // A chain of latencies: the lists' parts and heads are loaded together, and then all entries of the lists whose heads pass.
+template <int MT>
 __global__ void __launch_bounds__(MT) merge_kernel(BeamArgs a, int nb, const BeamPart* __restrict__ parts, const Cand* __restrict__ lists) {
     __shared__ Entry ent[ENT];
     __shared__ double tab[EXP_N], base[BEST], ps[MT];
     __shared__ uint64_t head[MT / 64][64];
     __shared__ float top[BEST], pm[MT];
     __shared__ int count, passed, won[MT / 64], pass[MT], length[MT];
-    __shared__ uint8_t taken[BEST * ((1 << 20) / BV)];
+    __shared__ uint8_t taken[BEST * ((1 << 20) / BV)], over[BEST];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = blockIdx.x, W = a.n_beams, K = a.n_best;
     const int64_t row0 = (int64_t)g * W;
     const int L = W * nb;
-    auto is_done = [&](int b) { return a.done != nullptr && a.done[row0 + b]; };
-    // the thread's first list: its part and its head (those of a finished beam's rows are not written)
-    const bool mine = tid < L && !is_done(tid / nb);
+    // the thread's first list, its part and its head (those of a finished beam's rows are not written, and not used), and the score of
+    // the wave's first beam
     BeamPart p0 = {0.0, -INFINITY, 0};
     Cand c0 = {0.f, 0};
-    if (mine) {
+    if (tid < L) {
         p0 = parts[row0 * nb + tid];
         c0 = lists[(row0 * nb + tid) * K];
     }
+    const float score = w < W ? a.scores[row0 + w] : 0.f;
+    for (int b = tid; b < W; b += MT) over[b] = a.done != nullptr && a.done[row0 + b] ? 1 : 0;
     exp_table(tab);
     ps[tid] = p0.sum;
     pm[tid] = p0.max;
     if (tid == 0) count = passed = 0;
     __syncthreads();
+    auto is_done = [&](int b) { return over[b] != 0; };
     // a row's sum: base + (z - m) is the score of a continuation (z - m first: of a row whose logits all are the type's
     // lowest value it is zero, and the sum's logarithm is not lost)
     for (int b = w; b < W; b += MT / 64) {
-        const float sc = a.scores[row0 + b];
+        const float sc = b == w ? score : a.scores[row0 + b];
         const bool done = is_done(b);
         float m = -INFINITY;
         double s = 0.0;
@@ -391,7 +393,12 @@ hipError_t launch_beam_select(const BeamArgs& a, hipStream_t st) {
     FP_LAUNCH(rows_kernel, dim3(nb, rows), dim3(NT), 0, st, a, parts, lists);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    FP_LAUNCH(merge_kernel, dim3(a.n_groups), dim3(MT), 0, st, a, nb, parts, lists);
+    // a merge is bound by what one CU's waves issue, idle ones too (us for both kernels, with 256, 512 and 1024 threads: 128
+    // entries 10.4, 10.7, 11.7; 1024 of 8 beams 13.5, 12.8, 13.8; 4096 35.9, 34.6, 35.0; 16384 34.4, 27.5, 26.6)
+    const int entries = a.n_beams * nb * a.n_best;
+    if (entries <= 512) FP_LAUNCH(merge_kernel<256>, dim3(a.n_groups), dim3(256), 0, st, a, nb, parts, lists);
+    else if (entries <= 8192) FP_LAUNCH(merge_kernel<512>, dim3(a.n_groups), dim3(512), 0, st, a, nb, parts, lists);
+    else FP_LAUNCH(merge_kernel<1024>, dim3(a.n_groups), dim3(1024), 0, st, a, nb, parts, lists);
     return hipGetLastError();
 }
 

@@ -42,7 +42,8 @@ def _select(logits, scores, done, K, eos=-1, pad=0, stride=None):
 
 
 @pytest.mark.parametrize("G,W,K,V", [(1, 1, 1, 1), (1, 1, 4, 3), (1, 4, 4, 32000), (3, 5, 9, 1000), (2, 1, 16, 4096), (2, 8, 16, 4097),
-                                     (70, 2, 3, 50), (1, 64, 64, 300), (1, 33, 64, 9001), (2, 3, 64, 20000), (4, 4, 1, 160001)])
+                                     (70, 2, 3, 50), (1, 64, 64, 300), (1, 33, 64, 9001), (2, 3, 64, 20000), (4, 4, 1, 160001),
+                                     (2, 64, 1, 32768), (2, 64, 4, 100000), (2, 16, 32, 70000)])
 def test_selection_matches(G, W, K, V):
     g = torch.Generator().manual_seed(G + W + K + V)
     logits = (2.5 * torch.randn(G, 1, V, generator=g) + torch.randn(G, W, V, generator=g))
