@@ -199,10 +199,16 @@ __global__ void __launch_bounds__(T, KV8 && !F32 ? 8 : 1) kv_append_paged_kernel
         for (int it = tid; it < D * PD; it += T)
             *(u32x4*)(dst + 16 * it) = *(const u32x4*)(vt + it / PD * VS + it % PD * 16);
     } else {
-        for (int it = tid; it < D * np; it += T) {
-            const int dim = it / np, slot = vt_slot(t0 + it % np);
-            if constexpr (KV8) dst[dim * VT_BLK + slot] = vt[dim * VS + slot];
-            else *(uint16_t*)(dst + 2 * (dim * VT_BLK + slot)) = *(const uint16_t*)(vt + dim * VS + 2 * slot);
+        // a thread's position stays the same: those of a dim take the next power of two of neighbouring threads (40 sequences' up to 27 rows,
+        // 8 heads of 128, int8, four layers and their move and read back: 52.8 us with a division for each element, 50.7)
+        int th = tid;
+        asm volatile("" : "+v"(th));                       // (computed above the loops this would cost them registers)
+        const int lg = np > 1 ? 32 - __builtin_clz(np - 1) : 0, i = th & ((1 << lg) - 1), slot = vt_slot(t0 + i);
+        if (i < np) {
+            for (int dim = th >> lg; dim < D; dim += T >> lg) {
+                if constexpr (KV8) dst[dim * VT_BLK + slot] = vt[dim * VS + slot];
+                else *(uint16_t*)(dst + 2 * (dim * VT_BLK + slot)) = *(const uint16_t*)(vt + dim * VS + 2 * slot);
+            }
         }
     }
 }
