@@ -159,7 +159,7 @@ __global__ void __launch_bounds__(64) beam_table_kernel(int page_size, ReorderAr
 // that goes elsewhere.  The workgroups of a (group, layer) take shares of its copies in turn: 32-position blocks of keys or of
 // values, eight 16-byte loads a thread in flight.  Whole blocks: what lies behind the last position may be anything.  Parents, table
 // and data are a chain of three latencies, so there are no more workgroups than run at a time.  16 groups of 8 beams, 4 layers, int8,
-// 121 MB in random pages: 27 us, 4.5 TB/s (one workgroup for each pair of blocks that might have to be copied 41; the eight loads
+// 121 MB in random pages: 26 us, 4.6 TB/s (one workgroup for each pair of blocks that might have to be copied 41; the eight loads
 // under a mask, each waiting for the one before, 58).
 template <int D, bool KV8>
 __global__ void __launch_bounds__(T) beam_copy_kernel(KvSet kvs, ReorderArgs a) {
