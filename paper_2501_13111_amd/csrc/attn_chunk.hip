@@ -204,14 +204,25 @@ int tile_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
     return blocks <= 8 || work <= (i8 ? 4096.0 : 2048.0) ? 32 : 64;
 }
 
-// The same for trees: as chunks, but 65 to 128 rows of 128 dims in calls that are large enough for tiles of 256 take those of
-// attn_wide.hip.  us, 64 heads on 8, 16 nodes of 32 sequences of up to 8192: bf16 140, in tiles of 256 225, of 64 216; int8 143, 279, of 32
-// 202.  (256 rows and more, in pairs of such tiles or tiles of 256 made the same way: no faster than attn_tile.hip's, 8 sequences of up to 30001 with
+// The same for trees: as chunks, but for 65 to 128 rows of 128 dims, a tree's most common number.  us, 64 heads on 8 (G: heads
+// of a group):
+//   Large calls take tiles of 128 (attn_wide.hip): 16 nodes of 32 sequences of up to 8192 bf16 140, in tiles of 256 225, of 64 216; int8
+// 143, 279, of 32 202.  So do those of whole tiles (nothing to join, and no room for pieces needed) that fill half of the CUs' tiles: 16
+// nodes of 32 sequences of 250 int8 22, in tiles of 64 37, of 32 30; of 16 sequences of 250 20, 17, 17.
+//   int8, less than half a tile a sequence: tiles of 32, which are no more than the rows need: 64 sequences of 2000 with up to 12 nodes, in wide
+// tiles 95, of 32 82; up to 16 after up to 8192, a little more than half, 142, 160.
+//   The rest: tiles of 32 instead of 64, which hold a CU each: 23 nodes of 17 sequences of up to 1777, G 4, int8 45, of 32 29;
+// bf16 42, 36.  Not bf16 calls whose tiles of 64 run at once: 4 sequences of 4000, 16 nodes, 28, 32.
+// (256 rows and more, in pairs of such tiles or tiles of 256 made the same way: no faster than attn_tile.hip's, 8 sequences of up to 30001 with
 // 512 rows to a kv head, bf16 69 and 61 against 61.  48 rows: int8 183, in tiles of 32 94; bf16 161, in tiles of 64 134.)
 int tree_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
     const int RT = tile_rows(kv, c, n_heads);
-    const int64_t R = (int64_t)std::min(c.max_new, c.n_rows) * (n_heads / kv.n_kv_heads);
-    return RT == TILE_ROWS && kv.head_dim == 128 && R <= 128 ? WIDE | 128 : RT;
+    const int64_t G = n_heads / kv.n_kv_heads, R = std::min(c.max_new, c.n_rows) * G, n_seqs = std::min(c.n_seqs, c.n_rows);
+    if (kv.head_dim != 128 || R <= 64 || R > 128) return RT;
+    const bool i8 = kv.format == FP_KV_INT8, half = c.n_rows * G >= 64 * n_seqs;
+    const bool whole = (c.max_len - 1) / VT_BLK < WHOLE<WIDE | 128>;
+    if (RT == TILE_ROWS ? half || !i8 : half && whole && c.n_rows * G * kv.n_kv_heads > 128 * 128) return WIDE | 128;
+    return i8 || 2 * n_seqs * kv.n_kv_heads > 256 ? 32 : RT;
 }
 
 // log2 of the workgroups that run at a time (those of few rows: a half more), and the least number of blocks
@@ -271,9 +282,9 @@ static hipError_t launch_wide(AttnChunkArgs a, hipStream_t st) {
     const int64_t nkv = a.kv.n_kv_heads, R = std::min<int64_t>(a.chunk.n_rows, (int64_t)a.chunk.n_seqs * a.chunk.max_new) * (a.n_heads / nkv);
     const int64_t tiles = std::min(R, R / 128 + a.chunk.n_seqs) * nkv, n = tiles + WIDE_PIECES + 8 * XCD_RUN;
     a.min_blocks = 32;
-    a.plan = (int*)(a.ws + (int64_t)WIDE_PIECES * 128 * wst(D));
     if (n > MAX_GRID) return hipErrorInvalidValue;
     const unsigned split = (a.chunk.max_len - 1) / VT_BLK < WHOLE<RT> ? 0u : (unsigned)std::min<int64_t>(tiles, WIDE_PIECES);
+    a.plan = (int*)(a.ws + (split > 0 ? (int64_t)WIDE_PIECES * 128 * wst(D) : 0));      // (whole tiles leave no pieces)
     hipError_t e;
     if (a.chunk.n_seqs > PLAN_LANES) {
         FP_LAUNCH(attn_plan_kernel<RT>, dim3(1), dim3(PLAN_T), 0, st, a);
@@ -286,8 +297,9 @@ static hipError_t launch_wide(AttnChunkArgs a, hipStream_t st) {
 
 template <int D, bool KV8>
 static hipError_t launch_d(const AttnChunkArgs& a, hipStream_t st) {
-    if (a.parent != nullptr && tree_rows(a.kv, a.chunk, a.n_heads) & WIDE) return launch_wide(a, st);
-    switch (tile_rows(a.kv, a.chunk, a.n_heads)) {
+    const int RT = a.parent != nullptr ? tree_rows(a.kv, a.chunk, a.n_heads) : tile_rows(a.kv, a.chunk, a.n_heads);
+    if (RT & WIDE) return launch_wide(a, st);
+    switch (RT) {
         case 16: return launch_rt<D, KV8, 16>(a, st);
         case 32: return launch_rt<D, KV8, 32>(a, st);
         case 64: return launch_rt<D, KV8, 64>(a, st);

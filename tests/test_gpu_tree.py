@@ -73,6 +73,27 @@ def test_attention_matches_the_reference(seqs, nkv, G, d, page, kvq, loose):
 
 
 @pytest.mark.parametrize("kvq", ["bf16", "int8"])
+@pytest.mark.parametrize("n_seqs,nkv,G,nodes", [(20, 8, 8, 16), (300, 1, 8, 16), (12, 4, 4, 32), (70, 4, 8, 9), (300, 1, 4, 17)])
+def test_many_short_sequences_with_65_to_128_rows(n_seqs, nkv, G, nodes, kvq):
+    """Contexts of up to 70: whole tiles of 128 rows, which leave no pieces, and of 32; up to and above 256 sequences.  The workspace is as
+    large as asked for and not a byte behind it is written."""
+    fp = _fp()
+    g = torch.Generator().manual_seed(n_seqs + nodes)
+    lens = [(int(torch.randint(0, 71, (1,), generator=g)), nodes - (b * 7 % 3 if b else 0)) for b in range(n_seqs)]
+    gg, pool, table = paged._case(lens, 32, nkv, 128, kvq, 23)
+    paged._fill(pool, table, lens, gg, upto=lambda c, n: c + n)
+    parent = _trees(g, lens)
+    chunk, starts = paged._chunk(lens, table)
+    q = torch.randn(starts[-1], nkv * G, 128, generator=g).bfloat16()
+    kv, out = pool.device(), torch.empty(q.shape, dtype=torch.bfloat16).cuda()
+    n = fp.attn_chunk_workspace(kv, chunk, starts[-1], nkv * G).numel()
+    room = torch.full((n + 4096,), 0xAB, dtype=torch.uint8).cuda()
+    fp.attn_tree(kv, chunk, _int(parent), q.cuda(), out, workspace=room[:n])
+    _check(pool, table, lens, parent, q, out, fp16=kvq == "int8", floor=2.0 ** -25 if kvq == "int8" else 0.0)
+    assert (room[n:] == 0xAB).all()
+
+
+@pytest.mark.parametrize("kvq", ["bf16", "int8"])
 @pytest.mark.parametrize("nkv,G,page", [(2, 8, 64), (1, 16, 32), (3, 5, 96), (1, 2, 256)])
 @pytest.mark.parametrize("seqs", ["one", "edge", "split", "ragged"])
 def test_tiles_of_128_rows(seqs, nkv, G, page, kvq):
