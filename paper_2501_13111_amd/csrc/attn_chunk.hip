@@ -204,25 +204,33 @@ int tile_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
     return blocks <= 8 || work <= (i8 ? 4096.0 : 2048.0) ? 32 : 64;
 }
 
-// The same for trees: as chunks, but for 65 to 128 rows of 128 dims, a tree's most common number.  us, 64 heads on 8 (G: heads
-// of a group):
-//   Large calls take tiles of 128 (attn_wide.hip): 16 nodes of 32 sequences of up to 8192 bf16 140, in tiles of 256 225, of 64 216; int8
-// 143, 279, of 32 202.  So do those of whole tiles (nothing to join, and no room for pieces needed) that fill half of the CUs' tiles: 16
-// nodes of 32 sequences of 250 int8 22, in tiles of 64 37, of 32 30; of 16 sequences of 250 20, 17, 17.
-//   int8, less than half a tile a sequence: tiles of 32, which are no more than the rows need: 64 sequences of 2000 with up to 12 nodes, in wide
-// tiles 95, of 32 82; up to 16 after up to 8192, a little more than half, 142, 160.
+// The same for trees: as chunks, but for more than 64 rows of 128 dims.  us, 64 heads on 8 (G: heads of a group):
+//   65 to 128 rows, a tree's most common number, take tiles of 128 (attn_wide.hip) in large calls: 16 nodes of 32 sequences of up to 8192
+// bf16 140, in tiles of 256 225, of 64 216; int8 143, 279, of 32 202.  int8 only with at least half a tile a sequence (64 sequences of
+// 2000 with up to 12 nodes, in tiles of 128 95, of 32 82; up to 16 after up to 8192, a little more than half, 142, 160).
+//   Whole tiles of 128 (nothing to join, no room for pieces needed) where they fill half of the CUs: 16 nodes of 32 sequences of 250, int8
+// 22, in tiles of 64 37, of 32 30; of 16 sequences 20, 17, 17.  With more than 128 rows, above 8 blocks: 32 nodes of 16 sequences of 500, int8
+// 26, in tiles of 256 48; and, more of them than run at once, where sequences have fewer rows than the most: up to 32 nodes of 64 sequences of 900 92,
+// in tiles of 256 115; 32 nodes of each 109, 119; bf16 104, 99; 20 of 64 of 300 int8 70, 58.
 //   The rest: tiles of 32 instead of 64, which hold a CU each: 23 nodes of 17 sequences of up to 1777, G 4, int8 45, of 32 29;
-// bf16 42, 36.  Not bf16 calls whose tiles of 64 run at once: 4 sequences of 4000, 16 nodes, 28, 32.
-// (256 rows and more, in pairs of such tiles or tiles of 256 made the same way: no faster than attn_tile.hip's, 8 sequences of up to 30001 with
-// 512 rows to a kv head, bf16 69 and 61 against 61.  48 rows: int8 183, in tiles of 32 94; bf16 161, in tiles of 64 134.)
+// bf16 42, 36; up to 32 of 8 of 900, int8 41, 28.  Not bf16 calls whose tiles of 64 run at once: 4 sequences of 4000, 16 nodes, 28, 32.
+// (Long contexts with 256 rows and more, in pairs of tiles of 128 or tiles of 256 made the same way: no faster than attn_tile.hip's, 8 sequences
+// of up to 30001 with 512 rows to a kv head, bf16 69 and 61 against 61.  48 rows: int8 183, in tiles of 32 94; bf16 161, in tiles of 64 134.)
 int tree_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
-    const int RT = tile_rows(kv, c, n_heads);
+    const int RT = tile_rows(kv, c, n_heads), blocks = (c.max_len - 1) / VT_BLK + 1;
     const int64_t G = n_heads / kv.n_kv_heads, R = std::min(c.max_new, c.n_rows) * G, n_seqs = std::min(c.n_seqs, c.n_rows);
-    if (kv.head_dim != 128 || R <= 64 || R > 128) return RT;
+    if (kv.head_dim != 128 || R <= 64) return RT;
     const bool i8 = kv.format == FP_KV_INT8, half = c.n_rows * G >= 64 * n_seqs;
-    const bool whole = (c.max_len - 1) / VT_BLK < WHOLE<WIDE | 128>;
-    if (RT == TILE_ROWS ? half || !i8 : half && whole && c.n_rows * G * kv.n_kv_heads > 128 * 128) return WIDE | 128;
-    return i8 || 2 * n_seqs * kv.n_kv_heads > 256 ? 32 : RT;
+    const bool whole = blocks <= WHOLE<WIDE | 128> && c.n_rows * G * kv.n_kv_heads > 128 * 128;
+    if (R > 128) {
+        const bool ragged = 4 * (int64_t)c.n_rows < 3 * n_seqs * c.max_new, at_once = (R + 127) / 128 * n_seqs * kv.n_kv_heads <= 256;
+        if (whole && blocks > 8 && (RT != TILE_ROWS || ragged || at_once)) return WIDE | 128;
+        if (RT == TILE_ROWS) return RT;
+    } else {
+        if (half && (whole || RT == TILE_ROWS)) return WIDE | 128;
+        if (RT == TILE_ROWS) return i8 ? 32 : WIDE | 128;
+    }
+    return i8 || (R + 63) / 64 * n_seqs * kv.n_kv_heads > 256 ? 32 : RT;
 }
 
 // log2 of the workgroups that run at a time (those of few rows: a half more), and the least number of blocks

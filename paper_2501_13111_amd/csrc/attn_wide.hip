@@ -1,4 +1,5 @@
-// Attention of drafted trees that bring 65 to 128 rows to a kv head of 128 dims: tiles of 128 rows, eight waves of 32 rows each.
+// Attention of drafted trees that bring 65 to 128 rows to a kv head of 128 dims, or more of them over short contexts: tiles of 128 rows,
+// eight waves of 32 rows each.
 // (Tiles of 256, attn_tile.hip, leave half of their waves without rows; tiles of 64 and 32 read and unpack the cache
 // several times.)
 //

@@ -73,13 +73,15 @@ def test_attention_matches_the_reference(seqs, nkv, G, d, page, kvq, loose):
 
 
 @pytest.mark.parametrize("kvq", ["bf16", "int8"])
-@pytest.mark.parametrize("n_seqs,nkv,G,nodes", [(20, 8, 8, 16), (300, 1, 8, 16), (12, 4, 4, 32), (70, 4, 8, 9), (300, 1, 4, 17)])
-def test_many_short_sequences_with_65_to_128_rows(n_seqs, nkv, G, nodes, kvq):
-    """Contexts of up to 70: whole tiles of 128 rows, which leave no pieces, and of 32; up to and above 256 sequences.  The workspace is as
+@pytest.mark.parametrize("n_seqs,nkv,G,nodes", [(20, 8, 8, 16), (300, 1, 8, 16), (12, 4, 4, 32), (70, 4, 8, 9), (300, 1, 4, 17),
+                                                      (24, 3, 8, 40)])
+def test_many_short_sequences_with_more_than_64_rows(n_seqs, nkv, G, nodes, kvq):
+    """Short contexts: whole tiles of 128 rows, which leave no pieces, and of 32; up to and above 256 sequences.  The workspace is as
     large as asked for and not a byte behind it is written."""
     fp = _fp()
     g = torch.Generator().manual_seed(n_seqs + nodes)
-    lens = [(int(torch.randint(0, 71, (1,), generator=g)), nodes - (b * 7 % 3 if b else 0)) for b in range(n_seqs)]
+    far = 300 if nodes == 40 else 71                            # (more than 128 rows, above 8 blocks)
+    lens = [(int(torch.randint(0, far, (1,), generator=g)), nodes - (b * 7 % 3 if b else 0)) for b in range(n_seqs)]
     gg, pool, table = paged._case(lens, 32, nkv, 128, kvq, 23)
     paged._fill(pool, table, lens, gg, upto=lambda c, n: c + n)
     parent = _trees(g, lens)
