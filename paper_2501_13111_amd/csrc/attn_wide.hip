@@ -347,17 +347,15 @@ __global__ void __launch_bounds__(512, 2) attn_wide_kernel(AttnChunkArgs a) {
     int any = 0;
 #pragma unroll
     for (int x = 0; x < 8; ++x) any |= lds.sw[x];
-    // a row's factors once, by a thread: of its two sums, and the whole's reference and sum
-    float m = M0, l = 0.f;
+    // a row's factors once, by a thread: of its two sums, and the whole's reference and sum.  (1 / l comes last, strays or not: rows
+    // that see none of them keep their bits.)
     if (tid < RT) {
-        const float m0 = lds.mw[tid], m1 = lds.mw[RT + tid];
-        m = fmaxf(m0, m1);
+        const float m0 = lds.mw[tid], m1 = lds.mw[RT + tid], m = fmaxf(m0, m1);
         const float e0 = __builtin_amdgcn_exp2f(m0 - m), e1 = __builtin_amdgcn_exp2f(m1 - m);
-        l = lds.lw[tid] * e0 + lds.lw[RT + tid] * e1;
-        const float f = un.pieces == 1 && !any ? 1.f / l : 1.f;
-        lds.mw[tid] = e0 * f;
-        lds.mw[RT + tid] = e1 * f;
-        lds.lw[tid] = l;
+        const float l = lds.lw[tid] * e0 + lds.lw[RT + tid] * e1;
+        lds.mw[tid] = e0;
+        lds.mw[RT + tid] = e1;
+        lds.lw[tid] = 1.f / l;
         if (un.pieces > 1 && tid < rows) *(f32x2*)(a.ws + ((int64_t)un.part * RT + tid) * wst(D) + D) = f32x2{m, l};
     }
     __syncthreads();
@@ -375,8 +373,7 @@ __global__ void __launch_bounds__(512, 2) attn_wide_kernel(AttnChunkArgs a) {
             }
         }
         if (un.pieces == 1) {
-            if (any) x *= 1.f / lds.lw[c];
-            store4(a.out + ((int64_t)(sq.row0 + r / G) * a.n_heads + kvh * G + r % G) * D + d0, x, a.out_fmt);
+            store4(a.out + ((int64_t)(sq.row0 + r / G) * a.n_heads + kvh * G + r % G) * D + d0, x * lds.lw[c], a.out_fmt);
         } else {
             *(f32x4*)(a.ws + ((int64_t)un.part * RT + c) * wst(D) + d0) = x;
         }

@@ -225,6 +225,8 @@ def test_long_attention(nkv, G, d, page, kvq, lens, loose):
     (2, 4, 64, 0, [(70, 40), (0, 33), (31, 64)], [5, 7, 50]), (2, 4, 64, 32, [(70, 40), (0, 33), (31, 64)], [5, 7, 50]),
     (1, 8, 128, 0, [(70, 40), (0, 33), (31, 64)], [5, 7, 50]), (1, 8, 128, 32, [(70, 40), (0, 33), (31, 64)], [5, 7, 50]),
     (1, 8, 128, 32, [(70, 16), (0, 13), (31, 15)], [5, 7, 2]),
+    (8, 8, 128, 0, [(60, 16)] * 20, [1 + b % 14 for b in range(20)]),                    # whole tiles of 128 rows, one and three
+    (8, 8, 128, 0, [(290 - b, 40) for b in range(10)], [1 + 4 * b for b in range(9)] + [39]),
 ])
 def test_values_that_are_not_finite_reach_the_nodes_that_see_them(nkv, G, d, loose, lens, sick, kvq):
     """An infinite or NaN value (and a NaN key) of one node makes its descendants' outputs what they are, and changes no
