@@ -206,8 +206,8 @@ int tile_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
 
 // The same for trees: as chunks, but for more than 64 rows of 128 dims.  us, 64 heads on 8 (G: heads of a group):
 //   65 to 128 rows, a tree's most common number, take tiles of 128 (attn_wide.hip) in large calls: 16 nodes of 32 sequences of up to 8192
-// bf16 140, in tiles of 256 225, of 64 216; int8 143, 279, of 32 202.  int8 only with at least half a tile a sequence (64 sequences of
-// 2000 with up to 12 nodes, in tiles of 128 95, of 32 82; up to 16 after up to 8192, a little more than half, 142, 160).
+// bf16 140, in tiles of 256 225, of 64 216; int8 143, 279, of 32 202.  int8 with less than half a tile a sequence only above 96 blocks
+// (up to 12 nodes of 64 sequences of 2000, in tiles of 128 95, of 32 82; of 48 of up to 3000 94, 94; of 24 of up to 8192 96, 106).
 //   Whole tiles of 128 (nothing to join, no room for pieces needed) where they fill half of the CUs: 16 nodes of 32 sequences of 250, int8
 // 22, in tiles of 64 37, of 32 30; of 16 sequences 20, 17, 17.  With more than 128 rows, above 8 blocks: 32 nodes of 16 sequences of 500, int8
 // 26, in tiles of 256 48; and, more of them than run at once, where sequences have fewer rows than the most: up to 32 nodes of 64 sequences of 900 92,
@@ -228,7 +228,7 @@ int tree_rows(const fp_paged_kv& kv, const fp_chunk& c, int n_heads) {
         if (RT == TILE_ROWS) return RT;
     } else {
         if (half && (whole || RT == TILE_ROWS)) return WIDE | 128;
-        if (RT == TILE_ROWS) return i8 ? 32 : WIDE | 128;
+        if (RT == TILE_ROWS) return i8 && blocks <= 96 ? 32 : WIDE | 128;
     }
     return i8 || (R + 63) / 64 * n_seqs * kv.n_kv_heads > 256 ? 32 : RT;
 }
