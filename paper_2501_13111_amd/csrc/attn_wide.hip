@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(512, 2) attn_wide_kernel(AttnChunkArgs a) {
     };
     // From block `edge` on some node does not see every key: values there that are not finite are taken out (they would make
     // NaN of zero probabilities) and what they are to the rows that do see them is added at the end.  Positions past the
-    // sequence hold anything: zeros.
+    // sequence hold anything: zeros.  (A step's first block may lie before the edge: its values stay as they are.)
     const int edge = sq.ctx / VT_BLK - beg;
     bool strays = false;
     // LDS layout of a block (attn_tile.hip): keys in groups of 8 by 128 bytes of dims, chunk c of 16 bytes of key k at 1024 (4 (c / 8)
@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(512, 2) attn_wide_kernel(AttnChunkArgs a) {
     auto store = [&](char* slot, int s, const Raw& r, auto keys, auto past_edge) {
 #pragma unroll
         for (int j = 0; j < UPW; ++j) {
-            const bool key = KV8 ? decltype(keys)::value : j % 2 == 0, odd = decltype(past_edge)::value && !key;
+            const bool key = KV8 ? decltype(keys)::value : j % 2 == 0;
+            const bool odd = decltype(past_edge)::value && !key && s * KP + 8 * j / UPB >= edge;
             const int nk = sq.len - (beg + s * KP + 8 * j / UPB) * VT_BLK;
             char* const dst = slot + 8 * j / UPB * SB + (key ? 0 : NKC * 1024);
             uint32_t bad = 0;
