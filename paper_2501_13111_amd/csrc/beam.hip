@@ -69,7 +69,7 @@ __device__ __forceinline__ uint32_t kth_largest(uint32_t key, int k, int low) {
     return t;
 }
 
-// exp(z - m) for a sum that is off by some 1e-12, from a table whose entries lie in different banks of LDS.  NaN and -inf give 2^-900.
+// exp(z - m) from a table whose entries lie in different banks of LDS.  NaN and -inf give 2^-900.
 __device__ __forceinline__ double exp_near(float z, double m, const double* tab) {
     return exp2_series<32>(fmax(((double)z - m) * 1.44269504088896340736, -900.0), tab);
 }

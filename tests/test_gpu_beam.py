@@ -369,3 +369,29 @@ def test_beams_on_another_stream():
         assert torch.equal(ref.bits(a.cpu()), ref.bits(b.cpu()))
     with pytest.raises(ValueError, match="workspace"):
         fp.beam_select(z, s, os, op, oi, stream=st)
+
+
+def test_scores_that_differ_beyond_12_digits():
+    """Beams whose sums of exponentials differ by some 5e-13 of themselves are told apart, whichever comes first: a row of n logits
+    a below one of zero has log(1 + n e^a).  The roundings of such a sum of some thousand 64-bit numbers, of its 64-bit
+    exponentials and of its logarithm stay below 1e-14."""
+    from decimal import Decimal, localcontext
+    rows = [(1081, -2.3070878982543945, 1342, -2.523362398147583), (2162, -2.3503623008728027, 2684, -2.566636800765991),
+            (2829, -2.328671455383301, 1957, -1.9601608514785767), (3929, -2.3936831951141357, 1922, -1.6786645650863647),
+            (3929, -1.9387843608856201, 1922, -1.2237657308578491), (1081, -1.202321171760559, 1342, -1.4185956716537476)]
+    fp = _fp()
+    for V in (4096, 9001):
+        for n0, a0, n1, a1 in rows:
+            z = torch.full((1, 2, V), -math.inf)
+            for w, (n, a) in enumerate(((n0, a0), (n1, a1))):
+                z[0, w, :1] = 0.0
+                z[0, w, V - n:] = a
+            with localcontext() as c:
+                c.prec = 40
+                lse = [(1 + n * Decimal(float(z[0, w, -1])).exp()).ln() for w, n in enumerate((n0, n1))]
+            assert 4e-13 < lse[0] - lse[1] < 1e-12
+            for turn in (0, 1):
+                o, p, i = torch.empty(1, 2).cuda(), _int([[7, 7]]), _int([[7, 7]])
+                fp.beam_select((z.flip(1) if turn else z)[0].contiguous().cuda(), torch.zeros(1, 2).cuda(), o, p, i)
+                assert i.tolist() == [[0, 0]]
+                assert p.tolist() == ([[0, 1]] if turn else [[1, 0]]), (V, n0, a0, turn)
