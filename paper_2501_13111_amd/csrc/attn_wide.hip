@@ -11,9 +11,11 @@
 // half a step apart: 32 sequences of 8192, 16 nodes, 64 heads on 8, int8 264 us, so 241; bf16 258 and 253).  Blocks pass
 // through registers into LDS, as 16-bit fragments (int8: codes times scales in fp16), loaded two steps before they are stored.
 //
-// Those 32 sequences with lengths spread up to 8192 (290 MB of int8 cache): 127 us, and 10 for the join.  A step of two blocks of keys takes
-// some 2300 cycles: 1030 of products on each SIMD, 1300 of LDS (a fragment serves the 32 rows of a wave, 128 KB a step, and
-// 32 KB stored), 200 vector instructions a wave; a unit's prologue and merge 12 us.
+// Those 32 sequences with lengths spread up to 8192 (290 MB of int8 cache): 131 to 141 us with the join, by a kernel trace 135 and 10.6.
+// Lengths up to 2048, 4096, 16384 and 32768 take 57, 80, 237 and 454; all five fit, within 4 %, 1.3 us a step of two blocks of keys and 9 us a
+// unit of prologue and merge, which nothing covers (135 KB of LDS: one workgroup a CU, two units after each other), in the order in
+// which the units start: 85 steps on the busiest CU, where an even share is 64.  A step, some 2900 cycles, has 1030 of products on each SIMD, 1300 of LDS
+// (a fragment serves the 32 rows of a wave, 128 KB a step, and 32 KB stored) and 200 vector instructions a wave.
 #include <type_traits>
 
 #include "attn_stream.h"

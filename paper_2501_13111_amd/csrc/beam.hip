@@ -9,8 +9,8 @@
 // at most the n_best-th largest logit, as each of those groups has one as large.  What is not below it, some n_best to 2 n_best
 // logits unless many are equal, is collected and ranked by counting.  The merge bounds its entries by the lists' heads in the same way.
 //
-// 24 groups of 8 beams over 128000 ids, 16 best, some beams finished: 25 us for the rows (98 MB if none were, 3.9 TB/s), 8 for the merge. One
-// group of 4 over 32000: 5.0 + 5.3, both chains of latencies.
+// 24 groups of 8 beams over 128000 ids, 16 best, some beams finished: 25.7 us for the rows (78.5 MB of those that are not, 3.1 TB/s), 7.8 for the
+// merge.  One group of 4 over 32000: 5.1 + 5.4, both chains of latencies.
 #include "vocab.h"
 
 namespace fpk {

@@ -15,7 +15,8 @@ constexpr int T = 256;
 // of one layer per workgroup.  Every element is read before any is written, so a path may be any list of nodes.
 // Elements of a value lie 32 slots apart: neighbouring threads take the positions of one dim, whose slots
 // are one or two cache lines.  Bound by latency: lengths and path, pages, elements, one after another.  Paths of up to 7 of 40 sequences
-// on 8 heads of 128, four int8 layers: 5.8 us (5 MB in, 5 out); one path of 3 on 32 heads, two bf16 layers: 3.7.
+// on 8 heads of 128, four int8 layers: 6.1 us in a graph of them, 6.9 by a kernel trace (5 MB in, 5 out); one path of 3 on 32 heads, two bf16
+// layers: 3.9 and 4.7.
 template <int D, bool KV8>
 __global__ void __launch_bounds__(T) kv_keep_kernel(KvSet kvs, KvKeepArgs a) {
     constexpr int ES = KV8 ? 1 : 2, NP = D * ES / 16;      // 16-byte pieces of a key
@@ -57,7 +58,7 @@ __global__ void __launch_bounds__(T) kv_keep_kernel(KvSet kvs, KvKeepArgs a) {
         if (i < n && from[i] >= 0)
             k[x] = *(const u32x4*)((const char*)kv.k + ((int64_t)from[i] * VT_BLK + (at[i] >> 8)) * D * ES + 16 * (it % NP));
     }
-    // eight at a time: most paths are short (the same 6.8 and 4.4 us if every turn asks for itself)
+    // eight at a time: most paths are short (in a graph 1.0 and 0.7 us less than if every turn asks for itself)
 #pragma unroll
     for (int x0 = 0; x0 < VX; x0 += 8) {
         if (T * x0 >= n * D) break;

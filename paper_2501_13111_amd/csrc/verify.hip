@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(NT) pick_kernel(VerifyArgs a, int nb, const do
 //   draw_kernel   per row: the block that holds the draw by the blocks' sums, then the id in it
 //   walk_kernel   per sequence, one wave, lane i its node i (T = 0: a node's token is its row's maximum)
 //
-// 16 trees of up to 48 nodes (383 rows) over 32000 ids, T = 0.8: 14.6 us for the rows (49 MB, 3.4 TB/s), 7 for the draws, each a chain of
-// the blocks' sums, the ids of one block and two joins over its waves, and 2 to 4 for the walks.  One tree of 8 nodes, T = 0: 3.5 + 2.5.
+// 16 trees of up to 48 nodes (383 rows) over 32000 ids, T = 0.8: 15 us for the rows (49 MB, 3.2 TB/s), 7 for the draws, each a chain of
+// the blocks' sums, the ids of one block and two joins over its waves, and 2.5 for the walks.  One tree of 8 nodes, T = 0: 3.9 + 2.5.
 
 constexpr int DT = 1024, DPT = VB / DT;     // threads of a draw, ids of one
 __global__ void __launch_bounds__(DT) draw_kernel(VerifyArgs a, int nb, int* __restrict__ drawn) {
