@@ -441,8 +441,9 @@ fp_status fp_kv_keep(const fp_paged_kv* kv, int32_t n_layers, const fp_chunk* ch
  * The n_best best of a group, in order (the larger score; of equal ones the lower beam, in it the larger logit, then the
  * lower id), go to out_scores (fp32), out_parent (int32, the beam), out_ids (int32) and, unless NULL, out_finished (uint8: its beam was
  * finished or its id is eos_id; eos_id -1: no id is), all [n_groups, n_best]; where there are fewer, -inf, -1, -1 and 0.
- * Sums and comparisons are in 64 bits; a sum of exponentials is off by some 3e-15 of itself.  -inf and NaN logits are no continuation, +inf ones share the whole; a beam of
- * score -inf or NaN has none.  With n_beams 1 and n_best the beams to come, a request's first step.
+ * Sums and comparisons are in 64 bits; a sum of exponentials is off by less than 1e-14 of itself.  -inf and NaN logits are no
+ * continuation, +inf ones share the whole; a beam of score -inf or NaN has none.  With n_beams 1 and n_best the beams to come, a
+ * request's first step.
  * 1 <= n_beams, n_best <= 64, n_groups * n_beams <= 65535, 1 <= vocab <= 2^20.  Outputs overlap neither
  * inputs nor each other.
  */
